@@ -1,7 +1,8 @@
 """Builds, in-tree, libcpattn.so (the attention step: HIP kernels + C ABI,
 gfx950, hipcc), libcplayer.so (the element-wise kernels of the decoder layer
-around it, gfx950), libcppeaks.so (peak-rate microbenchmarks, gfx950) and
-libcpsched.so (the host scheduler, plain C++17, g++)."""
+around it, gfx950), libcptree.so (drafted trees and forks over the cache, gfx950),
+libcppeaks.so (peak-rate microbenchmarks, gfx950) and libcpsched.so (the host
+scheduler, plain C++17, g++)."""
 
 from __future__ import annotations
 
@@ -18,6 +19,8 @@ LIB = os.path.join(PKG, "libcpattn.so")
 SCHED_LIB = os.path.join(PKG, "libcpsched.so")
 LAYER_LIB = os.path.join(PKG, "libcplayer.so")
 LAYER_SOURCES = ["layer.hip", "gemm.hip"]
+TREE_LIB = os.path.join(PKG, "libcptree.so")
+TREE_SOURCES = ["tree_api.hip", "tree_attn.hip", "tree_ops.hip"]
 PEAKS_LIB = os.path.join(PKG, "libcppeaks.so")
 PEAKS_SOURCES = ["peaks.hip"]
 CXX = os.environ.get("CXX", "g++")
@@ -46,11 +49,14 @@ def _compile(src: str) -> str:
 def build(jobs: int = 8) -> str:
     os.makedirs(BUILD, exist_ok=True)
     with cf.ThreadPoolExecutor(max_workers=jobs) as ex:
-        objs = list(ex.map(_compile, SOURCES + LAYER_SOURCES + PEAKS_SOURCES))
+        objs = list(ex.map(_compile, SOURCES + LAYER_SOURCES + TREE_SOURCES + PEAKS_SOURCES))
     n1, n2 = len(SOURCES), len(SOURCES) + len(LAYER_SOURCES)
+    n3 = n2 + len(TREE_SOURCES)
     _link(objs[:n1], LIB)
     _link(objs[n1:n2], LAYER_LIB)
-    _link(objs[n2:], PEAKS_LIB)
+    # the rows' checks are the attention library's own, linked in
+    _link(objs[n2:n3] + [objs[SOURCES.index("plan.cpp")]], TREE_LIB)
+    _link(objs[n3:], PEAKS_LIB)
     build_sched()
     return LIB
 
