@@ -2,6 +2,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <climits>
 #include <cstdlib>
 #include <new>
 #include <vector>
@@ -10,6 +11,7 @@
 #include "plan.hpp"
 #include "tree_attn.hpp"
 #include "tree_ops.hpp"
+#include "tree_plan.hpp"
 
 using namespace cptree;
 
@@ -129,6 +131,34 @@ int by_node_rows(const cp_row_meta* rows, int32_t n_rows, F&& f) {
   return CP_OK;
 }
 
+// f(rows of one launch, its workgroups) for rows in batches; items_of(row) is
+// the number of a row's workgroups.
+template <class Items, class F>
+int by_tree_rows(const std::vector<TreeRow>& rows, Items&& items_of, F&& f) {
+  for (size_t r0 = 0; r0 < rows.size(); r0 += kTreeRows) {
+    TreeRows batch;
+    int items = 0;
+    for (int i = 0; i < kTreeRows; ++i) {
+      if (r0 + i >= rows.size()) {  // no workgroup's
+        batch.r[i] = TreeRow{0, 0, 0, 0, INT_MAX, 1, 0, 0};
+        continue;
+      }
+      batch.r[i] = rows[r0 + i];
+      batch.r[i].item0 = items;
+      items += items_of(rows[r0 + i]);
+    }
+    const int rc = f(batch, items);
+    if (rc != CP_OK) return rc;
+  }
+  return CP_OK;
+}
+
+// One plan per thread, whose vectors keep their capacity.
+TreePlan& thread_plan() {
+  thread_local TreePlan p;
+  return p;
+}
+
 int check_forks(const cp_attn_desc* d, const cp_fork* forks, int32_t n_forks) {
   const int64_t cap = (int64_t)d->max_blocks_per_req * d->block_size;
   std::vector<int32_t> src, dst, fresh;
@@ -186,10 +216,17 @@ int cp_tree_layout(const int32_t* parents, const cp_row_meta* rows, int32_t n_ro
 
 size_t cp_tree_attn_workspace_bytes(const cp_attn_desc* desc, const cp_row_meta* rows,
                                     int32_t n_rows) {
-  int64_t tokens = 0;
-  if (guarded([&] { return check_geometry(desc, rows, n_rows, kMaxNodes, &tokens); }) != CP_OK)
-    return 0;
-  return 256;
+  size_t bytes = 0;
+  const int rc = guarded([&] {
+    int64_t tokens = 0;
+    const int e = check_geometry(desc, rows, n_rows, kMaxNodes, &tokens);
+    if (e != CP_OK) return e;
+    TreePlan& p = thread_plan();
+    plan_tree(*desc, rows, n_rows, p);
+    bytes = p.ws_bytes;
+    return CP_OK;
+  });
+  return rc == CP_OK ? bytes : 0;
 }
 
 int cp_tree_attn(const cp_attn_desc* desc, const void* q, const void* k_cache,
@@ -205,32 +242,47 @@ int cp_tree_attn(const cp_attn_desc* desc, const void* q, const void* k_cache,
         !aligned(k_cache, 16) || !aligned(v_cache, 16) || !aligned(out, 16) ||
         !aligned(block_tables, 4) || !aligned(mask, 8) || !aligned(ws, 256))
       return CP_ERR_INVALID_ARG;
-    if (ws_bytes < cp_tree_attn_workspace_bytes(desc, rows, n_rows)) return CP_ERR_WORKSPACE;
+    TreePlan& p = thread_plan();
+    plan_tree(*desc, rows, n_rows, p);
+    if (ws_bytes < p.ws_bytes) return CP_ERR_WORKSPACE;
     hipStream_t s = (hipStream_t)stream;
     rc = check_tables(desc, block_tables, rows, n_rows, false, s);
     if (rc != CP_OK) return rc;
     (void)hipGetLastError();
-    const AttnArgs a{static_cast<const uint16_t*>(q), static_cast<const uint16_t*>(k_cache),
-                     static_cast<const uint16_t*>(v_cache), block_tables, mask,
-                     static_cast<uint16_t*>(out), mask_words, desc->num_q_heads,
-                     desc->num_kv_heads, desc->max_blocks_per_req,
+    const int group = desc->num_q_heads / desc->num_kv_heads;
+    const AttnArgs a{static_cast<const uint16_t*>(q),
+                     static_cast<const uint16_t*>(k_cache),
+                     static_cast<const uint16_t*>(v_cache),
+                     block_tables,
+                     mask,
+                     static_cast<uint16_t*>(out),
+                     static_cast<float*>(ws),
+                     reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + p.off_lse),
+                     mask_words,
+                     desc->num_q_heads,
+                     desc->num_kv_heads,
+                     desc->max_blocks_per_req,
+                     __builtin_ctz(group),
                      desc->sm_scale * cpattn::kLog2e};
-    int32_t tok = 0;
-    for (int32_t r = 0; r < n_rows;) {
-      TreeRows batch;
-      int n = 0, items = 0;
-      for (; r < n_rows && n < kTreeRows; ++r) {
-        if (rows[r].chunk_len == 0) continue;
-        batch.r[n++] = TreeRow{tok, rows[r].chunk_len, rows[r].chunk_start, rows[r].req_id,
-                               items, 1, 0, 0};
-        items += rows[r].chunk_len;
-        tok += rows[r].chunk_len;
-      }
-      if (n == 0) break;
-      rc = finish(launch_attn(desc->head_dim, desc->block_size, a, batch, n, items, s), s);
-      if (rc != CP_OK) return rc;
-    }
-    return CP_OK;
+    const int d = desc->head_dim;
+    rc = by_tree_rows(
+        p.narrow,
+        [&](const TreeRow& t) {
+          return t.n_split * desc->num_kv_heads * narrow_tiles(t.n * group, p.narrow_rows);
+        },
+        [&](const TreeRows& batch, int items) {
+          return finish(launch_narrow(d, desc->block_size, p.narrow_rows, a, batch, items, s), s);
+        });
+    if (rc != CP_OK) return rc;
+    return by_tree_rows(
+        p.merge,
+        [&](const TreeRow& t) {
+          const int per = merge_rows(d, t.n_split);
+          return (t.n * desc->num_q_heads + per - 1) / per;
+        },
+        [&](const TreeRows& batch, int items) {
+          return finish(launch_tree_merge(d, a, batch, items, s), s);
+        });
   });
 }
 

@@ -1,92 +1,444 @@
 // Attention of drafted trees over the paged cache (include/cp_tree.h).
+//
+// With n nodes and G q heads per kv head, n G rows share every K and V that
+// is read.  Over c committed keys the work is 4 D n G c flop on 4 D c bytes per
+// kv head, n G flop a byte: up to some 150 rows the stream of K and V bounds
+// it, above that the matrix cores.
+//
+// Softmax runs in base 2, over one pass of the keys, with a running maximum
+// that moves lazily (a score has to exceed it by 2^8) and fp32 sums of the
+// weights as they were rounded to bf16 for the product with V.  Masks cost
+// nothing until the keys of the tree itself, the last ones of a row.
 #include "tree_attn.hpp"
 
 #include "device.hpp"
+#include "tree_plan.hpp"
 
 namespace cptree {
 
-using cpattn::bf16hi;
-using cpattn::bf16lo;
+using cpattn::bf16x8_t;
+using cpattn::dot2_bf16;
+using cpattn::f32x4_t;
+using cpattn::kRescaleThreshold;
+using cpattn::ld_global16;
+using cpattn::ld_global16_nt;
+using cpattn::pack_bf16x2;
+using cpattn::shfl_xor_f;
 using cpattn::to_bf16;
-using cpattn::wave_max;
-using cpattn::wave_sum;
+using cpattn::u32x4_t;
 
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kWaves = kThreads / 64;
 
-// One workgroup per (node, q head), 256 keys at a time: a thread scores one
-// key, the chunk's weights meet in LDS, and a thread then sums one feature's
-// values over half the chunk.  Keys without weight are not multiplied.
+__device__ __forceinline__ f32x4_t mfma16x16x32(uint4 a, uint4 b, f32x4_t c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a),
+                                                 __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
+}
+
+// The row whose workgroups item b belongs to: as many rows begin at or before
+// it as lanes say so (every lane of a wave looks at two rows).
+__device__ __forceinline__ TreeRow row_of(const TreeRows& rows, int b) {
+  static_assert(kTreeRows > 64 && kTreeRows <= 128, "two rows per lane");
+  const int lane = threadIdx.x & 63;
+  const bool lo = rows.r[lane].item0 <= b;
+  const bool hi = 64 + lane < kTreeRows && rows.r[min(64 + lane, kTreeRows - 1)].item0 <= b;
+  const int n = __popcll(__builtin_amdgcn_ballot_w64(lo)) +
+                __popcll(__builtin_amdgcn_ballot_w64(hi));
+  return rows.r[__builtin_amdgcn_readfirstlane(n - 1)];
+}
+
+// Bit b: whether a node with this mask sees the key at offset o + b of its
+// row's tree (negative offsets are committed keys, o > -32).
+__device__ __forceinline__ uint32_t seen32(const uint64_t* mask, int words, int n, int o) {
+  if (o >= n) return 0;
+  const int at = max(o, 0), w = at >> 6, sh = at & 63;
+  uint64_t x = mask[w] >> sh;
+  if (sh > 32 && w + 1 < words) x |= mask[w + 1] << (64 - sh);
+  if (n - at < 32) x &= (1u << (n - at)) - 1;
+  return o >= 0 ? (uint32_t)x : (uint32_t)x << -o | ((1u << -o) - 1);
+}
+
+// Whether a bf16 is an infinity or NaN, for both halves of a word.
+__device__ __forceinline__ bool bad_lo(uint32_t w) { return (w & 0x7f80u) == 0x7f80u; }
+__device__ __forceinline__ bool bad_hi(uint32_t w) { return (w & 0x7f800000u) == 0x7f800000u; }
+
+// What the infinite or NaN values of nodes in `bad` that a node with this mask
+// sees add to feature d of its output.
 template <int D, int B>
-__global__ __launch_bounds__(kThreads) void tree_attn_kernel(const TreeRows rows, int n_rows,
-                                                             const AttnArgs a) {
-  __shared__ float s_q[D], s_p[kThreads], s_red[4], s_o[kThreads];
-  const int tid = threadIdx.x, h = blockIdx.y;
-  int r = 0;
-  while (r + 1 < n_rows && rows.r[r + 1].item0 <= (int)blockIdx.x) ++r;
-  const TreeRow row = rows.r[r];
-  const int64_t t = row.tok0 + (int)blockIdx.x - row.item0;
-  const int kvh = h / (a.hq / a.hkv);
-  if (tid < D) s_q[tid] = __uint_as_float((uint32_t)a.q[(t * a.hq + h) * D + tid] << 16);
-  __syncthreads();
-  const int32_t* bt = a.bt + (int64_t)row.req * a.mbr;
-  const int ctx = row.start + row.n, d = tid % D, part = tid / D;
-  float m = -INFINITY, l = 0.f, o = 0.f;
-  for (int k0 = 0; k0 < ctx; k0 += kThreads) {
-    const int key = k0 + tid, j = key - row.start;
-    bool seen = key < ctx;
-    if (seen && j >= 0) seen = (a.mask[t * a.words + (j >> 6)] >> (j & 63)) & 1;
-    float s = -INFINITY;
-    if (seen) {
-      const uint16_t* k =
-          a.k_cache + (((int64_t)bt[key / B] * a.hkv + kvh) * B + key % B) * D;
-      s = 0.f;
-      for (int c = 0; c < D / 8; ++c) {
-        const uint4 w = cpattn::ld_global16(k + c * 8);
-        const uint32_t x[4] = {w.x, w.y, w.z, w.w};
-        for (int e = 0; e < 4; ++e)
-          s += bf16lo(x[e]) * s_q[c * 8 + 2 * e] + bf16hi(x[e]) * s_q[c * 8 + 2 * e + 1];
-      }
-      s *= a.scale_log2;
+__device__ float bad_values(const uint64_t* bad, const uint64_t* mask, int words,
+                            const TreeRow& row, const int32_t* bt_row, const uint16_t* v_cache,
+                            int hkv, int kvh, int d) {
+  float sum = 0.f;
+  for (int w = 0; w < words; ++w)
+    for (uint64_t x = bad[w] & mask[w]; x; x &= x - 1) {
+      const int p = row.start + 64 * w + __ffsll((unsigned long long)x) - 1;
+      const uint32_t v =
+          v_cache[(((int64_t)bt_row[p / B] * hkv + kvh) * D + d) * B + p % B];
+      if (bad_lo(v)) sum += __uint_as_float(v << 16);
     }
-    const float top = wave_max(s);
-    if ((tid & 63) == 0) s_red[tid >> 6] = top;
-    __syncthreads();
-    const float mn = fmaxf(m, fmaxf(fmaxf(s_red[0], s_red[1]), fmaxf(s_red[2], s_red[3])));
-    const float alpha = m == -INFINITY ? 0.f : exp2f(m - mn);
-    m = mn;
-    s_p[tid] = seen ? exp2f(s - m) : 0.f;
-    __syncthreads();
-    o *= alpha;
-    l *= alpha;
-    for (int i = part; i < min(kThreads, ctx - k0); i += kThreads / D) {
-      const float p = s_p[i];
-      if (p == 0.f) continue;
-      l += p;
-      const int x = k0 + i;
-      const uint16_t v = a.v_cache[(((int64_t)bt[x / B] * a.hkv + kvh) * D + d) * B + x % B];
-      o += p * __uint_as_float((uint32_t)v << 16);
-    }
-    __syncthreads();
+  return sum;
+}
+
+// A workgroup takes up to 16 NC of a kv head's rows and a piece of the key range, of which wave w takes tiles of 32 keys w, w + 4, ...  The
+// rows are the columns of both products (v_mfma_f32_16x16x32_bf16, NC of them
+// per operand of K or V).  Per tile and wave, lane l = 16 g + i:
+//   S^T (2 x 16 keys x 16 NC rows) = K . Q^T.  Row i of key half b is key
+//     8 (i / 4) + 4 b + i % 4, so that lane (g, i) ends up with rows i's scores
+//     of keys 8 g .. 8 g + 7, the B operand of the second product: the
+//     weights never leave the lane.
+//   O^T (D x 16 NC rows) += V^T . P^T: lane (g, i) reads 8 consecutive keys of
+//     feature rows 16 dt + i, the A operand as the [D][B] blocks store it.
+// K and V are loaded as they lie in memory, K's rows passing through a slice
+// of LDS that only this wave uses.  K of the next tile is on its way from
+// there on, V from the end of a tile to the product with it in the next.  The
+// waves' states are combined in LDS, 16 rows at a time.
+//
+// V of the tree's own keys enters the product with infinities and NaN as
+// zeros: a node that does not see the key would get 0 * NaN from it.  The
+// nodes that do get them added at the end.
+template <int D, int B, int NC>
+__global__ __launch_bounds__(kThreads, NC <= 2 ? 2 : 1) void narrow_kernel(const TreeRows rows,
+                                                                           const AttnArgs a) {
+  constexpr int TK = 32;       // keys per tile
+  constexpr int NKS = D / 32;  // k-steps of a score
+  constexpr int NDT = D / 16;  // 16-feature blocks of the output
+  constexpr int SLICE = 16 * D * 4;  // bytes of a wave: 32 keys' rows, then 16 rows' output
+  __shared__ __align__(16) uint8_t slices[kWaves][SLICE];
+  __shared__ float s_m[kWaves][16], s_l[kWaves][16];
+  __shared__ unsigned long long s_bad[kMaxWords];
+
+  const TreeRow row = row_of(rows, blockIdx.x);
+  const int unit = (int)blockIdx.x - row.item0;
+  const int G = 1 << a.log2_group, m_rows = row.n << a.log2_group;
+  const int tiles = (m_rows + 16 * NC - 1) / (16 * NC), m0 = unit % tiles * 16 * NC;
+  const int kvh = unit / tiles % a.hkv, split = unit / tiles / a.hkv;
+  const int tid = threadIdx.x, lane = tid & 63, i = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int ctx = row.start + row.n;
+  const int kv_begin = split * row.split_keys, kv_end = min(ctx, kv_begin + row.split_keys);
+  if (tid < kMaxWords) s_bad[tid] = 0;
+
+  // column c's row of this lane, past the last one that again (not stored)
+  uint4 qv[NC][NKS];
+  auto row_at = [&](int c) { return min(m0 + 16 * c + i, m_rows - 1); };
+#pragma unroll
+  for (int c = 0; c < NC; ++c) {
+    const int x = row_at(c);
+    const int64_t t = row.tok0 + (x >> a.log2_group);
+    const uint16_t* qb = a.q + (t * a.hq + kvh * G + (x & (G - 1))) * D + g * 8;
+#pragma unroll
+    for (int ks = 0; ks < NKS; ++ks) qv[c][ks] = ld_global16(qb + ks * 32);
   }
-  s_o[tid] = o;
-  s_p[tid] = l;
-  __syncthreads();
-  if (tid >= D) return;
-  o = 0.f;
-  l = 0.f;
-  for (int i = tid; i < kThreads; i += D) o += s_o[i], l += s_p[i];
-  a.out[(t * a.hq + h) * D + tid] = to_bf16(l == 0.f ? 0.f : o / l);
+  __builtin_amdgcn_sched_barrier(0);
+
+  float m_run[NC], l_run[NC];
+  f32x4_t o[NC][NDT];
+#pragma unroll
+  for (int c = 0; c < NC; ++c) {
+    m_run[c] = -INFINITY, l_run[c] = 0.f;
+#pragma unroll
+    for (int dt = 0; dt < NDT; ++dt) o[c][dt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  }
+
+  const int64_t head_elems = (int64_t)B * D;
+  const int32_t* bt_row = a.bt + (int64_t)row.req * a.mbr;
+  const int n_tiles = (kv_end - kv_begin + TK - 1) / TK;
+  const int lb_last = (kv_end - 1) / B;
+  const int voff = i * B + (8 * g) % B;
+  const bool v_second = 8 * g >= B;
+  constexpr int CH = D / 8, KPL = 64 / CH;  // 16-byte chunks per K row, rows per load
+  constexpr int NKL = 16 / KPL;             // loads per half
+  const int krow = lane / CH, kchunk = lane % CH;
+  const int koff = (8 * (krow >> 2) + (krow & 3)) * D + kchunk * 8;
+  uint8_t* slice = slices[wave];
+  auto slot = [](int r, int chunk) {
+    return r * (D * 2) + ((chunk ^ (CH == 16 ? r & 15 : (r >> 1) & 7)) * 16);
+  };
+  // Each byte of K and V is read by this workgroup only: streamed past the
+  // caches.  Past the range its last block comes again: those keys are not seen.
+  auto block_at = [&](int t, int second) {
+    const int lb = min(kv_begin / B + t * (TK / B) + second, lb_last);
+    return ((int64_t)bt_row[lb] * a.hkv + kvh) * head_elems;
+  };
+  u32x4_t kr[2][NKL];
+  uint4 vr[NDT];
+  auto load_k = [&](int t) {
+    const int64_t b0 = block_at(t, 0), b1 = B < TK ? block_at(t, 1) : b0;
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int j = 0; j < NKL; ++j) {
+        const int key0 = 2 * KPL * j + 4 * b;  // the load's first key
+        kr[b][j] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(
+            a.k_cache + (key0 < B ? b0 : b1) + (key0 % B) * D + koff));
+      }
+  };
+  auto load_v = [&](int t) {
+    const int64_t b0 = block_at(t, 0), b1 = B < TK ? block_at(t, 1) : b0;
+    const uint16_t* vp = a.v_cache + (v_second ? b1 : b0) + voff;
+#pragma unroll
+    for (int dt = 0; dt < NDT; ++dt) vr[dt] = ld_global16_nt(vp + dt * 16 * B);
+  };
+
+  // tile t, with K of tile next requested on the way and V of it at the end
+  auto step = [&](int t, int next) {
+    const int k0 = kv_begin + t * TK;
+    f32x4_t s[NC][2];
+#pragma unroll
+    for (int c = 0; c < NC; ++c) s[c][0] = s[c][1] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    // a wave's LDS accesses complete in order: no wait but for the data
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int j = 0; j < NKL; ++j)
+        *reinterpret_cast<u32x4_t*>(slice + b * 16 * D * 2 + slot(KPL * j + krow, kchunk)) =
+            kr[b][j];
+    load_k(next);
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+#pragma unroll
+    for (int ks = 0; ks < NKS; ++ks)
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        const uint4 k =
+            *reinterpret_cast<const uint4*>(slice + b * 16 * D * 2 + slot(i, 4 * ks + g));
+#pragma unroll
+        for (int c = 0; c < NC; ++c) s[c][b] = mfma16x16x32(k, qv[c][ks], s[c][b]);
+      }
+    __builtin_amdgcn_wave_barrier();
+    if (k0 + TK > row.start) {  // the tree's own keys (wave-uniform)
+      const int first = k0 + 8 * g - row.start;  // tree offset of this lane's keys
+#pragma unroll
+      for (int c = 0; c < NC; ++c) {
+        const uint64_t* m = a.mask + (int64_t)(row.tok0 + (row_at(c) >> a.log2_group)) * a.words;
+        const uint32_t seen = seen32(m, a.words, row.n, k0 - row.start) >> (8 * g);
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (!(seen >> e & 1)) s[c][e >> 2][e & 3] = -INFINITY;
+      }
+      uint32_t bad = 0;
+#pragma unroll
+      for (int dt = 0; dt < NDT; ++dt) {
+        uint32_t* w = reinterpret_cast<uint32_t*>(&vr[dt]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          // keys past the row hold anything; its committed keys are seen by all
+          const int k = first + 2 * e;
+          const bool lo = k >= 0 && bad_lo(w[e]), hi = k + 1 >= 0 && bad_hi(w[e]);
+          if (lo || k >= row.n) w[e] &= 0xffff0000u;
+          if (hi || k + 1 >= row.n) w[e] &= 0x0000ffffu;
+          if (lo && k < row.n) bad |= 1u << (2 * e);
+          if (hi && k + 1 < row.n) bad |= 2u << (2 * e);
+        }
+      }
+      for (; bad; bad &= bad - 1) {
+        const int k = first + __ffs(bad) - 1;
+        atomicOr(&s_bad[k >> 6], 1ull << (k & 63));
+      }
+    }
+    uint4 pv[NC];
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      float x = fmaxf(fmaxf(fmaxf(s[c][0][0], s[c][0][1]), fmaxf(s[c][0][2], s[c][0][3])),
+                      fmaxf(fmaxf(s[c][1][0], s[c][1][1]), fmaxf(s[c][1][2], s[c][1][3]))) *
+                a.scale_log2;
+      if (__builtin_amdgcn_ballot_w64(x > m_run[c] + kRescaleThreshold)) {
+        // the four lanes of a row share its maximum
+        x = fmaxf(x, shfl_xor_f(x, 16));
+        x = fmaxf(x, shfl_xor_f(x, 32));
+        const float mnew = fmaxf(m_run[c], x);
+        const float alpha = m_run[c] == -INFINITY ? 0.f : exp2f(m_run[c] - mnew);
+        m_run[c] = mnew;
+        l_run[c] *= alpha;
+#pragma unroll
+        for (int dt = 0; dt < NDT; ++dt) o[c][dt] *= alpha;
+      }
+      const float neg_m = m_run[c] == -INFINITY ? 0.f : -m_run[c];  // nothing seen yet
+      uint32_t p[4];  // keys 8 g + 2 e, + 1
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float p0 = exp2f(__builtin_fmaf(s[c][e >> 1][2 * (e & 1)], a.scale_log2, neg_m));
+        const float p1 = exp2f(__builtin_fmaf(s[c][e >> 1][2 * (e & 1) + 1], a.scale_log2, neg_m));
+        p[e] = pack_bf16x2(p0, p1);
+        l_run[c] = dot2_bf16(p[e], 0x3f803f80u, l_run[c]);  // the rounded weights
+      }
+      pv[c] = make_uint4(p[0], p[1], p[2], p[3]);
+    }
+#pragma unroll
+    for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+      for (int c = 0; c < NC; ++c) o[c][dt] = mfma16x16x32(vr[dt], pv[c], o[c][dt]);
+    load_v(next);
+  };
+
+  __syncthreads();  // s_bad is clear
+  {
+    // The requests are unconditional (past the range its last tile again,
+    // which is unused), so that the waits on them stay exact.
+    const int last = n_tiles - 1;  // a piece is never empty
+    load_k(min(wave, last));
+    load_v(min(wave, last));
+    for (int t = wave; t < n_tiles; t += kWaves) step(t, min(t + kWaves, last));
+  }
+
+  // ---- combine the waves and write: lane (g, i) holds features 16 dt + 4 g
+  // .. + 3 of its rows
+  auto red = reinterpret_cast<float(*)[16][D]>(&slices[0][0]);
+  static_assert(sizeof(float) * 16 * D == SLICE, "a wave's output fills its slice");
+#pragma unroll
+  for (int c = 0; c < NC; ++c) {
+    if (m0 + 16 * c >= m_rows) break;  // uniform
+    float l = l_run[c];
+    l += shfl_xor_f(l, 16);
+    l += shfl_xor_f(l, 32);
+    __syncthreads();
+#pragma unroll
+    for (int dt = 0; dt < NDT; ++dt)
+      *reinterpret_cast<f32x4_t*>(&red[wave][i][dt * 16 + 4 * g]) = o[c][dt];
+    if (g == 0) s_m[wave][i] = m_run[c], s_l[wave][i] = l;
+    __syncthreads();
+    const uint64_t any = s_bad[0] | s_bad[1] | s_bad[2] | s_bad[3];
+    for (int x = tid; x < 16 * D; x += kThreads) {
+      const int r = x / D, d = x % D, mr = m0 + 16 * c + r;
+      if (mr >= m_rows) break;  // rows come in increasing order
+      float M = -INFINITY;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) M = fmaxf(M, s_m[w][r]);
+      float L = 0.f, O = 0.f;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) {
+        const float mw = s_m[w][r];
+        const float f = mw == -INFINITY ? 0.f : exp2f(mw - M);
+        L += f * s_l[w][r];
+        O += f * red[w][r][d];
+      }
+      float val = L == 0.f ? 0.f : O / L;
+      const int64_t t = row.tok0 + (mr >> a.log2_group);
+      if (any)
+        val += bad_values<D, B>(reinterpret_cast<const uint64_t*>(s_bad), a.mask + t * a.words,
+                                a.words, row, bt_row, a.v_cache, a.hkv, kvh, d);
+      if (row.n_split == 1) {
+        a.out[(t * a.hq + kvh * G + (mr & (G - 1))) * D + d] = to_bf16(val);
+      } else {
+        const int64_t pr =
+            (int64_t)row.part0 + ((int64_t)kvh * row.n_split + split) * m_rows + mr;
+        a.part_o[pr * D + d] = val;
+        if (d == 0) a.part_lse[pr] = L == 0.f ? -INFINITY : M + __log2f(L);
+      }
+    }
+  }
+}
+
+// Merge of split key ranges: with O_s and L_s, a piece's normalised output and
+// the log2 of its weights' sum, the row's output is
+//     sum_s 2^(L_s - max L) O_s / sum_s 2^(L_s - max L).
+// A row (node, q head) takes D / 4 threads of 4 features; with many splits
+// several such slots share it, each taking every P-th split, and meet in LDS.
+template <int D>
+__global__ __launch_bounds__(kThreads) void tree_merge_kernel(const TreeRows rows,
+                                                              const AttnArgs a) {
+  constexpr int DQ = D / 4, SLOTS = kThreads / DQ, U = 8;
+  __shared__ float4 s_acc[SLOTS][DQ];
+  __shared__ float s_m[SLOTS], s_w[SLOTS];
+  const TreeRow row = row_of(rows, blockIdx.x);
+  const int per = merge_rows(D, row.n_split);
+  const int slot = threadIdx.x / DQ, dq = threadIdx.x % DQ;
+  const int P = SLOTS / per, p = slot / per;
+  const int x = ((int)blockIdx.x - row.item0) * per + slot % per;  // node * hq + head
+  const bool in = x < row.n * a.hq;
+  const int node = x / a.hq, h = x % a.hq;
+  const int G = 1 << a.log2_group, m_rows = row.n * G;
+  const int64_t base = (int64_t)row.part0 +
+                       (int64_t)(h >> a.log2_group) * row.n_split * m_rows + node * G +
+                       (h & (G - 1));
+  float M = -INFINITY, W = 0.f;
+  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+  if (in) {
+    for (int s0 = p; s0 < row.n_split; s0 += P * U) {
+      float ls[U];
+      float4 o[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {  // past the last split: it again, weight 0
+        const int s = s0 + u * P;
+        const int64_t pr = base + (int64_t)min(s, row.n_split - 1) * m_rows;
+        ls[u] = a.part_lse[pr];
+        o[u] = *reinterpret_cast<const float4*>(a.part_o + pr * D + dq * 4);
+        if (s >= row.n_split) ls[u] = -INFINITY;
+      }
+      float m = M;
+#pragma unroll
+      for (int u = 0; u < U; ++u) m = fmaxf(m, ls[u]);
+      const float keep = M == -INFINITY ? 0.f : exp2f(M - m);
+      M = m;
+      W *= keep;
+      acc.x *= keep, acc.y *= keep, acc.z *= keep, acc.w *= keep;
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        if (ls[u] == -INFINITY) continue;
+        const float w = exp2f(ls[u] - m);
+        W += w;
+        acc.x += w * o[u].x;
+        acc.y += w * o[u].y;
+        acc.z += w * o[u].z;
+        acc.w += w * o[u].w;
+      }
+    }
+  }
+  if (P > 1) {  // uniform
+    s_acc[slot][dq] = acc;
+    if (dq == 0) s_m[slot] = M, s_w[slot] = W;
+    __syncthreads();
+    if (p > 0) return;
+    for (int k = 1; k < P; ++k) M = fmaxf(M, s_m[k * per + slot]);
+    W = 0.f;
+    acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int k = 0; k < P; ++k) {
+      const float wk = s_w[k * per + slot];
+      if (wk == 0.f) continue;
+      const float w = exp2f(s_m[k * per + slot] - M);
+      const float4 v = s_acc[k * per + slot][dq];
+      W += w * wk;
+      acc.x += w * v.x;
+      acc.y += w * v.y;
+      acc.z += w * v.z;
+      acc.w += w * v.w;
+    }
+  }
+  if (!in) return;
+  const float inv = W == 0.f ? 0.f : 1.f / W;
+  uint2 w2;
+  w2.x = pack_bf16x2(acc.x * inv, acc.y * inv);
+  w2.y = pack_bf16x2(acc.z * inv, acc.w * inv);
+  *reinterpret_cast<uint2*>(a.out + ((int64_t)(row.tok0 + node) * a.hq + h) * D + dq * 4) = w2;
+}
+
+template <int D, int B>
+hipError_t launch_narrow_t(int most_rows, const AttnArgs& a, const TreeRows& rows, int items,
+                           hipStream_t s) {
+  auto kern = most_rows <= 16   ? narrow_kernel<D, B, 1>
+              : most_rows <= 32 ? narrow_kernel<D, B, 2>
+                                : narrow_kernel<D, B, 4>;
+  hipLaunchKernelGGL(kern, dim3(items), dim3(kThreads), 0, s, rows, a);
+  return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_attn(int d, int block, const AttnArgs& a, const TreeRows& rows, int n_rows,
-                       int items, hipStream_t s) {
-  auto kern = d == 128 ? (block == 16 ? tree_attn_kernel<128, 16> : tree_attn_kernel<128, 32>)
-                       : (block == 16 ? tree_attn_kernel<64, 16> : tree_attn_kernel<64, 32>);
-  hipLaunchKernelGGL(kern, dim3(items, a.hq), dim3(kThreads), 0, s, rows, n_rows, a);
+hipError_t launch_narrow(int d, int block, int most_rows, const AttnArgs& a, const TreeRows& rows,
+                         int items, hipStream_t s) {
+  if (d == 128 && block == 16) return launch_narrow_t<128, 16>(most_rows, a, rows, items, s);
+  if (d == 128) return launch_narrow_t<128, 32>(most_rows, a, rows, items, s);
+  if (block == 16) return launch_narrow_t<64, 16>(most_rows, a, rows, items, s);
+  return launch_narrow_t<64, 32>(most_rows, a, rows, items, s);
+}
+
+hipError_t launch_tree_merge(int d, const AttnArgs& a, const TreeRows& rows, int items,
+                             hipStream_t s) {
+  hipLaunchKernelGGL(d == 128 ? tree_merge_kernel<128> : tree_merge_kernel<64>, dim3(items),
+                     dim3(kThreads), 0, s, rows, a);
   return hipGetLastError();
 }
 

@@ -14,11 +14,17 @@ struct AttnArgs {
   const int32_t* bt;
   const uint64_t* mask;
   uint16_t* out;
-  int words, hq, hkv, mbr;
+  float* part_o;    // [partial rows][D], normalised
+  float* part_lse;  // [partial rows], log2 of the weights' sum
+  int words, hq, hkv, mbr, log2_group;
   float scale_log2;  // sm_scale * log2(e)
 };
 
-hipError_t launch_attn(int d, int block, const AttnArgs& a, const TreeRows& rows, int n_rows,
-                       int items, hipStream_t s);
+// The rows of a launch; the places behind them hold an item0 that no workgroup
+// reaches.
+hipError_t launch_narrow(int d, int block, int most_rows, const AttnArgs& a, const TreeRows& rows,
+                         int items, hipStream_t s);
+hipError_t launch_tree_merge(int d, const AttnArgs& a, const TreeRows& rows, int items,
+                             hipStream_t s);
 
 }  // namespace cptree
