@@ -20,7 +20,8 @@ SCHED_LIB = os.path.join(PKG, "libcpsched.so")
 LAYER_LIB = os.path.join(PKG, "libcplayer.so")
 LAYER_SOURCES = ["layer.hip", "gemm.hip"]
 TREE_LIB = os.path.join(PKG, "libcptree.so")
-TREE_SOURCES = ["tree_api.hip", "tree_plan.cpp", "tree_attn.hip", "tree_ops.hip"]
+TREE_SOURCES = ["tree_api.hip", "tree_plan.cpp", "tree_attn.hip", "tree_wide64.hip",
+                "tree_wide128.hip", "tree_ops.hip"]
 PEAKS_LIB = os.path.join(PKG, "libcppeaks.so")
 PEAKS_SOURCES = ["peaks.hip"]
 CXX = os.environ.get("CXX", "g++")

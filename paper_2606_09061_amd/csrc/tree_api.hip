@@ -266,12 +266,20 @@ int cp_tree_attn(const cp_attn_desc* desc, const void* q, const void* k_cache,
                      desc->sm_scale * cpattn::kLog2e};
     const int d = desc->head_dim;
     rc = by_tree_rows(
-        p.narrow,
+        p.narrow.rows, [&](const TreeRow& t) { return t.n_split * desc->num_kv_heads; },
+        [&](const TreeRows& batch, int items) {
+          return finish(launch_narrow(d, desc->block_size, p.narrow.most, a, batch, items, s), s);
+        });
+    if (rc != CP_OK) return rc;
+    const int waves = wide_waves(p.wide.most), tile = 32 * waves;
+    rc = by_tree_rows(
+        p.wide.rows,
         [&](const TreeRow& t) {
-          return t.n_split * desc->num_kv_heads * narrow_tiles(t.n * group, p.narrow_rows);
+          return t.n_split * desc->num_kv_heads * ((t.n * group + tile - 1) / tile);
         },
         [&](const TreeRows& batch, int items) {
-          return finish(launch_narrow(d, desc->block_size, p.narrow_rows, a, batch, items, s), s);
+          return finish((d == 128 ? launch_wide128 : launch_wide64)(desc->block_size, waves, a,
+                                                                    batch, items, s), s);
         });
     if (rc != CP_OK) return rc;
     return by_tree_rows(

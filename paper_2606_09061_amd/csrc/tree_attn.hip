@@ -11,7 +11,7 @@
 // nothing until the keys of the tree itself, the last ones of a row.
 #include "tree_attn.hpp"
 
-#include "device.hpp"
+#include "tree_device.hpp"
 #include "tree_plan.hpp"
 
 namespace cptree {
@@ -37,51 +37,7 @@ __device__ __forceinline__ f32x4_t mfma16x16x32(uint4 a, uint4 b, f32x4_t c) {
                                                  __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
 }
 
-// The row whose workgroups item b belongs to: as many rows begin at or before
-// it as lanes say so (every lane of a wave looks at two rows).
-__device__ __forceinline__ TreeRow row_of(const TreeRows& rows, int b) {
-  static_assert(kTreeRows > 64 && kTreeRows <= 128, "two rows per lane");
-  const int lane = threadIdx.x & 63;
-  const bool lo = rows.r[lane].item0 <= b;
-  const bool hi = 64 + lane < kTreeRows && rows.r[min(64 + lane, kTreeRows - 1)].item0 <= b;
-  const int n = __popcll(__builtin_amdgcn_ballot_w64(lo)) +
-                __popcll(__builtin_amdgcn_ballot_w64(hi));
-  return rows.r[__builtin_amdgcn_readfirstlane(n - 1)];
-}
-
-// Bit b: whether a node with this mask sees the key at offset o + b of its
-// row's tree (negative offsets are committed keys, o > -32).
-__device__ __forceinline__ uint32_t seen32(const uint64_t* mask, int words, int n, int o) {
-  if (o >= n) return 0;
-  const int at = max(o, 0), w = at >> 6, sh = at & 63;
-  uint64_t x = mask[w] >> sh;
-  if (sh > 32 && w + 1 < words) x |= mask[w + 1] << (64 - sh);
-  if (n - at < 32) x &= (1u << (n - at)) - 1;
-  return o >= 0 ? (uint32_t)x : (uint32_t)x << -o | ((1u << -o) - 1);
-}
-
-// Whether a bf16 is an infinity or NaN, for both halves of a word.
-__device__ __forceinline__ bool bad_lo(uint32_t w) { return (w & 0x7f80u) == 0x7f80u; }
-__device__ __forceinline__ bool bad_hi(uint32_t w) { return (w & 0x7f800000u) == 0x7f800000u; }
-
-// What the infinite or NaN values of nodes in `bad` that a node with this mask
-// sees add to feature d of its output.
-template <int D, int B>
-__device__ float bad_values(const uint64_t* bad, const uint64_t* mask, int words,
-                            const TreeRow& row, const int32_t* bt_row, const uint16_t* v_cache,
-                            int hkv, int kvh, int d) {
-  float sum = 0.f;
-  for (int w = 0; w < words; ++w)
-    for (uint64_t x = bad[w] & mask[w]; x; x &= x - 1) {
-      const int p = row.start + 64 * w + __ffsll((unsigned long long)x) - 1;
-      const uint32_t v =
-          v_cache[(((int64_t)bt_row[p / B] * hkv + kvh) * D + d) * B + p % B];
-      if (bad_lo(v)) sum += __uint_as_float(v << 16);
-    }
-  return sum;
-}
-
-// A workgroup takes up to 16 NC of a kv head's rows and a piece of the key range, of which wave w takes tiles of 32 keys w, w + 4, ...  The
+// Up to 16 NC rows: a workgroup takes all of a kv head's and a piece of the key range, of which wave w takes tiles of 32 keys w, w + 4, ...  The
 // rows are the columns of both products (v_mfma_f32_16x16x32_bf16, NC of them
 // per operand of K or V).  Per tile and wave, lane l = 16 g + i:
 //   S^T (2 x 16 keys x 16 NC rows) = K . Q^T.  Row i of key half b is key
@@ -112,8 +68,7 @@ __global__ __launch_bounds__(kThreads, NC <= 2 ? 2 : 1) void narrow_kernel(const
   const TreeRow row = row_of(rows, blockIdx.x);
   const int unit = (int)blockIdx.x - row.item0;
   const int G = 1 << a.log2_group, m_rows = row.n << a.log2_group;
-  const int tiles = (m_rows + 16 * NC - 1) / (16 * NC), m0 = unit % tiles * 16 * NC;
-  const int kvh = unit / tiles % a.hkv, split = unit / tiles / a.hkv;
+  const int kvh = unit % a.hkv, split = unit / a.hkv;
   const int tid = threadIdx.x, lane = tid & 63, i = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int ctx = row.start + row.n;
@@ -122,7 +77,7 @@ __global__ __launch_bounds__(kThreads, NC <= 2 ? 2 : 1) void narrow_kernel(const
 
   // column c's row of this lane, past the last one that again (not stored)
   uint4 qv[NC][NKS];
-  auto row_at = [&](int c) { return min(m0 + 16 * c + i, m_rows - 1); };
+  auto row_at = [&](int c) { return min(16 * c + i, m_rows - 1); };
 #pragma unroll
   for (int c = 0; c < NC; ++c) {
     const int x = row_at(c);
@@ -214,30 +169,19 @@ __global__ __launch_bounds__(kThreads, NC <= 2 ? 2 : 1) void narrow_kernel(const
 #pragma unroll
       for (int c = 0; c < NC; ++c) {
         const uint64_t* m = a.mask + (int64_t)(row.tok0 + (row_at(c) >> a.log2_group)) * a.words;
-        const uint32_t seen = seen32(m, a.words, row.n, k0 - row.start) >> (8 * g);
+        const uint32_t seen = (uint32_t)seen64(m, a.words, row.n, k0 - row.start) >> (8 * g);
 #pragma unroll
         for (int e = 0; e < 8; ++e)
           if (!(seen >> e & 1)) s[c][e >> 2][e & 3] = -INFINITY;
       }
-      uint32_t bad = 0;
+      uint32_t found = 0;
 #pragma unroll
       for (int dt = 0; dt < NDT; ++dt) {
         uint32_t* w = reinterpret_cast<uint32_t*>(&vr[dt]);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          // keys past the row hold anything; its committed keys are seen by all
-          const int k = first + 2 * e;
-          const bool lo = k >= 0 && bad_lo(w[e]), hi = k + 1 >= 0 && bad_hi(w[e]);
-          if (lo || k >= row.n) w[e] &= 0xffff0000u;
-          if (hi || k + 1 >= row.n) w[e] &= 0x0000ffffu;
-          if (lo && k < row.n) bad |= 1u << (2 * e);
-          if (hi && k + 1 < row.n) bad |= 2u << (2 * e);
-        }
+        for (int e = 0; e < 4; ++e) found |= clean_word(w[e], first + 2 * e, row.n) << (2 * e);
       }
-      for (; bad; bad &= bad - 1) {
-        const int k = first + __ffs(bad) - 1;
-        atomicOr(&s_bad[k >> 6], 1ull << (k & 63));
-      }
+      note_bad(s_bad, found, first);
     }
     uint4 pv[NC];
 #pragma unroll
@@ -290,7 +234,7 @@ __global__ __launch_bounds__(kThreads, NC <= 2 ? 2 : 1) void narrow_kernel(const
   static_assert(sizeof(float) * 16 * D == SLICE, "a wave's output fills its slice");
 #pragma unroll
   for (int c = 0; c < NC; ++c) {
-    if (m0 + 16 * c >= m_rows) break;  // uniform
+    if (16 * c >= m_rows) break;  // uniform
     float l = l_run[c];
     l += shfl_xor_f(l, 16);
     l += shfl_xor_f(l, 32);
@@ -302,7 +246,7 @@ __global__ __launch_bounds__(kThreads, NC <= 2 ? 2 : 1) void narrow_kernel(const
     __syncthreads();
     const uint64_t any = s_bad[0] | s_bad[1] | s_bad[2] | s_bad[3];
     for (int x = tid; x < 16 * D; x += kThreads) {
-      const int r = x / D, d = x % D, mr = m0 + 16 * c + r;
+      const int r = x / D, d = x % D, mr = 16 * c + r;
       if (mr >= m_rows) break;  // rows come in increasing order
       float M = -INFINITY;
 #pragma unroll
@@ -318,8 +262,7 @@ __global__ __launch_bounds__(kThreads, NC <= 2 ? 2 : 1) void narrow_kernel(const
       float val = L == 0.f ? 0.f : O / L;
       const int64_t t = row.tok0 + (mr >> a.log2_group);
       if (any)
-        val += bad_values<D, B>(reinterpret_cast<const uint64_t*>(s_bad), a.mask + t * a.words,
-                                a.words, row, bt_row, a.v_cache, a.hkv, kvh, d);
+        val += bad_values<D, B>(s_bad, a.mask + t * a.words, a.words, row, a, kvh, d);
       if (row.n_split == 1) {
         a.out[(t * a.hq + kvh * G + (mr & (G - 1))) * D + d] = to_bf16(val);
       } else {
@@ -418,9 +361,10 @@ __global__ __launch_bounds__(kThreads) void tree_merge_kernel(const TreeRows row
 template <int D, int B>
 hipError_t launch_narrow_t(int most_rows, const AttnArgs& a, const TreeRows& rows, int items,
                            hipStream_t s) {
-  auto kern = most_rows <= 16   ? narrow_kernel<D, B, 1>
-              : most_rows <= 32 ? narrow_kernel<D, B, 2>
-                                : narrow_kernel<D, B, 4>;
+  const int tile = narrow_tile(most_rows);
+  auto kern = tile == 16   ? narrow_kernel<D, B, 1>
+              : tile == 32 ? narrow_kernel<D, B, 2>
+                           : narrow_kernel<D, B, 4>;
   hipLaunchKernelGGL(kern, dim3(items), dim3(kThreads), 0, s, rows, a);
   return hipGetLastError();
 }
