@@ -128,7 +128,7 @@ struct CausalVis {
   static constexpr bool kTree = false;
   // of a tree only
   __device__ int start() const;
-  __device__ uint64_t seen(int t, int k0) const;
+  __device__ uint64_t seen(int node, int k0) const;
   template <int D, int B, int NW>
   __device__ void clean(uint8_t* vb, int k0, int tid) const;
 };

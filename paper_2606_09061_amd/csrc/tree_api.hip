@@ -266,20 +266,14 @@ int cp_tree_attn(const cp_attn_desc* desc, const void* q, const void* k_cache,
                      desc->sm_scale * cpattn::kLog2e};
     const int d = desc->head_dim;
     rc = by_tree_rows(
-        p.narrow.rows, [&](const TreeRow& t) { return t.n_split * desc->num_kv_heads; },
+        p.rows,
+        [&](const TreeRow& t) { return t.n_split * desc->num_kv_heads * p.tiles(t, group); },
         [&](const TreeRows& batch, int items) {
-          return finish(launch_narrow(d, desc->block_size, p.narrow.most, a, batch, items, s), s);
-        });
-    if (rc != CP_OK) return rc;
-    const int waves = wide_waves(p.wide.most), tile = 32 * waves;
-    rc = by_tree_rows(
-        p.wide.rows,
-        [&](const TreeRow& t) {
-          return t.n_split * desc->num_kv_heads * ((t.n * group + tile - 1) / tile);
-        },
-        [&](const TreeRows& batch, int items) {
-          return finish((d == 128 ? launch_wide128 : launch_wide64)(desc->block_size, waves, a,
-                                                                    batch, items, s), s);
+          const hipError_t e =
+              !p.wide()  ? launch_narrow(d, desc->block_size, p.most, a, batch, items, s)
+              : d == 128 ? launch_wide128(desc->block_size, a, batch, items, s)
+                         : launch_wide64(desc->block_size, a, batch, items, s);
+          return finish(e, s);
         });
     if (rc != CP_OK) return rc;
     return by_tree_rows(

@@ -25,7 +25,6 @@ using cpattn::ld_global16_nt;
 using cpattn::pack_bf16x2;
 using cpattn::shfl_xor_f;
 using cpattn::to_bf16;
-using cpattn::u32x4_t;
 
 namespace {
 
@@ -37,7 +36,8 @@ __device__ __forceinline__ f32x4_t mfma16x16x32(uint4 a, uint4 b, f32x4_t c) {
                                                  __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
 }
 
-// Up to 16 NC rows: a workgroup takes all of a kv head's and a piece of the key range, of which wave w takes tiles of 32 keys w, w + 4, ...  The
+// A workgroup takes all of a kv head's rows, up to 16 NC of them, and a piece
+// of the key range, of which wave w takes tiles of 32 keys w, w + 4, ...  The
 // rows are the columns of both products (v_mfma_f32_16x16x32_bf16, NC of them
 // per operand of K or V).  Per tile and wave, lane l = 16 g + i:
 //   S^T (2 x 16 keys x 16 NC rows) = K . Q^T.  Row i of key half b is key
@@ -55,36 +55,40 @@ __device__ __forceinline__ f32x4_t mfma16x16x32(uint4 a, uint4 b, f32x4_t c) {
 // zeros: a node that does not see the key would get 0 * NaN from it.  The
 // nodes that do get them added at the end.
 template <int D, int B, int NC>
-__global__ __launch_bounds__(kThreads, NC <= 2 ? 2 : 1) void narrow_kernel(const TreeRows rows,
-                                                                           const AttnArgs a) {
+__global__ __launch_bounds__(kThreads, 2) void narrow_kernel(const TreeRows rows,
+                                                             const AttnArgs a) {
   constexpr int TK = 32;       // keys per tile
-  constexpr int NKS = D / 32;  // k-steps of a score
-  constexpr int NDT = D / 16;  // 16-feature blocks of the output
+  constexpr int ROWS = 16 * NC;
+  constexpr int NKS = D / 32;    // k-steps of a score
+  constexpr int NDT = D / 16;    // 16-feature blocks of the output
   constexpr int SLICE = 16 * D * 4;  // bytes of a wave: 32 keys' rows, then 16 rows' output
   __shared__ __align__(16) uint8_t slices[kWaves][SLICE];
-  __shared__ float s_m[kWaves][16], s_l[kWaves][16];
+  __shared__ float s_m[kWaves][ROWS], s_l[kWaves][ROWS], s_f[kWaves][ROWS];
   __shared__ unsigned long long s_bad[kMaxWords];
 
   const TreeRow row = row_of(rows, blockIdx.x);
   const int unit = (int)blockIdx.x - row.item0;
-  const int G = 1 << a.log2_group, m_rows = row.n << a.log2_group;
   const int kvh = unit % a.hkv, split = unit / a.hkv;
   const int tid = threadIdx.x, lane = tid & 63, i = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int G = 1 << a.log2_group, m_rows = row.n << a.log2_group;
   const int ctx = row.start + row.n;
   const int kv_begin = split * row.split_keys, kv_end = min(ctx, kv_begin + row.split_keys);
   if (tid < kMaxWords) s_bad[tid] = 0;
 
-  // column c's row of this lane, past the last one that again (not stored)
+  // Column c's row of this lane, past the last one that again (not stored), and
+  // its node's mask: a narrow tree's nodes fit one word.
   uint4 qv[NC][NKS];
-  auto row_at = [&](int c) { return min(16 * c + i, m_rows - 1); };
+  uint64_t mask[NC];
+  static_assert(kNarrowRows <= 64, "one word");
 #pragma unroll
   for (int c = 0; c < NC; ++c) {
-    const int x = row_at(c);
+    const int x = min(16 * c + i, m_rows - 1);
     const int64_t t = row.tok0 + (x >> a.log2_group);
     const uint16_t* qb = a.q + (t * a.hq + kvh * G + (x & (G - 1))) * D + g * 8;
 #pragma unroll
     for (int ks = 0; ks < NKS; ++ks) qv[c][ks] = ld_global16(qb + ks * 32);
+    mask[c] = a.mask[t * a.words];
   }
   __builtin_amdgcn_sched_barrier(0);
 
@@ -111,14 +115,13 @@ __global__ __launch_bounds__(kThreads, NC <= 2 ? 2 : 1) void narrow_kernel(const
   auto slot = [](int r, int chunk) {
     return r * (D * 2) + ((chunk ^ (CH == 16 ? r & 15 : (r >> 1) & 7)) * 16);
   };
-  // Each byte of K and V is read by this workgroup only: streamed past the
-  // caches.  Past the range its last block comes again: those keys are not seen.
+  // Each byte of K and V is read by one wave only: streamed past the caches.
+  // Past the range its last block comes again: those keys are not seen.
   auto block_at = [&](int t, int second) {
     const int lb = min(kv_begin / B + t * (TK / B) + second, lb_last);
     return ((int64_t)bt_row[lb] * a.hkv + kvh) * head_elems;
   };
-  u32x4_t kr[2][NKL];
-  uint4 vr[NDT];
+  uint4 kr[2][NKL], vr[NDT];
   auto load_k = [&](int t) {
     const int64_t b0 = block_at(t, 0), b1 = B < TK ? block_at(t, 1) : b0;
 #pragma unroll
@@ -126,8 +129,7 @@ __global__ __launch_bounds__(kThreads, NC <= 2 ? 2 : 1) void narrow_kernel(const
 #pragma unroll
       for (int j = 0; j < NKL; ++j) {
         const int key0 = 2 * KPL * j + 4 * b;  // the load's first key
-        kr[b][j] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(
-            a.k_cache + (key0 < B ? b0 : b1) + (key0 % B) * D + koff));
+        kr[b][j] = ld_global16_nt(a.k_cache + (key0 < B ? b0 : b1) + (key0 % B) * D + koff);
       }
   };
   auto load_v = [&](int t) {
@@ -148,7 +150,7 @@ __global__ __launch_bounds__(kThreads, NC <= 2 ? 2 : 1) void narrow_kernel(const
     for (int b = 0; b < 2; ++b)
 #pragma unroll
       for (int j = 0; j < NKL; ++j)
-        *reinterpret_cast<u32x4_t*>(slice + b * 16 * D * 2 + slot(KPL * j + krow, kchunk)) =
+        *reinterpret_cast<uint4*>(slice + b * 16 * D * 2 + slot(KPL * j + krow, kchunk)) =
             kr[b][j];
     load_k(next);
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
@@ -165,23 +167,50 @@ __global__ __launch_bounds__(kThreads, NC <= 2 ? 2 : 1) void narrow_kernel(const
       }
     __builtin_amdgcn_wave_barrier();
     if (k0 + TK > row.start) {  // the tree's own keys (wave-uniform)
-      const int first = k0 + 8 * g - row.start;  // tree offset of this lane's keys
+      const int o0 = k0 - row.start, first = o0 + 8 * g;  // tree offsets: tile's, this lane's
 #pragma unroll
       for (int c = 0; c < NC; ++c) {
-        const uint64_t* m = a.mask + (int64_t)(row.tok0 + (row_at(c) >> a.log2_group)) * a.words;
-        const uint32_t seen = (uint32_t)seen64(m, a.words, row.n, k0 - row.start) >> (8 * g);
+        uint64_t m = row.n < 64 ? mask[c] & ((1ull << row.n) - 1) : mask[c];
+        m = o0 >= 64 ? 0 : o0 >= 0 ? m >> o0 : m << -o0 | ((1ull << -o0) - 1);
+        const uint32_t seen = (uint32_t)m >> (8 * g);
 #pragma unroll
         for (int e = 0; e < 8; ++e)
           if (!(seen >> e & 1)) s[c][e >> 2][e & 3] = -INFINITY;
       }
-      uint32_t found = 0;
+      // keys past the row, whose slots may hold anything
+      uint32_t keep[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        keep[e] = (first + 2 * e < row.n ? 0x0000ffffu : 0u) |
+                  (first + 2 * e + 1 < row.n ? 0xffff0000u : 0u);
+      u16x2_t top = {0, 0};  // of the values without their signs
 #pragma unroll
       for (int dt = 0; dt < NDT; ++dt) {
         uint32_t* w = reinterpret_cast<uint32_t*>(&vr[dt]);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) found |= clean_word(w[e], first + 2 * e, row.n) << (2 * e);
+        for (int e = 0; e < 4; ++e) {
+          w[e] &= keep[e];
+          top = __builtin_elementwise_max(top,
+                                          __builtin_bit_cast(u16x2_t, w[e] & 0x7fff7fffu));
+        }
       }
-      note_bad(s_bad, found, first);
+      if (__builtin_amdgcn_ballot_w64(max(top[0], top[1]) >= 0x7f80)) {
+        // rare: one word at a time, in the slice that K no longer needs
+        uint4* own = reinterpret_cast<uint4*>(slice) + lane;
+#pragma unroll
+        for (int dt = 0; dt < NDT; ++dt) own[64 * dt] = vr[dt];
+        uint32_t found = 0;
+#pragma unroll 1
+        for (int x = 0; x < 4 * NDT; ++x) {
+          uint32_t* w = reinterpret_cast<uint32_t*>(own + 64 * (x >> 2)) + (x & 3);
+          uint32_t v = *w;
+          found |= clean_word(v, first + 2 * (x & 3), row.n) << (2 * (x & 3));
+          *w = v;
+        }
+#pragma unroll
+        for (int dt = 0; dt < NDT; ++dt) vr[dt] = own[64 * dt];
+        note_bad(s_bad, found, first);
+      }
     }
     uint4 pv[NC];
 #pragma unroll
@@ -204,8 +233,10 @@ __global__ __launch_bounds__(kThreads, NC <= 2 ? 2 : 1) void narrow_kernel(const
       uint32_t p[4];  // keys 8 g + 2 e, + 1
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const float p0 = exp2f(__builtin_fmaf(s[c][e >> 1][2 * (e & 1)], a.scale_log2, neg_m));
-        const float p1 = exp2f(__builtin_fmaf(s[c][e >> 1][2 * (e & 1) + 1], a.scale_log2, neg_m));
+        const float p0 = __builtin_amdgcn_exp2f(
+            __builtin_fmaf(s[c][e >> 1][2 * (e & 1)], a.scale_log2, neg_m));
+        const float p1 = __builtin_amdgcn_exp2f(
+            __builtin_fmaf(s[c][e >> 1][2 * (e & 1) + 1], a.scale_log2, neg_m));
         p[e] = pack_bf16x2(p0, p1);
         l_run[c] = dot2_bf16(p[e], 0x3f803f80u, l_run[c]);  // the rounded weights
       }
@@ -228,48 +259,63 @@ __global__ __launch_bounds__(kThreads, NC <= 2 ? 2 : 1) void narrow_kernel(const
     for (int t = wave; t < n_tiles; t += kWaves) step(t, min(t + kWaves, last));
   }
 
-  // ---- combine the waves and write: lane (g, i) holds features 16 dt + 4 g
-  // .. + 3 of its rows
+  // ---- combine the waves and write: wave w's row r counts with factor
+  // s_f[w][r] = 2^(m_w - max m) / (sum of the waves' sums so weighted)
+#pragma unroll
+  for (int c = 0; c < NC; ++c) {
+    float l = l_run[c];
+    l += shfl_xor_f(l, 16);
+    l += shfl_xor_f(l, 32);
+    if (g == 0) s_m[wave][16 * c + i] = m_run[c], s_l[wave][16 * c + i] = l;
+  }
+  __syncthreads();
+  const int64_t part0 =
+      (int64_t)row.part0 + ((int64_t)kvh * row.n_split + split) * m_rows;
+  if (tid < ROWS) {
+    float M = -INFINITY, L = 0.f, f[kWaves];
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) M = fmaxf(M, s_m[w][tid]);
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      const float m = s_m[w][tid];
+      f[w] = m == -INFINITY ? 0.f : exp2f(m - M);
+      L += f[w] * s_l[w][tid];
+    }
+    const float inv = L == 0.f ? 0.f : 1.f / L;  // L == 0: it saw no key
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) s_f[w][tid] = f[w] * inv;
+    if (row.n_split > 1 && tid < m_rows)
+      a.part_lse[part0 + tid] = L == 0.f ? -INFINITY : M + __log2f(L);
+  }
+  const uint64_t any = s_bad[0];
   auto red = reinterpret_cast<float(*)[16][D]>(&slices[0][0]);
   static_assert(sizeof(float) * 16 * D == SLICE, "a wave's output fills its slice");
 #pragma unroll
   for (int c = 0; c < NC; ++c) {
     if (16 * c >= m_rows) break;  // uniform
-    float l = l_run[c];
-    l += shfl_xor_f(l, 16);
-    l += shfl_xor_f(l, 32);
     __syncthreads();
+    // lane (g, i) holds features 16 dt + 4 g .. + 3 of row i; 16-byte piece p
+    // of row r lies at p ^ r, so that neither side meets a bank twice
 #pragma unroll
     for (int dt = 0; dt < NDT; ++dt)
-      *reinterpret_cast<f32x4_t*>(&red[wave][i][dt * 16 + 4 * g]) = o[c][dt];
-    if (g == 0) s_m[wave][i] = m_run[c], s_l[wave][i] = l;
+      *reinterpret_cast<f32x4_t*>(&red[wave][i][((4 * dt + g) ^ i) * 4]) = o[c][dt];
     __syncthreads();
-    const uint64_t any = s_bad[0] | s_bad[1] | s_bad[2] | s_bad[3];
-    for (int x = tid; x < 16 * D; x += kThreads) {
-      const int r = x / D, d = x % D, mr = 16 * c + r;
-      if (mr >= m_rows) break;  // rows come in increasing order
-      float M = -INFINITY;
+    for (int x = tid; x < 16 * (D / 4); x += kThreads) {
+      const int p = x % (D / 4), r = x / (D / 4), mr = 16 * c + r;
+      if (mr >= m_rows) break;  // a thread's rows come in increasing order
+      f32x4_t v = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int w = 0; w < kWaves; ++w) M = fmaxf(M, s_m[w][r]);
-      float L = 0.f, O = 0.f;
-#pragma unroll
-      for (int w = 0; w < kWaves; ++w) {
-        const float mw = s_m[w][r];
-        const float f = mw == -INFINITY ? 0.f : exp2f(mw - M);
-        L += f * s_l[w][r];
-        O += f * red[w][r][d];
-      }
-      float val = L == 0.f ? 0.f : O / L;
+      for (int w = 0; w < kWaves; ++w)
+        v += s_f[w][mr] * *reinterpret_cast<const f32x4_t*>(&red[w][r][(p ^ r) * 4]);
       const int64_t t = row.tok0 + (mr >> a.log2_group);
       if (any)
-        val += bad_values<D, B>(s_bad, a.mask + t * a.words, a.words, row, a, kvh, d);
+        for (int e = 0; e < 4; ++e)
+          v[e] += bad_values<D, B>(s_bad, a.mask + t * a.words, a.words, row, a, kvh, 4 * p + e);
       if (row.n_split == 1) {
-        a.out[(t * a.hq + kvh * G + (mr & (G - 1))) * D + d] = to_bf16(val);
+        const uint2 w = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+        *reinterpret_cast<uint2*>(a.out + (t * a.hq + kvh * G + (mr & (G - 1))) * D + 4 * p) = w;
       } else {
-        const int64_t pr =
-            (int64_t)row.part0 + ((int64_t)kvh * row.n_split + split) * m_rows + mr;
-        a.part_o[pr * D + d] = val;
-        if (d == 0) a.part_lse[pr] = L == 0.f ? -INFINITY : M + __log2f(L);
+        *reinterpret_cast<f32x4_t*>(a.part_o + (part0 + mr) * D + 4 * p) = v;
       }
     }
   }
@@ -359,24 +405,22 @@ __global__ __launch_bounds__(kThreads) void tree_merge_kernel(const TreeRows row
 }
 
 template <int D, int B>
-hipError_t launch_narrow_t(int most_rows, const AttnArgs& a, const TreeRows& rows, int items,
+hipError_t launch_narrow_t(int most, const AttnArgs& a, const TreeRows& rows, int items,
                            hipStream_t s) {
-  const int tile = narrow_tile(most_rows);
-  auto kern = tile == 16   ? narrow_kernel<D, B, 1>
-              : tile == 32 ? narrow_kernel<D, B, 2>
-                           : narrow_kernel<D, B, 4>;
-  hipLaunchKernelGGL(kern, dim3(items), dim3(kThreads), 0, s, rows, a);
+  static_assert(kNarrowRows == 32, "columns");
+  hipLaunchKernelGGL((most <= 16 ? narrow_kernel<D, B, 1> : narrow_kernel<D, B, 2>), dim3(items),
+                     dim3(kThreads), 0, s, rows, a);
   return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_narrow(int d, int block, int most_rows, const AttnArgs& a, const TreeRows& rows,
+hipError_t launch_narrow(int d, int block, int most, const AttnArgs& a, const TreeRows& rows,
                          int items, hipStream_t s) {
-  if (d == 128 && block == 16) return launch_narrow_t<128, 16>(most_rows, a, rows, items, s);
-  if (d == 128) return launch_narrow_t<128, 32>(most_rows, a, rows, items, s);
-  if (block == 16) return launch_narrow_t<64, 16>(most_rows, a, rows, items, s);
-  return launch_narrow_t<64, 32>(most_rows, a, rows, items, s);
+  if (d == 128 && block == 16) return launch_narrow_t<128, 16>(most, a, rows, items, s);
+  if (d == 128) return launch_narrow_t<128, 32>(most, a, rows, items, s);
+  if (block == 16) return launch_narrow_t<64, 16>(most, a, rows, items, s);
+  return launch_narrow_t<64, 32>(most, a, rows, items, s);
 }
 
 hipError_t launch_tree_merge(int d, const AttnArgs& a, const TreeRows& rows, int items,

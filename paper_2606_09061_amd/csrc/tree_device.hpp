@@ -6,6 +6,8 @@
 
 namespace cptree {
 
+typedef uint16_t u16x2_t __attribute__((ext_vector_type(2)));
+
 // The row whose workgroups item b belongs to: as many rows begin at or before
 // it as lanes say so (every lane of a wave looks at two rows).
 __device__ __forceinline__ TreeRow row_of(const TreeRows& rows, int b) {

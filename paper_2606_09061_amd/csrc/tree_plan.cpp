@@ -1,5 +1,4 @@
-// Plan of cp_tree_attn: which kernel a row goes to, the key ranges' pieces and
-// the workspace.
+// Plan of cp_tree_attn: the kernel, the key ranges' pieces and the workspace.
 #include "tree_plan.hpp"
 
 #include <algorithm>
@@ -9,102 +8,126 @@ namespace cptree {
 
 namespace {
 
-constexpr int kCus = 256;  // MI355X
+constexpr int kSlots = 2 * 256;  // workgroups at a time: two on each of MI355X's CUs
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-// A launch's workgroups run `slots` at a time and take `turn` keys per turn; a
-// workgroup costs about `setup` turns besides its keys, and a merge pass
-// `merge`.  Pieces are not cut below `least` keys.
+// Estimated times of a kernel, in us: a turn of `turn` keys while every slot
+// is busy, and alone (bound by the memory's latency); a workgroup's start and
+// end; the merge launch and its 1,000 partial rows.
 struct Cost {
-  int slots, turn, least;
-  double setup, merge;
+  int turn;
+  double loaded, alone, setup, merge, partial;
 };
 
-int64_t workgroups(const std::vector<TreeRow>& rows, const std::vector<int>& per_split,
-                   int64_t piece) {
-  int64_t n = 0;
-  for (size_t i = 0; i < rows.size(); ++i)
-    n += per_split[i] * ((rows[i].start + rows[i].n + piece - 1) / piece);
-  return n;
+struct Load {
+  int64_t n, work, partial;  // workgroups, their turns, partial rows
+  int longest;               // turns of the longest piece
+};
+
+Load load_of(const std::vector<TreeRow>& rows, const std::vector<int>& per_split, int hq, int turn,
+             int piece) {
+  Load l{0, 0, 0, 0};
+  for (size_t i = 0; i < rows.size(); ++i) {
+    const int turns = (rows[i].start + rows[i].n + turn - 1) / turn;
+    const int s = (turns + piece - 1) / piece;
+    l.n += (int64_t)s * per_split[i];
+    l.work += (int64_t)turns * per_split[i];
+    l.longest = std::max(l.longest, std::min(turns, piece));
+    if (s > 1) l.partial += (int64_t)s * rows[i].n * hq;
+  }
+  return l;
 }
 
-// The piece length with the shortest estimated time: the shortest pieces that
-// fill r rounds of the slots, for a few r, or none cut.
-int64_t best_piece(const std::vector<TreeRow>& rows, const std::vector<int>& per_split,
-                   const Cost& c) {
-  int64_t longest = 0, whole = 0;
-  for (size_t i = 0; i < rows.size(); ++i) {
-    longest = std::max<int64_t>(longest, rows[i].start + rows[i].n);
-    whole += per_split[i];
-  }
-  longest = ceil_div(longest, c.turn) * c.turn;
-  const int64_t r0 = ceil_div(whole, c.slots);
-  int64_t best = longest;
-  double time = r0 * ((double)longest / c.turn + c.setup);
-  for (int64_t r = r0; r < r0 + 3; ++r) {
-    int64_t lo = ceil_div(c.least, c.turn), hi = longest / c.turn;  // in turns; hi always fits
+// The estimated time: the slots' share of the work, but at least the longest
+// piece alone; with more workgroups than slots (the longest come first) the
+// slots end apart by a part of a piece.
+double time_of(const Load& l, const Cost& c) {
+  const double merge = l.partial ? c.merge + c.partial * l.partial * 1e-3 : 0.0;
+  if (l.n <= kSlots)
+    return std::max(l.longest * c.alone, l.work * c.loaded / kSlots) + c.setup + merge;
+  const double one = l.longest * c.loaded + c.setup;
+  return (l.work * c.loaded + l.n * c.setup) / kSlots + 0.2 * one + merge;
+}
+
+// The pieces' length in turns: of the whole ranges, their parts, and the
+// shortest pieces that fill the slots once, twice and so on, the one with the
+// shortest estimated time.
+int best_piece(const std::vector<TreeRow>& rows, const std::vector<int>& per_split, int hq,
+               const Cost& c, int least) {
+  const auto load = [&](int piece) { return load_of(rows, per_split, hq, c.turn, piece); };
+  const Load whole = load(1 << 30);  // longer than any range
+  int best = whole.longest;
+  double time = time_of(whole, c);
+  const auto look = [&](int piece) {
+    if (piece >= whole.longest) return;
+    const double t = time_of(load(piece), c);
+    if (t < time) time = t, best = piece;
+  };
+  const int64_t rounds = ceil_div(whole.n, kSlots);
+  int hi = whole.longest;  // fits the rounds before
+  for (int64_t r = rounds; r < rounds + 4 && hi > least; ++r) {
+    int lo = least;
     while (lo < hi) {
-      const int64_t mid = (lo + hi) / 2;
-      if (workgroups(rows, per_split, mid * c.turn) <= r * c.slots) hi = mid;
+      const int mid = (lo + hi) / 2;
+      if (load(mid).n <= r * kSlots) hi = mid;
       else lo = mid + 1;
     }
-    const double t = r * (hi + c.setup) + c.merge;
-    if (hi * c.turn < longest && t < time) time = t, best = hi * c.turn;
+    look(hi);
   }
-  return std::max<int64_t>(best, c.turn);
-}
-
-void cut(TreeLaunch& l, const std::vector<int>& per_split, const Cost& c, int hq, TreePlan& out) {
-  if (l.rows.empty()) return;
-  const int64_t piece = best_piece(l.rows, per_split, c);
-  for (TreeRow& t : l.rows) {
-    const int64_t keys = t.start + t.n, n = ceil_div(keys, piece);
-    t.split_keys = (int32_t)(ceil_div(ceil_div(keys, n), c.turn) * c.turn);
-    t.n_split = (int32_t)ceil_div(keys, t.split_keys);
-    if (t.n_split == 1) continue;
-    const int64_t rows = (int64_t)t.n_split * t.n * hq;
-    if (out.partial_rows + rows > INT_MAX) {  // beyond their index type
-      t.n_split = 1;
-      t.split_keys = (int32_t)(ceil_div(keys, c.turn) * c.turn);
-      continue;
-    }
-    t.part0 = (int32_t)out.partial_rows;
-    out.partial_rows += rows;
-    out.merge.push_back(t);
-  }
-  std::stable_sort(l.rows.begin(), l.rows.end(), [](const TreeRow& a, const TreeRow& b) {
-    return std::min(a.split_keys, a.start + a.n) > std::min(b.split_keys, b.start + b.n);
-  });
+  // few workgroups whatever the pieces: the shortest are not always best
+  if (rounds == 1)
+    for (int n = 2; n <= 8; n *= 2)
+      if (whole.longest / n >= least) look((int)ceil_div(whole.longest, n));
+  return best;
 }
 
 }  // namespace
 
 void plan_tree(const cp_attn_desc& desc, const cp_row_meta* rows, int32_t n_rows, TreePlan& out) {
-  out.narrow.rows.clear();
-  out.wide.rows.clear();
+  out.rows.clear();
   out.merge.clear();
-  out.narrow.most = out.wide.most = 0;
+  out.most = 0;
   out.partial_rows = 0;
   const int hq = desc.num_q_heads, hkv = desc.num_kv_heads, group = hq / hkv;
   int32_t tok = 0;
   for (int32_t r = 0; r < n_rows; ++r) {
     const cp_row_meta& m = rows[r];
     if (m.chunk_len <= 0) continue;
-    TreeLaunch& l = m.chunk_len * group <= kNarrowRows ? out.narrow : out.wide;
-    l.rows.push_back(TreeRow{tok, m.chunk_len, m.chunk_start, m.req_id, 0, 1, 0, 0});
-    l.most = std::max(l.most, m.chunk_len * group);
+    out.rows.push_back(TreeRow{tok, m.chunk_len, m.chunk_start, m.req_id, 0, 1, 0, 0});
+    out.most = std::max(out.most, m.chunk_len * group);
     tok += m.chunk_len;
   }
+  out.off_lse = 0;
+  out.ws_bytes = 256;
+  if (out.rows.empty()) return;
+
   thread_local std::vector<int> per_split;
-  per_split.assign(out.narrow.rows.size(), hkv);
-  cut(out.narrow, per_split, Cost{(out.narrow.most <= 32 ? 2 : 1) * kCus, 128, 256, 1.0, 1.0}, hq,
-      out);
-  const int waves = wide_waves(out.wide.most), tile = 32 * waves;
   per_split.clear();
-  for (const TreeRow& t : out.wide.rows)
-    per_split.push_back(hkv * (int)ceil_div((int64_t)t.n * group, tile));
-  cut(out.wide, per_split, Cost{(waves == 4 ? 2 : 1) * kCus, 64, 256, 2.0, 3.0}, hq, out);
+  for (const TreeRow& t : out.rows) per_split.push_back(hkv * out.tiles(t, group));
+  const double d = desc.head_dim / 128.0;
+  const Cost c = out.wide() ? Cost{64, 2.8 * d, 2.4 * d, 7.0, 3.0, 0.2 * d}
+                            : Cost{128, 5.5 * d, 4.0 * d, 4.0, 4.0, 0.2 * d};
+  const int piece = best_piece(out.rows, per_split, hq, c, 256 / c.turn);
+  for (TreeRow& t : out.rows) {
+    const int turns = (t.start + t.n + c.turn - 1) / c.turn;
+    const int n = (turns + piece - 1) / piece, per = (turns + n - 1) / n;
+    t.split_keys = per * c.turn;
+    t.n_split = (turns + per - 1) / per;
+    if (t.n_split == 1) continue;
+    const int64_t partial = (int64_t)t.n_split * t.n * hq;
+    if (out.partial_rows + partial > INT_MAX) {  // beyond their index type
+      t.split_keys = turns * c.turn;
+      t.n_split = 1;
+      continue;
+    }
+    t.part0 = (int32_t)out.partial_rows;
+    out.partial_rows += partial;
+    out.merge.push_back(t);
+  }
+  std::stable_sort(out.rows.begin(), out.rows.end(), [](const TreeRow& a, const TreeRow& b) {
+    return std::min(a.split_keys, a.start + a.n) > std::min(b.split_keys, b.start + b.n);
+  });
   out.off_lse = (size_t)out.partial_rows * desc.head_dim * 4;
   out.ws_bytes = std::max<size_t>(256, out.off_lse + (size_t)out.partial_rows * 4);
 }

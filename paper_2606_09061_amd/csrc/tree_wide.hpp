@@ -1,7 +1,7 @@
 // Tree attention of many rows: the prefill tile (prefill_tile.inc, where its
 // pipeline is described) with the mask of a drafted tree.
 //
-// A workgroup takes 32 NW of a kv head's rows, 32 a wave, and a piece of the
+// A workgroup takes 128 of a kv head's rows, 32 a wave, and a piece of the
 // key range, 64 keys at a time, K and V copied straight into LDS.  Steps that
 // hold keys of the tree itself mask their scores by a 64-bit window of each
 // row's mask and take infinities and NaN out of the V tile; those are noted,
@@ -17,13 +17,14 @@ namespace cptree {
 
 struct TreeVis {
   static constexpr bool kTree = true;
-  const uint64_t* mask;
-  int words, n, first;  // nodes of the row, its first key of the tree
+  const uint64_t (*mask)[kMaxWords];  // of the tile's nodes, in LDS
+  int words, n, first;                // nodes of the row, its first key of the tree
   unsigned long long* bad;
 
   __device__ __forceinline__ int start() const { return first; }
-  __device__ __forceinline__ uint64_t seen(int t, int k0) const {
-    return seen64(mask + (int64_t)t * words, words, n, k0 - first);
+  // of the tile's node `node`, the keys from k0 on
+  __device__ __forceinline__ uint64_t seen(int node, int k0) const {
+    return seen64(mask[node], words, n, k0 - first);
   }
   // the V tile of keys k0 .. k0 + 63 in LDS
   template <int D, int B, int NW>
@@ -33,15 +34,17 @@ struct TreeVis {
     for (int x = tid; x < SLOTS * D; x += NW * 64) {
       const int sl = x % SLOTS, d = x / SLOTS, k = k0 + sl * 8 - first;
       if (k + 8 <= 0) continue;
-      uint32_t* p = reinterpret_cast<uint32_t*>(
+      uint4* p = reinterpret_cast<uint4*>(
           vb + (L::v_off(sl / (B / 8), d, sl % (B / 8)) - L::K_BYTES));
-      uint32_t found = 0;
+      uint32_t w[4] = {p->x, p->y, p->z, p->w}, found = 0;
+      u16x2_t top = {0, 0};  // of the values without their signs
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        uint32_t w = p[e];
-        found |= clean_word(w, k + 2 * e, n) << (2 * e);
-        p[e] = w;
-      }
+      for (int e = 0; e < 4; ++e)
+        top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2_t, w[e] & 0x7fff7fffu));
+      if (k + 8 <= n && max(top[0], top[1]) < 0x7f80) continue;  // as it should be
+#pragma unroll
+      for (int e = 0; e < 4; ++e) found |= clean_word(w[e], k + 2 * e, n) << (2 * e);
+      *p = make_uint4(w[0], w[1], w[2], w[3]);
       note_bad(bad, found, k);
     }
   }
@@ -52,9 +55,10 @@ namespace {
 using namespace cpattn;
 using namespace cpattn::prefill_impl;
 
-template <int D, int B, int G, int NW>
-__global__ __launch_bounds__(NW * 64, 2) void wide_kernel(const TreeRows rows, const AttnArgs a) {
-  constexpr int RG = 1;  // groups of 32 rows per wave
+template <int D, int B, int G>
+__global__ __launch_bounds__(2 * kWideRows, 2) void wide_kernel(const TreeRows rows,
+                                                                const AttnArgs a) {
+  constexpr int NW = kWideRows / 32, RG = 1;  // waves, groups of 32 rows of each
   using C = PrefillGeom<D, B, NW>;
   using L = PrefillLayout<D, B>;
   constexpr int NKS = C::NKS, NDT = C::NDT, NQK = C::NQK, NPV = C::NPV, PW = C::PW;
@@ -67,9 +71,10 @@ __global__ __launch_bounds__(NW * 64, 2) void wide_kernel(const TreeRows rows, c
   __shared__ __attribute__((aligned(1024))) uint8_t vb0[C::TILE_BYTES];
   __shared__ __attribute__((aligned(1024))) uint8_t vb1[C::TILE_BYTES];
   __shared__ unsigned long long s_bad[kMaxWords];
+  __shared__ uint64_t s_mask[kWideRows / G][kMaxWords];
 
   const TreeRow row = row_of(rows, blockIdx.x);
-  constexpr int kNodes = 32 * NW / G;  // nodes per tile
+  constexpr int kNodes = kWideRows / G;  // nodes per tile
   const int tiles = (row.n + kNodes - 1) / kNodes, units = row.n_split * a.hkv;
   // tiles of the same keys go to the same XCD: eight units at a time, tile by tile
   const int x = (int)blockIdx.x - row.item0;
@@ -90,9 +95,12 @@ __global__ __launch_bounds__(NW * 64, 2) void wide_kernel(const TreeRows rows, c
                 : row.part0 + (kvh_ * row.n_split + split) * row.n * G + tile * kNodes * G;
   it.kvh = kvh_;
   if (threadIdx.x < kMaxWords) s_bad[threadIdx.x] = 0;
+  if (it.kv_end > row.start)  // some of the tree's own keys
+    for (int e = threadIdx.x; e < it.n_tok * a.words; e += 2 * kWideRows)
+      s_mask[e / a.words][e % a.words] = a.mask[(int64_t)it.tok0 * a.words + e];
   __syncthreads();
   using Vis = TreeVis;
-  const Vis vis{a.mask, a.words, row.n, row.start, s_bad};
+  const Vis vis{s_mask, a.words, row.n, row.start, s_bad};
   const uint16_t* q = a.q;
   const uint16_t* k_cache = a.k_cache;
   const uint16_t* v_cache = a.v_cache;
@@ -107,10 +115,10 @@ __global__ __launch_bounds__(NW * 64, 2) void wide_kernel(const TreeRows rows, c
   }
 
   // ---- infinities and NaN that some node sees: rare, and not part of the tile
+  if (!(s_bad[0] | s_bad[1] | s_bad[2] | s_bad[3])) return;  // complete since the last step
   __threadfence_block();
-  __syncthreads();
-  if (!(s_bad[0] | s_bad[1] | s_bad[2] | s_bad[3])) return;
-  for (int e = threadIdx.x; e < it.n_tok * G * D; e += NW * 64) {
+  __syncthreads();  // the tile's rows are written
+  for (int e = threadIdx.x; e < it.n_tok * G * D; e += 2 * kWideRows) {
     const int r = e / D, d = e % D;
     const int64_t t = it.tok0 + r / G;
     const float v = bad_values<D, B>(s_bad, a.mask + t * a.words, a.words, row, a, it.kvh, d);
@@ -124,26 +132,14 @@ __global__ __launch_bounds__(NW * 64, 2) void wide_kernel(const TreeRows rows, c
   }
 }
 
-template <int D, int B, int G>
-hipError_t launch_wide_w(int waves, const AttnArgs& a, const TreeRows& rows, int items,
-                         hipStream_t s) {
-  if (waves == 8)
-    hipLaunchKernelGGL((wide_kernel<D, B, G, 8>), dim3(items), dim3(512), 0, s, rows, a);
-  else
-    hipLaunchKernelGGL((wide_kernel<D, B, G, 4>), dim3(items), dim3(256), 0, s, rows, a);
-  return hipGetLastError();
-}
-
 template <int D, int B>
-hipError_t launch_wide_g(int waves, const AttnArgs& a, const TreeRows& rows, int items,
-                         hipStream_t s) {
-  switch (a.log2_group) {
-    case 0: return launch_wide_w<D, B, 1>(waves, a, rows, items, s);
-    case 1: return launch_wide_w<D, B, 2>(waves, a, rows, items, s);
-    case 2: return launch_wide_w<D, B, 4>(waves, a, rows, items, s);
-    case 3: return launch_wide_w<D, B, 8>(waves, a, rows, items, s);
-  }
-  return hipErrorInvalidValue;
+hipError_t launch_wide_g(const AttnArgs& a, const TreeRows& rows, int items, hipStream_t s) {
+  auto kern = a.log2_group == 0   ? wide_kernel<D, B, 1>
+              : a.log2_group == 1 ? wide_kernel<D, B, 2>
+              : a.log2_group == 2 ? wide_kernel<D, B, 4>
+                                  : wide_kernel<D, B, 8>;
+  hipLaunchKernelGGL(kern, dim3(items), dim3(2 * kWideRows), 0, s, rows, a);
+  return hipGetLastError();
 }
 
 }  // namespace

@@ -3,10 +3,10 @@
 
 namespace cptree {
 
-hipError_t launch_wide64(int block, int waves, const AttnArgs& a, const TreeRows& rows, int items,
+hipError_t launch_wide64(int block, const AttnArgs& a, const TreeRows& rows, int items,
                          hipStream_t s) {
-  return block == 16 ? launch_wide_g<64, 16>(waves, a, rows, items, s)
-                     : launch_wide_g<64, 32>(waves, a, rows, items, s);
+  return block == 16 ? launch_wide_g<64, 16>(a, rows, items, s)
+                     : launch_wide_g<64, 32>(a, rows, items, s);
 }
 
 }  // namespace cptree
