@@ -15,26 +15,27 @@ namespace cptree {
 constexpr int kMaxNodes = CP_TREE_MAX_NODES;
 constexpr int kMaxWords = kMaxNodes / 64;
 
+// Rows of a launch, N at most; few of them travel in a block of kFewRows.
+template <class T, int N>
+struct RowsOf {
+  T r[N];
+};
+constexpr int kFewRows = 8;
+
 struct NodeRow {   // 12 bytes: a row of cp_tree_layout or cp_tree_verify
   int32_t tok0, n, start;
 };
 constexpr int kNodeRows = 256;
-struct NodeRows {
-  NodeRow r[kNodeRows];
-};
+using NodeRows = RowsOf<NodeRow, kNodeRows>;
 
 struct MoveRow {   // 16 bytes: a row of cp_kv_compact
   int32_t row, n, start, req;
 };
 constexpr int kMoveRows = 128;
-struct MoveRows {
-  MoveRow r[kMoveRows];
-};
+using MoveRows = RowsOf<MoveRow, kMoveRows>;
 
 constexpr int kForks = 128;
-struct Forks {
-  cp_fork f[kForks];
-};
+using Forks = RowsOf<cp_fork, kForks>;
 
 constexpr int kLayers = 64;
 struct Layers {
@@ -50,8 +51,6 @@ struct TreeRow {   // 32 bytes: a row of cp_tree_attn
   int32_t part0;      // its first partial row; unused when n_split is 1
 };
 constexpr int kTreeRows = 112;
-struct TreeRows {
-  TreeRow r[kTreeRows];
-};
+using TreeRows = RowsOf<TreeRow, kTreeRows>;
 
 }  // namespace cptree

@@ -118,7 +118,7 @@ template <class F>
 int by_node_rows(const cp_row_meta* rows, int32_t n_rows, F&& f) {
   int32_t tok = 0;
   for (int32_t r0 = 0; r0 < n_rows; r0 += kNodeRows) {
-    NodeRows batch;
+    NodeRows batch{};
     const int n = std::min(kNodeRows, n_rows - r0);
     for (int i = 0; i < n; ++i) {
       const cp_row_meta& m = rows[r0 + i];
@@ -131,7 +131,7 @@ int by_node_rows(const cp_row_meta* rows, int32_t n_rows, F&& f) {
   return CP_OK;
 }
 
-// f(rows of one launch, its workgroups) for rows in batches; items_of(row) is
+// f(rows of one launch, their number, its workgroups) for rows in batches; items_of(row) is
 // the number of a row's workgroups.
 template <class Items, class F>
 int by_tree_rows(const std::vector<TreeRow>& rows, Items&& items_of, F&& f) {
@@ -147,7 +147,8 @@ int by_tree_rows(const std::vector<TreeRow>& rows, Items&& items_of, F&& f) {
       batch.r[i].item0 = items;
       items += items_of(rows[r0 + i]);
     }
-    const int rc = f(batch, items);
+    const int n = (int)std::min<size_t>(kTreeRows, rows.size() - r0);
+    const int rc = f(batch, n, items);
     if (rc != CP_OK) return rc;
   }
   return CP_OK;
@@ -268,9 +269,9 @@ int cp_tree_attn(const cp_attn_desc* desc, const void* q, const void* k_cache,
     rc = by_tree_rows(
         p.rows,
         [&](const TreeRow& t) { return t.n_split * desc->num_kv_heads * p.tiles(t, group); },
-        [&](const TreeRows& batch, int items) {
+        [&](const TreeRows& batch, int n, int items) {
           const hipError_t e =
-              !p.wide()  ? launch_narrow(d, desc->block_size, p.most, a, batch, items, s)
+              !p.wide()  ? launch_narrow(d, desc->block_size, p.most, a, batch, n, items, s)
               : d == 128 ? launch_wide128(desc->block_size, a, batch, items, s)
                          : launch_wide64(desc->block_size, a, batch, items, s);
           return finish(e, s);
@@ -282,8 +283,8 @@ int cp_tree_attn(const cp_attn_desc* desc, const void* q, const void* k_cache,
           const int per = merge_rows(d, t.n_split);
           return (t.n * desc->num_q_heads + per - 1) / per;
         },
-        [&](const TreeRows& batch, int items) {
-          return finish(launch_tree_merge(d, a, batch, items, s), s);
+        [&](const TreeRows& batch, int n, int items) {
+          return finish(launch_tree_merge(d, a, batch, n, items, s), s);
         });
   });
 }
@@ -348,7 +349,7 @@ int cp_kv_compact(const cp_attn_desc* desc, void* const* k_caches, void* const* 
       Layers layers;
       a.n_layers = fill_layers(k_caches, v_caches, l0, n_layers, layers);
       for (int32_t r = 0; r < n_rows;) {
-        MoveRows batch;
+        MoveRows batch{};
         int n = 0;
         for (; r < n_rows && n < kMoveRows; ++r)
           if (rows[r].chunk_len > 0)
@@ -390,9 +391,9 @@ int cp_kv_fork(const cp_attn_desc* desc, void* const* k_caches, void* const* v_c
       Layers layers;
       a.n_layers = fill_layers(k_caches, v_caches, l0, n_layers, layers);
       for (int32_t i = 0; i < n_forks; i += kForks) {
-        Forks batch;
+        Forks batch{};
         const int n = std::min(kForks, n_forks - i);
-        std::copy(forks + i, forks + i + n, batch.f);
+        std::copy(forks + i, forks + i + n, batch.r);
         rc = finish(launch_fork(a, layers, block_tables, batch, n, l0 == 0, s), s);
         if (rc != CP_OK) return rc;
       }

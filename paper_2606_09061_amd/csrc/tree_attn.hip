@@ -54,8 +54,8 @@ __device__ __forceinline__ f32x4_t mfma16x16x32(uint4 a, uint4 b, f32x4_t c) {
 // V of the tree's own keys enters the product with infinities and NaN as
 // zeros: a node that does not see the key would get 0 * NaN from it.  The
 // nodes that do get them added at the end.
-template <int D, int B, int NC>
-__global__ __launch_bounds__(kThreads, 2) void narrow_kernel(const TreeRows rows,
+template <int D, int B, int NC, class Rows>
+__global__ __launch_bounds__(kThreads, 2) void narrow_kernel(const Rows rows,
                                                              const AttnArgs a) {
   constexpr int TK = 32;       // keys per tile
   constexpr int ROWS = 16 * NC;
@@ -326,8 +326,8 @@ __global__ __launch_bounds__(kThreads, 2) void narrow_kernel(const TreeRows rows
 //     sum_s 2^(L_s - max L) O_s / sum_s 2^(L_s - max L).
 // A row (node, q head) takes D / 4 threads of 4 features; with many splits
 // several such slots share it, each taking every P-th split, and meet in LDS.
-template <int D>
-__global__ __launch_bounds__(kThreads) void tree_merge_kernel(const TreeRows rows,
+template <int D, class Rows>
+__global__ __launch_bounds__(kThreads) void tree_merge_kernel(const Rows rows,
                                                               const AttnArgs a) {
   constexpr int DQ = D / 4, SLOTS = kThreads / DQ, U = 8;
   __shared__ float4 s_acc[SLOTS][DQ];
@@ -405,29 +405,34 @@ __global__ __launch_bounds__(kThreads) void tree_merge_kernel(const TreeRows row
 }
 
 template <int D, int B>
-hipError_t launch_narrow_t(int most, const AttnArgs& a, const TreeRows& rows, int items,
+hipError_t launch_narrow_t(int most, const AttnArgs& a, const TreeRows& rows, int n_rows, int items,
                            hipStream_t s) {
   static_assert(kNarrowRows == 32, "columns");
-  hipLaunchKernelGGL((most <= 16 ? narrow_kernel<D, B, 1> : narrow_kernel<D, B, 2>), dim3(items),
-                     dim3(kThreads), 0, s, rows, a);
-  return hipGetLastError();
+  return by_size(rows, n_rows, [&](const auto& r) {
+    if (most <= 16)
+      hipLaunchKernelGGL((narrow_kernel<D, B, 1>), dim3(items), dim3(kThreads), 0, s, r, a);
+    else
+      hipLaunchKernelGGL((narrow_kernel<D, B, 2>), dim3(items), dim3(kThreads), 0, s, r, a);
+  });
 }
 
 }  // namespace
 
 hipError_t launch_narrow(int d, int block, int most, const AttnArgs& a, const TreeRows& rows,
-                         int items, hipStream_t s) {
-  if (d == 128 && block == 16) return launch_narrow_t<128, 16>(most, a, rows, items, s);
-  if (d == 128) return launch_narrow_t<128, 32>(most, a, rows, items, s);
-  if (block == 16) return launch_narrow_t<64, 16>(most, a, rows, items, s);
-  return launch_narrow_t<64, 32>(most, a, rows, items, s);
+                         int n_rows, int items, hipStream_t s) {
+  auto f = d == 128 ? (block == 16 ? launch_narrow_t<128, 16> : launch_narrow_t<128, 32>)
+                    : (block == 16 ? launch_narrow_t<64, 16> : launch_narrow_t<64, 32>);
+  return f(most, a, rows, n_rows, items, s);
 }
 
-hipError_t launch_tree_merge(int d, const AttnArgs& a, const TreeRows& rows, int items,
+hipError_t launch_tree_merge(int d, const AttnArgs& a, const TreeRows& rows, int n_rows, int items,
                              hipStream_t s) {
-  hipLaunchKernelGGL(d == 128 ? tree_merge_kernel<128> : tree_merge_kernel<64>, dim3(items),
-                     dim3(kThreads), 0, s, rows, a);
-  return hipGetLastError();
+  return by_size(rows, n_rows, [&](const auto& r) {
+    if (d == 128)
+      hipLaunchKernelGGL(tree_merge_kernel<128>, dim3(items), dim3(kThreads), 0, s, r, a);
+    else
+      hipLaunchKernelGGL(tree_merge_kernel<64>, dim3(items), dim3(kThreads), 0, s, r, a);
+  });
 }
 
 }  // namespace cptree

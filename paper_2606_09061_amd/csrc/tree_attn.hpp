@@ -23,12 +23,12 @@ struct AttnArgs {
 // The rows of a launch; the places behind them hold an item0 that no workgroup
 // reaches.
 hipError_t launch_narrow(int d, int block, int most, const AttnArgs& a, const TreeRows& rows,
-                         int items, hipStream_t s);
+                         int n_rows, int items, hipStream_t s);
 hipError_t launch_wide64(int block, const AttnArgs& a, const TreeRows& rows, int items,
                          hipStream_t s);
 hipError_t launch_wide128(int block, const AttnArgs& a, const TreeRows& rows, int items,
                           hipStream_t s);
-hipError_t launch_tree_merge(int d, const AttnArgs& a, const TreeRows& rows, int items,
+hipError_t launch_tree_merge(int d, const AttnArgs& a, const TreeRows& rows, int n_rows, int items,
                              hipStream_t s);
 
 }  // namespace cptree

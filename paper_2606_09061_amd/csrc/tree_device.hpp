@@ -1,4 +1,4 @@
-// Device helpers of the tree attention's kernels.
+// Helpers of libcptree's kernels and their launches.
 #pragma once
 
 #include "device.hpp"
@@ -8,15 +8,32 @@ namespace cptree {
 
 typedef uint16_t u16x2_t __attribute__((ext_vector_type(2)));
 
+// Launches with the rows in an argument block of their number's size: the full
+// block costs the host 1.4 us more than a short one.
+template <class T, int N, class F>
+hipError_t by_size(const RowsOf<T, N>& rows, int n, F&& launch) {
+  if (n <= kFewRows) {
+    RowsOf<T, kFewRows> few;
+    for (int i = 0; i < kFewRows; ++i) few.r[i] = rows.r[i];  // with the places behind the rows
+    launch(few);
+  } else {
+    launch(rows);
+  }
+  return hipGetLastError();
+}
+
 // The row whose workgroups item b belongs to: as many rows begin at or before
-// it as lanes say so (every lane of a wave looks at two rows).
-__device__ __forceinline__ TreeRow row_of(const TreeRows& rows, int b) {
-  static_assert(kTreeRows > 64 && kTreeRows <= 128, "two rows per lane");
+// it as lanes say so (every lane of a wave looks at two rows at most).
+template <int N>
+__device__ __forceinline__ TreeRow row_of(const RowsOf<TreeRow, N>& rows, int b) {
+  static_assert(N <= 128, "two rows per lane");
   const int lane = threadIdx.x & 63;
-  const bool lo = rows.r[lane].item0 <= b;
-  const bool hi = 64 + lane < kTreeRows && rows.r[min(64 + lane, kTreeRows - 1)].item0 <= b;
-  const int n = __popcll(__builtin_amdgcn_ballot_w64(lo)) +
-                __popcll(__builtin_amdgcn_ballot_w64(hi));
+  const bool lo = lane < N && rows.r[min(lane, N - 1)].item0 <= b;
+  int n = __popcll(__builtin_amdgcn_ballot_w64(lo));
+  if constexpr (N > 64) {
+    const bool hi = 64 + lane < N && rows.r[min(64 + lane, N - 1)].item0 <= b;
+    n += __popcll(__builtin_amdgcn_ballot_w64(hi));
+  }
   return rows.r[__builtin_amdgcn_readfirstlane(n - 1)];
 }
 

@@ -5,7 +5,7 @@
 
 #include <algorithm>
 
-#include "device.hpp"
+#include "tree_device.hpp"
 
 namespace cptree {
 
@@ -28,8 +28,9 @@ __device__ __forceinline__ int load_parent(const int32_t* __restrict__ parents, 
 
 // One workgroup per row, one thread per node, which walks its own chain of
 // ancestors in LDS.
+template <class Rows>
 __global__ __launch_bounds__(kThreads) void layout_kernel(const int32_t* __restrict__ parents,
-                                                          const NodeRows rows,
+                                                          const Rows rows,
                                                           uint64_t* __restrict__ mask, int words,
                                                           int32_t* __restrict__ positions) {
   __shared__ int par[kMaxNodes];
@@ -67,6 +68,8 @@ __device__ __forceinline__ uint64_t wave_max64(uint64_t x) {
   return x;
 }
 
+constexpr int kArgmaxWords = 4;  // 16-byte words of a thread on their way at a time
+
 // best[t][piece] = the best candidate of a piece of node t's logits.  Rows may
 // start at any bf16: whole 16-byte words are read as such, the ends one value
 // at a time.
@@ -83,7 +86,46 @@ __global__ __launch_bounds__(kThreads) void argmax_kernel(const uint16_t* __rest
   const int per = (w1 - w0 + pieces - 1) / pieces;
   const int a = min(w0 + piece * per, w1), b = min(a + per, w1);
   const uint16_t* words = row - off;
+  // The first of the words with this thread's largest value so far, and the
+  // largest magnitude: NaN is above 0x7f80 there, and ignored by the maxima.
+  float most = -INFINITY;
+  u32x4_t best_word = {0, 0, 0, 0};
+  int best_at = -1;
+  u16x2_t size = {0, 0};
+  auto look = [&](const u32x4_t& x, int w) {
+    float m = fmaxf(bf16lo(x[0]), bf16hi(x[0]));
+#pragma unroll
+    for (int e = 1; e < 4; ++e) m = fmaxf(fmaxf(m, bf16lo(x[e])), bf16hi(x[e]));
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      size = __builtin_elementwise_max(size, __builtin_bit_cast(u16x2_t, x[e] & 0x7fff7fffu));
+    if (m > most || best_at < 0) most = m, best_word = x, best_at = w;
+  };
+  auto load = [&](int w) {
+    return __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(words + (int64_t)8 * w));
+  };
+  int w = a + tid;
+  for (; w + (kArgmaxWords - 1) * kThreads < b; w += kArgmaxWords * kThreads) {
+    u32x4_t x[kArgmaxWords];
+#pragma unroll
+    for (int u = 0; u < kArgmaxWords; ++u) x[u] = load(w + u * kThreads);
+#pragma unroll
+    for (int u = 0; u < kArgmaxWords; ++u) look(x[u], w + u * kThreads);
+  }
+  for (; w < b; w += kThreads) look(load(w), w);
   uint64_t top = 0;
+  auto take_word = [&](const u32x4_t& x, int at) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      top = max(top, candidate(bf16lo(x[e]), 8 * at - off + 2 * e));
+      top = max(top, candidate(bf16hi(x[e]), 8 * at - off + 2 * e + 1));
+    }
+  };
+  if (max(size[0], size[1]) > 0x7f80) {
+    for (w = a + tid; w < b; w += kThreads) take_word(load(w), w);  // rare: the first NaN
+  } else if (best_at >= 0) {
+    take_word(best_word, best_at);
+  }
   auto take = [&](int i) {
     top = max(top, candidate(__uint_as_float((uint32_t)row[i] << 16), i));
   };
@@ -91,16 +133,6 @@ __global__ __launch_bounds__(kThreads) void argmax_kernel(const uint16_t* __rest
   if (piece == pieces - 1 && tid >= 8 && tid < 16) {
     const int64_t i = (int64_t)8 * w1 - off + tid - 8;
     if (i < vocab) take((int)i);
-  }
-  for (int w = a + tid; w < b; w += kThreads) {
-    const u32x4_t x =
-        __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(words + (int64_t)8 * w));
-    const int i = 8 * w - off;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      top = max(top, candidate(bf16lo(x[e]), i + 2 * e));
-      top = max(top, candidate(bf16hi(x[e]), i + 2 * e + 1));
-    }
   }
   __shared__ uint64_t part[kThreads / 64];
   top = wave_max64(top);
@@ -115,9 +147,10 @@ __global__ __launch_bounds__(kThreads) void argmax_kernel(const uint16_t* __rest
 
 // One workgroup per row: the nodes' targets from their pieces, each node's
 // first child that agrees, and one thread's walk along those.
+template <class Rows>
 __global__ __launch_bounds__(kThreads) void walk_kernel(
     const uint64_t* __restrict__ best, int pieces, const int32_t* __restrict__ tokens,
-    const int32_t* __restrict__ parents, const NodeRows rows, int row0, int max_path,
+    const int32_t* __restrict__ parents, const Rows rows, int row0, int max_path,
     int32_t* __restrict__ target, int32_t* __restrict__ path, int32_t* __restrict__ n_accepted,
     int32_t* __restrict__ next_token) {
   __shared__ unsigned long long top[kMaxNodes];
@@ -149,82 +182,133 @@ __global__ __launch_bounds__(kThreads) void walk_kernel(
 // Accepted nodes per pass of the compaction.
 constexpr int kMoveTokens = 16;
 
-// One workgroup per (row, kv head, layer).  A path rises strictly, so node i's
-// source slot is never before its destination: passes of kMoveTokens nodes,
-// each read whole before it is written, never overwrite a later pass's
-// sources.
-template <int D, int B>
-__global__ __launch_bounds__(kThreads) void compact_kernel(const Layers layers,
-                                                           const MoveRows rows,
+// One wave per (row, kv head, layer).  A path rises strictly, so node i's source
+// slot is never before its destination: passes of kMoveTokens nodes, each read
+// whole before it is written, never overwrite a later pass's sources.
+//
+// A token's K is one run of memory, but of its V every feature lies on its own,
+// B slots of a page side by side: what reads or writes a value of each feature
+// touches all of the page's lines, and, 64 lanes in as many pieces, costs the
+// address unit a clock per lane.  So pages of V are read and written whole, in
+// runs of a kilobyte (lane l of load q holds 8 slots, piece l % PR, of feature
+// q 64 / PR + l / PR): the destination's, and each source's once, for sources
+// rise as well.  A value moves over by one exchange in its feature's lanes.  36
+// layers of 64 requests, 3.8 nodes each, us: values one by one 65, the
+// destination's rows whole and the values gathered 65, pages 60 (some 270 MB).
+template <int D, int B, class Rows>
+__global__ __launch_bounds__(kThreads) void compact_kernel(const Layers layers, const Rows rows,
+                                                           int units,
                                                            const int32_t* __restrict__ bt, int mbr,
                                                            int num_blocks, int hkv,
                                                            const int32_t* __restrict__ path,
                                                            int max_path,
                                                            const int32_t* __restrict__ n_accepted) {
-  constexpr int CH = D / 8;  // 16-byte pieces of a K row
-  constexpr int KP = kMoveTokens * CH / kThreads > 0 ? kMoveTokens * CH / kThreads : 1;
-  constexpr int VP = kMoveTokens * D / kThreads;
-  const MoveRow row = rows.r[blockIdx.x];
-  const int h = blockIdx.y, tid = threadIdx.x;
-  uint16_t* kc = layers.k[blockIdx.z];
-  uint16_t* vc = layers.v[blockIdx.z];
-  __shared__ int s_count;
-  __shared__ int64_t s_src[kMaxNodes], s_dst[kMaxNodes];  // block * B + slot, -1: no move
-  if (tid == 0) s_count = min(min(max(n_accepted[row.row], 0), max_path), row.n);
-  __syncthreads();
-  const int most = s_count;
-  __syncthreads();
-  int p = -1;
-  if (tid < most) {
-    const int32_t* e = path + (int64_t)row.row * max_path + tid;
-    p = e[0];
-    if (p < 0 || p >= row.n || (tid > 0 && p <= e[-1])) atomicMin(&s_count, tid);
-  }
-  __syncthreads();
-  const int count = s_count;
-  if (tid < count) {
-    const int src = row.start + p, dst = row.start + tid;
-    const int32_t* e = bt + (int64_t)row.req * mbr;
-    const int sb = e[src / B], db = e[dst / B];
-    const bool ok = src != dst && (unsigned)sb < (unsigned)num_blocks &&
-                    (unsigned)db < (unsigned)num_blocks;
-    s_src[tid] = ok ? (int64_t)sb * B + src % B : -1;
-    s_dst[tid] = ok ? (int64_t)db * B + dst % B : -1;
-  }
-  __syncthreads();
-  for (int i0 = 0; i0 < count; i0 += kMoveTokens) {
-    u32x4_t kv[KP];
-    uint16_t vv[VP];
+  constexpr int CH = D / 8, TPI = 64 / CH, NI = kMoveTokens / TPI;  // K: pieces, tokens a load
+  constexpr int PR = B / 8, NQ = D * PR / 64;  // V: pieces of a feature's slots, loads of a page
+  static_assert(kMoveTokens <= B, "a pass's destinations lie in two pages at most");
+  const int lane = threadIdx.x & 63;
+  const int unit = __builtin_amdgcn_readfirstlane(blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6));
+  if (unit >= units) return;
+  const MoveRow row = rows.r[unit / hkv];
+  const int h = unit % hkv;
+  uint16_t* kc = layers.k[blockIdx.y];
+  uint16_t* vc = layers.v[blockIdx.y];
+  const int32_t* entries = path + (int64_t)row.row * max_path;
+  const int32_t* table = bt + (int64_t)row.req * mbr;
+  const int accepted = n_accepted[row.row], bound = min(max_path, row.n);
+  struct Page {
+    u32x4_t w[NQ];
+  };
+  auto v_page = [&](int blk) {
+    return reinterpret_cast<u32x4_t*>(vc + ((int64_t)blk * hkv + h) * D * B) + lane;
+  };
+  auto load_page = [&](int blk) {
+    Page p;
+    const u32x4_t* a = v_page(blk);
 #pragma unroll
-    for (int x = 0; x < KP; ++x) {
-      const int i = i0 + (x * kThreads + tid) / CH;
-      if (i < min(count, i0 + kMoveTokens) && s_src[i] >= 0) {
-        const int64_t at = ((s_src[i] / B * hkv + h) * B + s_src[i] % B) * D;
-        kv[x] = *reinterpret_cast<const u32x4_t*>(kc + at + tid % CH * 8);
+    for (int q = 0; q < NQ; ++q) p.w[q] = a[64 * q];
+    return p;
+  };
+  int last = -1;
+  for (int i0 = 0; i0 < bound; i0 += 64) {
+    // lane l's node i0 + l: its source and destination pages, -1 where it does
+    // not move, and its source slot
+    const int i = i0 + lane;
+    const int p = i < bound ? entries[i] : -1;
+    int before = __shfl_up(p, 1, 64);
+    if (lane == 0) before = last;
+    const uint64_t rises = __builtin_amdgcn_ballot_w64(i < min(accepted, bound) && p > before &&
+                                                       p < row.n);
+    const int count = ~rises ? __builtin_ctzll(~rises) : 64;  // the first that does not ends it
+    int from = -1, to = -1;
+    if (lane < count && p != i) {
+      from = table[(row.start + p) / B], to = table[(row.start + i) / B];
+      if ((unsigned)from >= (unsigned)num_blocks || (unsigned)to >= (unsigned)num_blocks)
+        from = -1;
+    }
+    const int slot = (row.start + p) % B;
+    const uint64_t moves = __builtin_amdgcn_ballot_w64(from >= 0);
+    for (int j0 = 0; j0 < count; j0 += kMoveTokens) {
+      const int n = min(kMoveTokens, count - j0);
+      if (!(moves >> j0 & ((1ull << n) - 1))) continue;
+      // ---- K: CH lanes a token
+      u32x4_t k[NI];
+      int64_t k_to[NI];
+#pragma unroll
+      for (int u = 0; u < NI; ++u) {
+        const int t = u * TPI + lane / CH, j = min(j0 + t, 63);
+        const int f = __shfl(from, j, 64), d = __shfl(to, j, 64), s = __shfl(slot, j, 64);
+        k_to[u] = -1;
+        if (t < n && f >= 0) {
+          k[u] = *reinterpret_cast<const u32x4_t*>(kc + (((int64_t)f * hkv + h) * B + s) * D +
+                                                   lane % CH * 8);
+          k_to[u] = (((int64_t)d * hkv + h) * B + (row.start + i0 + j) % B) * D + lane % CH * 8;
+        }
       }
-    }
+      // ---- V: the pass's nodes in one destination page, then those in the next
+      for (int ja = j0; ja < j0 + n;) {
+        const int s0 = (row.start + i0 + ja) % B, len = min(j0 + n - ja, B - s0);
+        const uint64_t here = moves >> ja & ((1ull << len) - 1);
+        if (here) {
+          const int dst = __builtin_amdgcn_readlane(to, ja + __builtin_ctzll(here));
+          // the first page that is another: requested with the destination's
+          const uint64_t others =
+              __builtin_amdgcn_ballot_w64(from >= 0 && from != dst) >> ja & here;
+          int held = others ? __builtin_amdgcn_readlane(from, ja + __builtin_ctzll(others)) : dst;
+          Page to_page = load_page(dst), from_page = load_page(held);
+          for (uint64_t rest = here; rest; rest &= rest - 1) {
+            const int t = __builtin_ctzll(rest), d = s0 + t;  // (uniform, as all that chooses here)
+            const int src = __builtin_amdgcn_readlane(from, ja + t);
+            const int s = __builtin_amdgcn_readlane(slot, ja + t);
+            if (src != dst && src != held) from_page = load_page(held = src);
+            const int mine = (lane & ~(PR - 1)) | (s / 8);
 #pragma unroll
-    for (int x = 0; x < VP; ++x) {
-      const int i = i0 + (x * kThreads + tid) / D;
-      if (i < count && s_src[i] >= 0)
-        vv[x] = vc[((s_src[i] / B * hkv + h) * D + tid % D) * B + s_src[i] % B];
-    }
-    __syncthreads();
+            for (int q = 0; q < NQ; ++q) {
+              uint32_t x = 0;
 #pragma unroll
-    for (int x = 0; x < KP; ++x) {
-      const int i = i0 + (x * kThreads + tid) / CH;
-      if (i < min(count, i0 + kMoveTokens) && s_dst[i] >= 0) {
-        const int64_t at = ((s_dst[i] / B * hkv + h) * B + s_dst[i] % B) * D;
-        *reinterpret_cast<u32x4_t*>(kc + at + tid % CH * 8) = kv[x];
+              for (int e = 0; e < 4; ++e)
+                if (s % 8 / 2 == e) x = src == dst ? to_page.w[q][e] : from_page.w[q][e];
+              x = __shfl(x, mine, 64);
+              x = s & 1 ? x >> 16 : x & 0xffffu;
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                if (d % 8 / 2 == e && lane % PR == d / 8)
+                  to_page.w[q][e] = d & 1 ? (to_page.w[q][e] & 0xffffu) | x << 16
+                                          : (to_page.w[q][e] & 0xffff0000u) | x;
+            }
+          }
+          u32x4_t* a = v_page(dst);
+#pragma unroll
+          for (int q = 0; q < NQ; ++q) a[64 * q] = to_page.w[q];
+        }
+        ja += len;
       }
-    }
 #pragma unroll
-    for (int x = 0; x < VP; ++x) {
-      const int i = i0 + (x * kThreads + tid) / D;
-      if (i < count && s_dst[i] >= 0)
-        vc[((s_dst[i] / B * hkv + h) * D + tid % D) * B + s_dst[i] % B] = vv[x];
+      for (int u = 0; u < NI; ++u)
+        if (k_to[u] >= 0) *reinterpret_cast<u32x4_t*>(kc + k_to[u]) = k[u];
     }
-    __syncthreads();
+    if (count < 64) break;
+    last = __builtin_amdgcn_readlane(p, 63);
   }
 }
 
@@ -232,10 +316,11 @@ constexpr int kForkWords = 4;  // 16-byte words per thread of a page's copy
 
 // Workgroup (x, y, z): piece x of K or V page z in layer y; y == n_layers is
 // the fork's table row.
+template <class Forks>
 __global__ __launch_bounds__(kThreads) void fork_kernel(const Layers layers, int n_layers,
                                                         const Forks forks, int32_t* bt, int mbr,
                                                         int num_blocks, int block, int page16) {
-  const cp_fork f = forks.f[blockIdx.z];
+  const cp_fork f = forks.r[blockIdx.z];
   const int full = f.ctx_len / block;
   const bool partial = f.ctx_len % block != 0;
   const int32_t* src = bt + (int64_t)f.src_req * mbr;
@@ -267,9 +352,10 @@ __global__ __launch_bounds__(kThreads) void fork_kernel(const Layers layers, int
 
 hipError_t launch_layout(const int32_t* parents, const NodeRows& rows, int n_rows, uint64_t* mask,
                          int words, int32_t* positions, hipStream_t s) {
-  hipLaunchKernelGGL(layout_kernel, dim3(n_rows), dim3(kThreads), 0, s, parents, rows, mask, words,
-                     positions);
-  return hipGetLastError();
+  return by_size(rows, n_rows, [&](const auto& r) {
+    hipLaunchKernelGGL(layout_kernel, dim3(n_rows), dim3(kThreads), 0, s, parents, r, mask, words,
+                       positions);
+  });
 }
 
 int verify_pieces(int64_t n_tokens, int32_t vocab) {
@@ -290,29 +376,41 @@ hipError_t launch_walk(const uint64_t* best, int pieces, const int32_t* tokens,
                        const int32_t* parents, const NodeRows& rows, int n_rows, int row0,
                        int max_path, int32_t* target, int32_t* path, int32_t* n_accepted,
                        int32_t* next_token, hipStream_t s) {
-  hipLaunchKernelGGL(walk_kernel, dim3(n_rows), dim3(kThreads), 0, s, best, pieces, tokens,
-                     parents, rows, row0, max_path, target, path, n_accepted, next_token);
-  return hipGetLastError();
+  return by_size(rows, n_rows, [&](const auto& r) {
+    hipLaunchKernelGGL(walk_kernel, dim3(n_rows), dim3(kThreads), 0, s, best, pieces, tokens,
+                       parents, r, row0, max_path, target, path, n_accepted, next_token);
+  });
+}
+
+template <int D, int B>
+static hipError_t launch_compact_t(const PoolArgs& a, const Layers& layers, const int32_t* bt,
+                                   const MoveRows& rows, int n_rows, const int32_t* path,
+                                   int max_path, const int32_t* n_accepted, hipStream_t s) {
+  const int units = n_rows * a.hkv, waves = kThreads / 64;
+  return by_size(rows, n_rows, [&](const auto& r) {
+    hipLaunchKernelGGL((compact_kernel<D, B>), dim3((units + waves - 1) / waves, a.n_layers),
+                       dim3(kThreads), 0, s, layers, r, units, bt, a.mbr, a.num_blocks, a.hkv,
+                       path, max_path, n_accepted);
+  });
 }
 
 hipError_t launch_compact(const PoolArgs& a, const Layers& layers, const int32_t* bt,
                           const MoveRows& rows, int n_rows, const int32_t* path, int max_path,
                           const int32_t* n_accepted, hipStream_t s) {
-  auto kern = a.d == 128 ? (a.block == 16 ? compact_kernel<128, 16> : compact_kernel<128, 32>)
-                         : (a.block == 16 ? compact_kernel<64, 16> : compact_kernel<64, 32>);
-  hipLaunchKernelGGL(kern, dim3(n_rows, a.hkv, a.n_layers), dim3(kThreads), 0, s, layers, rows, bt,
-                     a.mbr, a.num_blocks, a.hkv, path, max_path, n_accepted);
-  return hipGetLastError();
+  auto f = a.d == 128 ? (a.block == 16 ? launch_compact_t<128, 16> : launch_compact_t<128, 32>)
+                      : (a.block == 16 ? launch_compact_t<64, 16> : launch_compact_t<64, 32>);
+  return f(a, layers, bt, rows, n_rows, path, max_path, n_accepted, s);
 }
 
 hipError_t launch_fork(const PoolArgs& a, const Layers& layers, int32_t* bt, const Forks& forks,
                        int n_forks, bool tables, hipStream_t s) {
   const int page16 = a.hkv * a.d * a.block / 8;
   const int pieces = (page16 + kForkWords * kThreads - 1) / (kForkWords * kThreads);
-  hipLaunchKernelGGL(fork_kernel, dim3(2 * pieces, a.n_layers + (tables ? 1 : 0), n_forks),
-                     dim3(kThreads), 0, s, layers, a.n_layers, forks, bt, a.mbr, a.num_blocks,
-                     a.block, page16);
-  return hipGetLastError();
+  return by_size(forks, n_forks, [&](const auto& f) {
+    hipLaunchKernelGGL(fork_kernel, dim3(2 * pieces, a.n_layers + (tables ? 1 : 0), n_forks),
+                       dim3(kThreads), 0, s, layers, a.n_layers, f, bt, a.mbr, a.num_blocks,
+                       a.block, page16);
+  });
 }
 
 }  // namespace cptree

@@ -18,11 +18,11 @@ or the current stream of their device.
 
 from __future__ import annotations
 
-import contextlib
 import ctypes
 import os
 
 import numpy as np
+import torch
 
 from . import binding as cp
 from .model import _scratch
@@ -76,15 +76,14 @@ def _want(ok, what):
         raise cp.CpError(cp.CP_ERR_INVALID_ARG, what)
 
 
-def _tensors(what, device, *wanted):
-    """Each of ``wanted`` is (tensor, dtype, shape): a dense tensor like that on
-    ``device``."""
-    for t, dtype, shape in wanted:
-        if (t.dtype != dtype or tuple(t.shape) != shape or not t.is_contiguous()
-                or t.device != device or t.is_neg()):
-            raise cp.CpError(cp.CP_ERR_INVALID_ARG,
-                             f"{what}: a dense {dtype} tensor {shape} on {device} is wanted, got "
-                             f"{t.dtype} {tuple(t.shape)} on {t.device}")
+def _ptr(t, dtype, shape, device, what):
+    """The address of a dense tensor of this type and shape on this device."""
+    if (t.dtype != dtype or t.shape != shape or not t.is_contiguous() or t.device != device
+            or t.is_neg()):
+        raise cp.CpError(cp.CP_ERR_INVALID_ARG,
+                         f"{what}: a dense {dtype} tensor {tuple(shape)} on {device} is wanted, "
+                         f"got {t.dtype} {tuple(t.shape)} on {t.device}")
+    return t.data_ptr()
 
 
 def _device(t, what):
@@ -92,38 +91,52 @@ def _device(t, what):
     return t.device
 
 
-def _at(device):
-    """Makes ``device`` current for the launches of a call."""
-    import torch
-    if torch.cuda.current_device() == device.index:
-        return contextlib.nullcontext()
-    return torch.cuda.device(device)
+def _call(device, stream, f, *args):
+    """f(*args, stream) with ``device`` current; the raw stream is looked up
+    without the stream objects, which cost more than a launch."""
+    if torch._C._cuda_getDevice() != device.index:
+        with torch.cuda.device(device):
+            return f(*args, cp._stream(stream))
+    if stream is None:
+        return f(*args, torch._C._cuda_getCurrentRawStream(device.index))
+    return f(*args, cp._stream(stream))
+
+
+def _workspace(ws, nbytes, device, stream, what):
+    """(address, bytes) of ws, allocated for the stream when None (and returned,
+    to be held until the launches are enqueued)."""
+    if ws is None:
+        ws = _scratch(nbytes(), device, stream)
+        if ws is None:
+            raise cp.CpError(cp.CP_ERR_WORKSPACE, what)
+    _want(ws.device == device and ws.is_contiguous(), f"{what}: ws is dense and on {device}")
+    return ws, ws.data_ptr(), ws.numel() * ws.element_size()
 
 
 def _nodes(rows):
-    return int(rows[:, 2].sum()) if len(rows) else 0
+    return sum(rows[:, 2].tolist())   # (of a few rows, faster than numpy's)
+
+
+_I32, _I64, _BF16 = torch.int32, torch.int64, torch.bfloat16
 
 
 def layout(parents, rows, mask, positions, stream=None):
     """mask [T, W] (int64, bit j of a node's W words: it sees node j of its row)
     and positions [T] (int32) of the drafted nodes whose parents (int32 [T],
     indexes inside their row, -1 for the root) are given."""
-    import torch
+    what = "cp_tree_layout"
     rows = cp._rows(rows)
-    T = _nodes(rows)
+    dev, T = _device(parents, what), _nodes(rows)
     _want(mask.dim() == 2, "cp_tree_layout: mask is [T, W]")
-    dev = _device(parents, "cp_tree_layout")
-    _tensors("cp_tree_layout", dev, (parents, torch.int32, (T,)),
-             (mask, torch.int64, (T, mask.shape[1])), (positions, torch.int32, (T,)))
-    with _at(dev):
-        _check(load().cp_tree_layout(parents.data_ptr(), rows.ctypes.data, rows.shape[0],
-                                     mask.data_ptr(), mask.shape[1], positions.data_ptr(),
-                                     cp._stream(stream)), "cp_tree_layout")
+    W = mask.shape[1]
+    _check(_call(dev, stream, load().cp_tree_layout, _ptr(parents, _I32, (T,), dev, what),
+                 rows.tobytes(), rows.shape[0], _ptr(mask, _I64, (T, W), dev, what), W,
+                 _ptr(positions, _I32, (T,), dev, what)), what)
 
 
 def attn_workspace_bytes(desc, rows) -> int:
     rows = cp._rows(rows)
-    n = load().cp_tree_attn_workspace_bytes(ctypes.byref(desc), rows.ctypes.data, rows.shape[0])
+    n = load().cp_tree_attn_workspace_bytes(ctypes.byref(desc), rows.tobytes(), rows.shape[0])
     if n == 0:
         rc = cp.check_batch(desc, rows)
         raise cp.CpError(rc if rc != cp.CP_OK else cp.CP_ERR_BAD_META,
@@ -135,28 +148,21 @@ def attn(desc, q, k_cache, v_cache, block_tables, mask, rows, out, ws=None, stre
     """out [T, Hq, D]: every drafted node over its request's committed keys and
     the nodes that its mask (int64 [T, W]) names.  ``ws``: uint8 of at least
     attn_workspace_bytes (allocated here when None)."""
-    import torch
+    what = "cp_tree_attn"
     rows = cp._rows(rows)
-    T, bf16 = _nodes(rows), torch.bfloat16
-    hq, hkv, d, b = desc.num_q_heads, desc.num_kv_heads, desc.head_dim, desc.block_size
+    dev, T = _device(q, what), _nodes(rows)
+    hq, hkv, d, b, nb = (desc.num_q_heads, desc.num_kv_heads, desc.head_dim, desc.block_size,
+                         desc.num_blocks)
     _want(mask.dim() == 2, "cp_tree_attn: mask is [T, W]")
-    dev = _device(q, "cp_tree_attn")
-    _tensors("cp_tree_attn", dev, (q, bf16, (T, hq, d)), (out, bf16, (T, hq, d)),
-             (k_cache, bf16, (desc.num_blocks, hkv, b, d)),
-             (v_cache, bf16, (desc.num_blocks, hkv, d, b)),
-             (block_tables, torch.int32, (desc.num_reqs_in_table, desc.max_blocks_per_req)),
-             (mask, torch.int64, (T, mask.shape[1])))
-    if ws is None:
-        ws = _scratch(attn_workspace_bytes(desc, rows), dev, stream)
-        if ws is None:
-            raise cp.CpError(cp.CP_ERR_WORKSPACE, "cp_tree_attn")
-    _want(ws.device == dev and ws.is_contiguous(), "cp_tree_attn: ws is on another device")
-    with _at(dev):
-        _check(load().cp_tree_attn(ctypes.byref(desc), q.data_ptr(), k_cache.data_ptr(),
-                                   v_cache.data_ptr(), block_tables.data_ptr(), mask.data_ptr(),
-                                   mask.shape[1], rows.ctypes.data, rows.shape[0], out.data_ptr(),
-                                   ws.data_ptr(), ws.numel() * ws.element_size(),
-                                   cp._stream(stream)), "cp_tree_attn")
+    W = mask.shape[1]
+    ws, ws_ptr, ws_bytes = _workspace(ws, lambda: attn_workspace_bytes(desc, rows), dev, stream,
+                                      what)
+    _check(_call(dev, stream, load().cp_tree_attn, ctypes.byref(desc),
+                 _ptr(q, _BF16, (T, hq, d), dev, what), _ptr(k_cache, _BF16, (nb, hkv, b, d), dev, what),
+                 _ptr(v_cache, _BF16, (nb, hkv, d, b), dev, what),
+                 _ptr(block_tables, _I32, (desc.num_reqs_in_table, desc.max_blocks_per_req), dev,
+                      what), _ptr(mask, _I64, (T, W), dev, what), W, rows.tobytes(),
+                 rows.shape[0], _ptr(out, _BF16, (T, hq, d), dev, what), ws_ptr, ws_bytes), what)
 
 
 def verify_workspace_bytes(n_tokens, vocab) -> int:
@@ -172,31 +178,22 @@ def verify(logits, tokens, parents, rows, target, path, n_accepted, next_token, 
     any stride) and tokens, parents [T] (int32) give target [T], each node's
     greedy token; path [R, P], the accepted nodes of each row, -1 behind them;
     n_accepted [R] and next_token [R] (all int32)."""
-    import torch
+    what = "cp_tree_verify"
     rows = cp._rows(rows)
-    T, R, i32 = _nodes(rows), rows.shape[0], torch.int32
-    dev = _device(logits, "cp_tree_verify")
-    _want(logits.dim() == 2 and logits.dtype == torch.bfloat16 and logits.shape[0] == T
+    dev, T, R = _device(logits, what), _nodes(rows), rows.shape[0]
+    _want(logits.dim() == 2 and logits.dtype == _BF16 and logits.shape[0] == T
           and (logits.stride(1) == 1 or logits.shape[1] == 1 or T == 0) and not logits.is_neg(),
           "cp_tree_verify: logits are bf16 [T, V] with dense rows")
     _want(path.dim() == 2, "cp_tree_verify: path is [R, P]")
-    _tensors("cp_tree_verify", dev, (tokens, i32, (T,)), (parents, i32, (T,)),
-             (target, i32, (T,)), (path, i32, (R, path.shape[1])), (n_accepted, i32, (R,)),
-             (next_token, i32, (R,)))
-    vocab = logits.shape[1]
+    vocab, P = logits.shape[1], path.shape[1]
     ld = logits.stride(0) if T > 1 else vocab
-    if ws is None:
-        ws = _scratch(verify_workspace_bytes(T, vocab), dev, stream)
-        if ws is None:
-            raise cp.CpError(cp.CP_ERR_WORKSPACE, "cp_tree_verify")
-    _want(ws.device == dev and ws.is_contiguous(), "cp_tree_verify: ws is on another device")
-    with _at(dev):
-        _check(load().cp_tree_verify(logits.data_ptr(), ld, vocab, tokens.data_ptr(),
-                                     parents.data_ptr(), rows.ctypes.data, R, path.shape[1],
-                                     target.data_ptr(), path.data_ptr(), n_accepted.data_ptr(),
-                                     next_token.data_ptr(), ws.data_ptr(),
-                                     ws.numel() * ws.element_size(), cp._stream(stream)),
-               "cp_tree_verify")
+    ws, ws_ptr, ws_bytes = _workspace(ws, lambda: verify_workspace_bytes(T, vocab), dev, stream,
+                                      what)
+    _check(_call(dev, stream, load().cp_tree_verify, logits.data_ptr(), ld, vocab,
+                 _ptr(tokens, _I32, (T,), dev, what), _ptr(parents, _I32, (T,), dev, what),
+                 rows.tobytes(), R, P, _ptr(target, _I32, (T,), dev, what),
+                 _ptr(path, _I32, (R, P), dev, what), _ptr(n_accepted, _I32, (R,), dev, what),
+                 _ptr(next_token, _I32, (R,), dev, what), ws_ptr, ws_bytes), what)
 
 
 class KvLayers:
@@ -204,46 +201,39 @@ class KvLayers:
     checked once, and kept alive by this handle."""
 
     def __init__(self, desc, k_caches, v_caches):
-        import torch
         _want(len(k_caches) == len(v_caches) > 0, "kv_layers: one K and one V pool per layer")
         hkv, d, b = desc.num_kv_heads, desc.head_dim, desc.block_size
         self.device = _device(k_caches[0], "kv_layers")
-        for k, v in zip(k_caches, v_caches):
-            _tensors("kv_layers", self.device, (k, torch.bfloat16, (desc.num_blocks, hkv, b, d)),
-                     (v, torch.bfloat16, (desc.num_blocks, hkv, d, b)))
-        self.desc, self.n = desc, len(k_caches)
-        self.pools = list(k_caches), list(v_caches)
-        self.k, self.v = ((ctypes.c_void_p * self.n)(*(t.data_ptr() for t in p))
-                          for p in self.pools)
+        self.desc, self.n = cp.Desc.from_buffer_copy(desc), len(k_caches)
+        self.pools = list(k_caches), list(v_caches)   # kept alive
+        self.k, self.v = (
+            (ctypes.c_void_p * self.n)(*(_ptr(t, _BF16, (desc.num_blocks, hkv, *page), self.device,
+                                              "kv_layers") for t in pools))
+            for pools, page in zip(self.pools, ((b, d), (d, b))))
+
+    def table(self, block_tables, what):
+        d = self.desc
+        return _ptr(block_tables, _I32, (d.num_reqs_in_table, d.max_blocks_per_req), self.device,
+                    what)
 
 
 def kv_layers(desc, k_caches, v_caches) -> KvLayers:
     return KvLayers(desc, k_caches, v_caches)
 
 
-def _table(layers, block_tables, what):
-    import torch
-    d = layers.desc
-    _tensors(what, layers.device,
-             (block_tables, torch.int32, (d.num_reqs_in_table, d.max_blocks_per_req)))
-
-
 def kv_compact(layers, block_tables, rows, path, n_accepted, stream=None):
     """Moves the K/V of each row's accepted nodes, path [R, P] and n_accepted [R]
     (int32, as verify writes them), to slots start, start + 1, ..., in every
     layer of ``layers`` (kv_layers)."""
-    import torch
+    what = "cp_kv_compact"
     rows = cp._rows(rows)
-    R = rows.shape[0]
-    _table(layers, block_tables, "cp_kv_compact")
+    dev, R = layers.device, rows.shape[0]
     _want(path.dim() == 2, "cp_kv_compact: path is [R, P]")
-    _tensors("cp_kv_compact", layers.device, (path, torch.int32, (R, path.shape[1])),
-             (n_accepted, torch.int32, (R,)))
-    with _at(layers.device):
-        _check(load().cp_kv_compact(ctypes.byref(layers.desc), layers.k, layers.v, layers.n,
-                                    block_tables.data_ptr(), rows.ctypes.data, R, path.data_ptr(),
-                                    path.shape[1], n_accepted.data_ptr(), cp._stream(stream)),
-               "cp_kv_compact")
+    P = path.shape[1]
+    _check(_call(dev, stream, load().cp_kv_compact, ctypes.byref(layers.desc), layers.k, layers.v,
+                 layers.n, layers.table(block_tables, what), rows.tobytes(), R,
+                 _ptr(path, _I32, (R, P), dev, what), P, _ptr(n_accepted, _I32, (R,), dev, what)),
+           what)
 
 
 def kv_fork(layers, block_tables, forks, stream=None):
@@ -252,8 +242,7 @@ def kv_fork(layers, block_tables, forks, stream=None):
     new request's row of block_tables is filled in, and the page copied in
     every layer of ``layers`` (kv_layers)."""
     forks = np.ascontiguousarray(forks, dtype=np.int32).reshape(-1, 4)
-    _table(layers, block_tables, "cp_kv_fork")
-    with _at(layers.device):
-        _check(load().cp_kv_fork(ctypes.byref(layers.desc), layers.k, layers.v, layers.n,
-                                 block_tables.data_ptr(), forks.ctypes.data, forks.shape[0],
-                                 cp._stream(stream)), "cp_kv_fork")
+    what = "cp_kv_fork"
+    _check(_call(layers.device, stream, load().cp_kv_fork, ctypes.byref(layers.desc), layers.k,
+                 layers.v, layers.n, layers.table(block_tables, what), forks.tobytes(),
+                 forks.shape[0]), what)
