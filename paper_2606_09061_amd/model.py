@@ -9,6 +9,9 @@ scheduler's batch through every layer of such a model with synthetic weights:
     cpl_swiglu -> down GEMM (+ residual)] -> RMSNorm -> LM head on each row's
     last token -> argmax
 
+``Model.verify`` runs the same layers over trees of drafted tokens
+(libcptree.so): every node's logits, the accepted path, its K/V moved up.
+
 Every step runs in this package's HIP kernels (libcplayer.so for the
 projections and the element-wise parts, libcpattn.so for append and
 attention); the largest of the feed-forward's projections, and those of shapes
@@ -440,6 +443,7 @@ class Model:
         self.pos = torch.zeros(T, dtype=torch.int32, device=self.dev)
         self.tokens = torch.randint(0, c.vocab, (T,), generator=gen, device=self.dev)
         self.ws = torch.empty(64 << 20, dtype=torch.uint8, device=self.dev)      # attention plan
+        self.kv = None   # the pools as verify's compaction takes them
         # split-K partials of the projections (grown on demand)
         self.ws_gemm = torch.empty(256, dtype=torch.uint8, device=self.dev)
         # an append item covers one row's tokens inside one block: at most
@@ -466,10 +470,8 @@ class Model:
         with torch.cuda.stream(s):
             self.pos[:T].copy_(self.pos_host[:T], non_blocking=True)
             self.pos_copied.record(s)
-            x, h = self.x[:T], self.h[:T]
+            x = self.x[:T]
             torch.index_select(self.embed, 0, self.tokens[:T], out=x)
-            qkv, q, k, v, attn = self.qkv[:T], self.q[:T], self.k[:T], self.v[:T], self.attn[:T]
-            gu, act = self.gu[:T], self.act[:T]
             # every layer attends with the same rows: plan once, run per layer
             # (the plan is built once per iteration; only a workspace that is
             # too small costs a second planning, to learn the size)
@@ -481,27 +483,9 @@ class Model:
                 self.ws = torch.empty(cp.workspace_bytes(self.desc, rows), dtype=torch.uint8,
                                       device=self.dev)
                 plan = cp.attn_prepare(self.desc, rows, self.ws, stream=s)
-            n_last = int((rows[:, 2] > 0).sum())
-            need = max(gemm_workspace_bytes(T, qkv.shape[1], c.hidden),
-                       gemm_workspace_bytes(T, c.hidden, c.hq * c.head_dim),
-                       gemm_workspace_bytes(T, 2 * c.inter, c.hidden),
-                       gemm_workspace_bytes(T, c.hidden, c.inter),
-                       gemm_workspace_bytes(n_last, c.vocab, c.hidden)
-                       if self.lm_head is not None else 0)
-            if need > self.ws_gemm.numel():
-                self.ws_gemm = torch.empty(need, dtype=torch.uint8, device=self.dev)
-            for L, kc, vc in zip(self.layers, self.kc, self.vc):
-                rmsnorm(x, L["in_norm"], h, c.eps, s)
-                project_attn(h, L["qkv"], qkv, None, s, self.ws_gemm)
-                qkv_rope(qkv, L["q_norm"], L["k_norm"], self.pos, c.hq, c.hkv, c.head_dim,
-                         c.theta, c.eps, q, k, v, s)
-                cp.kv_append(self.desc, k, v, kc, vc, self.bt, rows, self.ws_append, stream=s)
-                cp.attn_run(plan, q, kc, vc, self.bt, attn, self.ws, stream=s)
-                project_attn(attn.view(T, c.hq * c.head_dim), L["o"], x, x, s, self.ws_gemm)
-                rmsnorm(x, L["post_norm"], h, c.eps, s)
-                project(h, L["gate_up"], gu, None, s, self.ws_gemm)
-                swiglu(gu, act, s)
-                project(act, L["down"], x, x, s, self.ws_gemm)
+            self._layers(rows, T, int((rows[:, 2] > 0).sum()), s,
+                         lambda q, kc, vc, out: cp.attn_run(plan, q, kc, vc, self.bt, out, self.ws,
+                                                            stream=s))
             if self.lm_head is None:
                 return None
             last = torch.from_numpy(np.cumsum(rows[:, 2]).astype(np.int64) - 1)
@@ -511,6 +495,86 @@ class Model:
             logits = torch.empty(len(last), c.vocab, dtype=torch.bfloat16, device=self.dev)
             project(hl, self.lm_head, logits, None, s, self.ws_gemm)
             return torch.argmax(logits, dim=-1)
+
+    def _layers(self, rows, T, n_head, s, attend):
+        """The decoder layers over the embeddings in x[:T], whose positions are in
+        pos[:T], on stream ``s``: K/V appended, ``attend(q, kc, vc, out)`` for the
+        attention.  The projections' workspace is grown for ``n_head`` rows of
+        the LM head too."""
+        import torch
+        c = self.cfg
+        x, h, qkv, q, k, v = (b[:T] for b in (self.x, self.h, self.qkv, self.q, self.k, self.v))
+        attn, gu, act = self.attn[:T], self.gu[:T], self.act[:T]
+        need = max(gemm_workspace_bytes(T, qkv.shape[1], c.hidden),
+                   gemm_workspace_bytes(T, c.hidden, c.hq * c.head_dim),
+                   gemm_workspace_bytes(T, 2 * c.inter, c.hidden),
+                   gemm_workspace_bytes(T, c.hidden, c.inter),
+                   gemm_workspace_bytes(n_head, c.vocab, c.hidden)
+                   if self.lm_head is not None else 0)
+        if need > self.ws_gemm.numel():
+            self.ws_gemm = torch.empty(need, dtype=torch.uint8, device=self.dev)
+        for L, kc, vc in zip(self.layers, self.kc, self.vc):
+            rmsnorm(x, L["in_norm"], h, c.eps, s)
+            project_attn(h, L["qkv"], qkv, None, s, self.ws_gemm)
+            qkv_rope(qkv, L["q_norm"], L["k_norm"], self.pos, c.hq, c.hkv, c.head_dim,
+                     c.theta, c.eps, q, k, v, s)
+            cp.kv_append(self.desc, k, v, kc, vc, self.bt, rows, self.ws_append, stream=s)
+            attend(q, kc, vc, attn)
+            project_attn(attn.view(T, c.hq * c.head_dim), L["o"], x, x, s, self.ws_gemm)
+            rmsnorm(x, L["post_norm"], h, c.eps, s)
+            project(h, L["gate_up"], gu, None, s, self.ws_gemm)
+            swiglu(gu, act, s)
+            project(act, L["down"], x, x, s, self.ws_gemm)
+
+    def verify(self, rows, tokens, parents, max_path=16, stream=None):
+        """One iteration over drafted trees: every row (slot, start, nodes, ctx)
+        brings a tree of ``nodes`` guessed tokens, at most 256, node 0 the
+        last token known (a decode row is a tree of one).  tokens (in [0, vocab))
+        and parents: int32 device tensors [T], packed in row order, parents as
+        indexes inside their row and -1 for node 0.
+
+        The greedy token of every node is found, the path of drafted tokens that
+        agrees with them accepted, and its K/V moved to the slots from ``start``
+        on, in every layer: the row's next start is start + n_accepted, with
+        next_token as its root.  Returns device int32 tensors (target [T], path
+        [rows, max_path], n_accepted [rows], next_token [rows])."""
+        import torch
+        from . import tree
+        c = self.cfg
+        if self.lm_head is None:
+            raise ValueError("verify needs a model with an LM head")
+        rows = np.ascontiguousarray(np.asarray(rows, dtype=np.int32).reshape(-1, 4))
+        T, R = int(rows[:, 2].sum()), len(rows)
+        if T > self.max_tokens:
+            raise ValueError(f"batch of {T} tokens exceeds the model's {self.max_tokens}")
+        if (rows[:, 2] > tree.MAX_NODES).any() or not 1 <= max_path <= tree.MAX_NODES:
+            raise ValueError(f"a tree has at most {tree.MAX_NODES} nodes, and so its path")
+        s = stream or torch.cuda.current_stream(self.dev)
+        with torch.cuda.stream(s):
+            i32 = dict(dtype=torch.int32, device=self.dev)
+            target, n_accepted, after = (torch.empty(n, **i32) for n in (T, R, R))
+            path = torch.empty(R, max_path, **i32)
+            logits = torch.empty(T, c.vocab, dtype=torch.bfloat16, device=self.dev)
+            if T > 0:
+                words = -(-int(rows[:, 2].max()) // 64)
+                mask = torch.empty(T, words, dtype=torch.int64, device=self.dev)
+                tree.layout(parents, rows, mask, self.pos[:T], s)
+                need = tree.attn_workspace_bytes(self.desc, rows)
+                if need > self.ws.numel():
+                    self.ws = torch.empty(need, dtype=torch.uint8, device=self.dev)
+                x, h = self.x[:T], self.h[:T]
+                torch.index_select(self.embed, 0, tokens, out=x)
+                self._layers(rows, T, T, s,
+                             lambda q, kc, vc, out: tree.attn(self.desc, q, kc, vc, self.bt, mask,
+                                                              rows, out, self.ws, s))
+                rmsnorm(x, self.final_norm, h, c.eps, s)
+                project(h, self.lm_head, logits, None, s, self.ws_gemm)
+            tree.verify(logits, tokens, parents, rows, target, path, n_accepted, after, stream=s)
+            if T > 0:
+                if self.kv is None:
+                    self.kv = tree.kv_layers(self.desc, self.kc, self.vc)
+                tree.kv_compact(self.kv, self.bt, rows, path, n_accepted, s)
+        return target, path, n_accepted, after
 
 
 class ModelEngine:

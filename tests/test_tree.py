@@ -282,3 +282,19 @@ def test_calls_want_tensors_on_a_gpu():
     with pytest.raises(cp.CpError):
         tree.kv_layers(_desc(), [torch.zeros(100, 8, 16, 128, dtype=torch.bfloat16)],
                        [torch.zeros(100, 8, 128, 16, dtype=torch.bfloat16)])
+
+
+def test_plan_under_sanitizers(tmp_path):
+    """Host C++: random batches through the plan (tests/native/tree_fuzz.cpp)."""
+    import shutil
+    import subprocess
+    if shutil.which("g++") is None:
+        pytest.skip("needs g++")
+    csrc = os.path.join(ROOT, "paper_2606_09061_amd", "csrc")
+    exe = str(tmp_path / "tree_fuzz")
+    subprocess.run(["g++", "-std=c++17", "-O1", "-g", "-fsanitize=address,undefined",
+                    "-fno-sanitize-recover=all", "-I", os.path.join(ROOT, "include"), "-I", csrc,
+                    os.path.join(ROOT, "tests", "native", "tree_fuzz.cpp"),
+                    os.path.join(csrc, "tree_plan.cpp"), "-o", exe], check=True, timeout=300)
+    r = subprocess.run([exe], capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and r.stdout.startswith("ok"), r.stderr[-2000:]
