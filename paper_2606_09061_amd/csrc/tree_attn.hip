@@ -55,8 +55,10 @@ __device__ __forceinline__ f32x4_t mfma16x16x32(uint4 a, uint4 b, f32x4_t c) {
 // zeros: a node that does not see the key would get 0 * NaN from it.  The
 // nodes that do get them added at the end.
 template <int D, int B, int NC, class Rows>
-__global__ __launch_bounds__(kThreads, 2) void narrow_kernel(const Rows rows,
-                                                             const AttnArgs a) {
+__global__ __launch_bounds__(kThreads, 2) void narrow_kernel(
+    const Rows rows, const AttnArgs a, const uint16_t* __restrict__ q,
+    const uint16_t* __restrict__ k_cache, const uint16_t* __restrict__ v_cache,
+    const int32_t* __restrict__ bt, const uint64_t* __restrict__ masks) {
   constexpr int TK = 32;       // keys per tile
   constexpr int ROWS = 16 * NC;
   constexpr int NKS = D / 32;    // k-steps of a score
@@ -85,10 +87,10 @@ __global__ __launch_bounds__(kThreads, 2) void narrow_kernel(const Rows rows,
   for (int c = 0; c < NC; ++c) {
     const int x = min(16 * c + i, m_rows - 1);
     const int64_t t = row.tok0 + (x >> a.log2_group);
-    const uint16_t* qb = a.q + (t * a.hq + kvh * G + (x & (G - 1))) * D + g * 8;
+    const uint16_t* qb = q + (t * a.hq + kvh * G + (x & (G - 1))) * D + g * 8;
 #pragma unroll
     for (int ks = 0; ks < NKS; ++ks) qv[c][ks] = ld_global16(qb + ks * 32);
-    mask[c] = a.mask[t * a.words];
+    mask[c] = masks[t * a.words];
   }
   __builtin_amdgcn_sched_barrier(0);
 
@@ -102,7 +104,7 @@ __global__ __launch_bounds__(kThreads, 2) void narrow_kernel(const Rows rows,
   }
 
   const int64_t head_elems = (int64_t)B * D;
-  const int32_t* bt_row = a.bt + (int64_t)row.req * a.mbr;
+  const int32_t* bt_row = bt + (int64_t)row.req * a.mbr;
   const int n_tiles = (kv_end - kv_begin + TK - 1) / TK;
   const int lb_last = (kv_end - 1) / B;
   const int voff = i * B + (8 * g) % B;
@@ -129,12 +131,12 @@ __global__ __launch_bounds__(kThreads, 2) void narrow_kernel(const Rows rows,
 #pragma unroll
       for (int j = 0; j < NKL; ++j) {
         const int key0 = 2 * KPL * j + 4 * b;  // the load's first key
-        kr[b][j] = ld_global16_nt(a.k_cache + (key0 < B ? b0 : b1) + (key0 % B) * D + koff);
+        kr[b][j] = ld_global16_nt(k_cache + (key0 < B ? b0 : b1) + (key0 % B) * D + koff);
       }
   };
   auto load_v = [&](int t) {
     const int64_t b0 = block_at(t, 0), b1 = B < TK ? block_at(t, 1) : b0;
-    const uint16_t* vp = a.v_cache + (v_second ? b1 : b0) + voff;
+    const uint16_t* vp = v_cache + (v_second ? b1 : b0) + voff;
 #pragma unroll
     for (int dt = 0; dt < NDT; ++dt) vr[dt] = ld_global16_nt(vp + dt * 16 * B);
   };
@@ -309,6 +311,7 @@ __global__ __launch_bounds__(kThreads, 2) void narrow_kernel(const Rows rows,
         v += s_f[w][mr] * *reinterpret_cast<const f32x4_t*>(&red[w][r][(p ^ r) * 4]);
       const int64_t t = row.tok0 + (mr >> a.log2_group);
       if (any)
+#pragma unroll 1
         for (int e = 0; e < 4; ++e)
           v[e] += bad_values<D, B>(s_bad, a.mask + t * a.words, a.words, row, a, kvh, 4 * p + e);
       if (row.n_split == 1) {
@@ -410,9 +413,11 @@ hipError_t launch_narrow_t(int most, const AttnArgs& a, const TreeRows& rows, in
   static_assert(kNarrowRows == 32, "columns");
   return by_size(rows, n_rows, [&](const auto& r) {
     if (most <= 16)
-      hipLaunchKernelGGL((narrow_kernel<D, B, 1>), dim3(items), dim3(kThreads), 0, s, r, a);
+      hipLaunchKernelGGL((narrow_kernel<D, B, 1>), dim3(items), dim3(kThreads), 0, s, r, a, a.q,
+                         a.k_cache, a.v_cache, a.bt, a.mask);
     else
-      hipLaunchKernelGGL((narrow_kernel<D, B, 2>), dim3(items), dim3(kThreads), 0, s, r, a);
+      hipLaunchKernelGGL((narrow_kernel<D, B, 2>), dim3(items), dim3(kThreads), 0, s, r, a, a.q,
+                         a.k_cache, a.v_cache, a.bt, a.mask);
   });
 }
 
