@@ -21,6 +21,7 @@ namespace {
 constexpr int kMaxKvHeads = 1024;
 constexpr int64_t kMaxTokens = 1 << 23;
 constexpr int32_t kMaxVocab = 1 << 30;
+constexpr int kMaxItems = 1 << 22;
 
 bool aligned(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
 
@@ -131,23 +132,20 @@ int by_node_rows(const cp_row_meta* rows, int32_t n_rows, F&& f) {
   return CP_OK;
 }
 
-// f(rows of one launch, their number, its workgroups) for rows in batches; items_of(row) is
-// the number of a row's workgroups.
+// f(rows of one launch, their number, its workgroups) for rows in batches, the
+// places behind them no workgroup's; items_of(row) is the number of a row's
+// workgroups, of which a launch takes some 2^22 (2^32 threads are its limit).
 template <class Items, class F>
 int by_tree_rows(const std::vector<TreeRow>& rows, Items&& items_of, F&& f) {
-  for (size_t r0 = 0; r0 < rows.size(); r0 += kTreeRows) {
+  for (size_t r = 0; r < rows.size();) {
     TreeRows batch;
-    int items = 0;
-    for (int i = 0; i < kTreeRows; ++i) {
-      if (r0 + i >= rows.size()) {  // no workgroup's
-        batch.r[i] = TreeRow{0, 0, 0, 0, INT_MAX, 1, 0, 0};
-        continue;
-      }
-      batch.r[i] = rows[r0 + i];
-      batch.r[i].item0 = items;
-      items += items_of(rows[r0 + i]);
+    int items = 0, n = 0;
+    for (; r < rows.size() && n < kTreeRows && items < kMaxItems; ++r) {
+      batch.r[n] = rows[r];
+      batch.r[n++].item0 = items;
+      items += items_of(rows[r]);
     }
-    const int n = (int)std::min<size_t>(kTreeRows, rows.size() - r0);
+    for (int i = n; i < kTreeRows; ++i) batch.r[i] = TreeRow{0, 0, 0, 0, INT_MAX, 1, 0, 0};
     const int rc = f(batch, n, items);
     if (rc != CP_OK) return rc;
   }
@@ -268,10 +266,10 @@ int cp_tree_attn(const cp_attn_desc* desc, const void* q, const void* k_cache,
     const int d = desc->head_dim;
     rc = by_tree_rows(
         p.rows,
-        [&](const TreeRow& t) { return t.n_split * desc->num_kv_heads * p.tiles(t, group); },
+        [&](const TreeRow& t) { return t.n_split * desc->num_kv_heads * tree_tiles(t.n * group, p.wide); },
         [&](const TreeRows& batch, int n, int items) {
           const hipError_t e =
-              !p.wide()  ? launch_narrow(d, desc->block_size, p.most, a, batch, n, items, s)
+              !p.wide    ? launch_narrow(d, desc->block_size, p.most, a, batch, n, items, s)
               : d == 128 ? launch_wide128(desc->block_size, a, batch, items, s)
                          : launch_wide64(desc->block_size, a, batch, items, s);
           return finish(e, s);

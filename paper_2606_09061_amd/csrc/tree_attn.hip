@@ -1,4 +1,5 @@
-// Attention of drafted trees over the paged cache (include/cp_tree.h).
+// Attention of drafted trees over the paged cache (include/cp_tree.h): the
+// narrow kernel and the merge (tree_wide.hpp has the wide one).
 //
 // With n nodes and G q heads per kv head, n G rows share every K and V that
 // is read.  Over c committed keys the work is 4 D n G c flop on 4 D c bytes per
@@ -36,9 +37,10 @@ __device__ __forceinline__ f32x4_t mfma16x16x32(uint4 a, uint4 b, f32x4_t c) {
                                                  __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
 }
 
-// A workgroup takes all of a kv head's rows, up to 16 NC of them, and a piece
-// of the key range, of which wave w takes tiles of 32 keys w, w + 4, ...  The
-// rows are the columns of both products (v_mfma_f32_16x16x32_bf16, NC of them
+// A workgroup takes 16 NC of a kv head's rows and a piece of the key range, of
+// which wave w takes tiles of 32 keys w, w + 4, ...  (With one such tile of rows
+// the stream of K and V bounds it: 32 requests of 8 nodes on 32/8 heads, 206 MB,
+// 39 us or 5.3 TB/s.)  The rows are the columns of both products (v_mfma_f32_16x16x32_bf16, NC of them
 // per operand of K or V).  Per tile and wave, lane l = 16 g + i:
 //   S^T (2 x 16 keys x 16 NC rows) = K . Q^T.  Row i of key half b is key
 //     8 (i / 4) + 4 b + i % 4, so that lane (g, i) ends up with rows i's scores
@@ -70,22 +72,23 @@ __global__ __launch_bounds__(kThreads, 2) void narrow_kernel(
 
   const TreeRow row = row_of(rows, blockIdx.x);
   const int unit = (int)blockIdx.x - row.item0;
-  const int kvh = unit % a.hkv, split = unit / a.hkv;
+  const int G = 1 << a.log2_group, m_rows = row.n << a.log2_group;
+  const int tiles = (m_rows + ROWS - 1) / ROWS, m0 = unit % tiles * ROWS;
+  const int kvh = unit / tiles % a.hkv, split = unit / tiles / a.hkv;
   const int tid = threadIdx.x, lane = tid & 63, i = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int G = 1 << a.log2_group, m_rows = row.n << a.log2_group;
   const int ctx = row.start + row.n;
   const int kv_begin = split * row.split_keys, kv_end = min(ctx, kv_begin + row.split_keys);
   if (tid < kMaxWords) s_bad[tid] = 0;
 
   // Column c's row of this lane, past the last one that again (not stored), and
-  // its node's mask: a narrow tree's nodes fit one word.
+  // its node's mask, one word.
   uint4 qv[NC][NKS];
   uint64_t mask[NC];
-  static_assert(kNarrowRows <= 64, "one word");
+  static_assert(kNarrowNodes <= 64, "one word");
 #pragma unroll
   for (int c = 0; c < NC; ++c) {
-    const int x = min(16 * c + i, m_rows - 1);
+    const int x = min(m0 + 16 * c + i, m_rows - 1);
     const int64_t t = row.tok0 + (x >> a.log2_group);
     const uint16_t* qb = q + (t * a.hq + kvh * G + (x & (G - 1))) * D + g * 8;
 #pragma unroll
@@ -117,7 +120,8 @@ __global__ __launch_bounds__(kThreads, 2) void narrow_kernel(
   auto slot = [](int r, int chunk) {
     return r * (D * 2) + ((chunk ^ (CH == 16 ? r & 15 : (r >> 1) & 7)) * 16);
   };
-  // Each byte of K and V is read by one wave only: streamed past the caches.
+  // Each byte of K and V is read by one wave of the workgroup: streamed past the
+  // caches.
   // Past the range its last block comes again: those keys are not seen.
   auto block_at = [&](int t, int second) {
     const int lb = min(kv_begin / B + t * (TK / B) + second, lb_last);
@@ -286,15 +290,15 @@ __global__ __launch_bounds__(kThreads, 2) void narrow_kernel(
     const float inv = L == 0.f ? 0.f : 1.f / L;  // L == 0: it saw no key
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) s_f[w][tid] = f[w] * inv;
-    if (row.n_split > 1 && tid < m_rows)
-      a.part_lse[part0 + tid] = L == 0.f ? -INFINITY : M + __log2f(L);
+    if (row.n_split > 1 && m0 + tid < m_rows)
+      a.part_lse[part0 + m0 + tid] = L == 0.f ? -INFINITY : M + __log2f(L);
   }
   const uint64_t any = s_bad[0];
   auto red = reinterpret_cast<float(*)[16][D]>(&slices[0][0]);
   static_assert(sizeof(float) * 16 * D == SLICE, "a wave's output fills its slice");
 #pragma unroll
   for (int c = 0; c < NC; ++c) {
-    if (16 * c >= m_rows) break;  // uniform
+    if (m0 + 16 * c >= m_rows) break;  // uniform
     __syncthreads();
     // lane (g, i) holds features 16 dt + 4 g .. + 3 of row i; 16-byte piece p
     // of row r lies at p ^ r, so that neither side meets a bank twice
@@ -303,12 +307,12 @@ __global__ __launch_bounds__(kThreads, 2) void narrow_kernel(
       *reinterpret_cast<f32x4_t*>(&red[wave][i][((4 * dt + g) ^ i) * 4]) = o[c][dt];
     __syncthreads();
     for (int x = tid; x < 16 * (D / 4); x += kThreads) {
-      const int p = x % (D / 4), r = x / (D / 4), mr = 16 * c + r;
+      const int p = x % (D / 4), r = x / (D / 4), mr = m0 + 16 * c + r;
       if (mr >= m_rows) break;  // a thread's rows come in increasing order
       f32x4_t v = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int w = 0; w < kWaves; ++w)
-        v += s_f[w][mr] * *reinterpret_cast<const f32x4_t*>(&red[w][r][(p ^ r) * 4]);
+        v += s_f[w][16 * c + r] * *reinterpret_cast<const f32x4_t*>(&red[w][r][(p ^ r) * 4]);
       const int64_t t = row.tok0 + (mr >> a.log2_group);
       if (any)
 #pragma unroll 1

@@ -8,16 +8,18 @@ namespace cptree {
 
 namespace {
 
-constexpr int kSlots = 2 * 256;  // workgroups at a time: two on each of MI355X's CUs
+constexpr int kCus = 256;         // MI355X
+constexpr int kSlots = 2 * kCus;  // workgroups at a time: two on each CU
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 // Estimated times of a kernel, in us: a turn of `turn` keys while every slot
-// is busy, and alone (bound by the memory's latency); a workgroup's start and
-// end; the merge launch and its 1,000 partial rows.
+// is busy, and with a CU to itself (bound by the memory's latency); a
+// workgroup's start and end; the merge launch and its 1,000 partial rows; and
+// the batch's K and V at the rate they come from memory.
 struct Cost {
   int turn;
-  double loaded, alone, setup, merge, partial;
+  double loaded, alone, setup, merge, partial, memory;
 };
 
 struct Load {
@@ -40,41 +42,46 @@ Load load_of(const std::vector<TreeRow>& rows, const std::vector<int>& per_split
 }
 
 // The estimated time: the slots' share of the work, but at least the longest
-// piece alone; with more workgroups than slots (the longest come first) the
-// slots end apart by a part of a piece.
+// piece, which is slower where workgroups share a CU; with more workgroups than
+// slots (the longest come first) the slots end apart by a part of a piece.
 double time_of(const Load& l, const Cost& c) {
   const double merge = l.partial ? c.merge + c.partial * l.partial * 1e-3 : 0.0;
+  const double share = l.work * c.loaded / kSlots;
+  if (l.n <= kCus)  // (a workgroup per CU does not quite reach the memory's rate)
+    return std::max(l.longest * c.alone, 1.06 * c.memory) + c.setup + merge;
   if (l.n <= kSlots)
-    return std::max(l.longest * c.alone, l.work * c.loaded / kSlots) + c.setup + merge;
-  const double one = l.longest * c.loaded + c.setup;
-  return (l.work * c.loaded + l.n * c.setup) / kSlots + 0.2 * one + merge;
+    return std::max({l.longest * 0.75 * c.loaded, share, c.memory}) + c.setup + merge;
+  return std::max(share, c.memory) + l.n * c.setup / kSlots + 0.2 * (l.longest * c.loaded + c.setup) + merge;
 }
 
 // The pieces' length in turns: of the whole ranges, their parts, and the
-// shortest pieces that fill the slots once, twice and so on, the one with the
-// shortest estimated time.
+// shortest pieces that fill the CUs, the slots once, twice and so on, the one
+// with the shortest estimated time, which is added to `time`.
 int best_piece(const std::vector<TreeRow>& rows, const std::vector<int>& per_split, int hq,
-               const Cost& c, int least) {
+               const Cost& c, double* time) {
+  const int least = 256 / c.turn;
   const auto load = [&](int piece) { return load_of(rows, per_split, hq, c.turn, piece); };
   const Load whole = load(1 << 30);  // longer than any range
   int best = whole.longest;
-  double time = time_of(whole, c);
+  *time = time_of(whole, c);
   const auto look = [&](int piece) {
     if (piece >= whole.longest) return;
     const double t = time_of(load(piece), c);
-    if (t < time) time = t, best = piece;
+    if (t < *time) *time = t, best = piece;
   };
   const int64_t rounds = ceil_div(whole.n, kSlots);
   int hi = whole.longest;  // fits the rounds before
-  for (int64_t r = rounds; r < rounds + 4 && hi > least; ++r) {
+  const auto fill = [&](int64_t workgroups) {
     int lo = least;
     while (lo < hi) {
       const int mid = (lo + hi) / 2;
-      if (load(mid).n <= r * kSlots) hi = mid;
+      if (load(mid).n <= workgroups) hi = mid;
       else lo = mid + 1;
     }
     look(hi);
-  }
+  };
+  if (whole.n < kCus) fill(kCus);
+  for (int64_t r = rounds; r < rounds + 4 && hi > least; ++r) fill(r * kSlots);
   // few workgroups whatever the pieces: the shortest are not always best
   if (rounds == 1)
     for (int n = 2; n <= 8; n *= 2)
@@ -90,34 +97,52 @@ void plan_tree(const cp_attn_desc& desc, const cp_row_meta* rows, int32_t n_rows
   out.most = 0;
   out.partial_rows = 0;
   const int hq = desc.num_q_heads, hkv = desc.num_kv_heads, group = hq / hkv;
-  int32_t tok = 0;
+  int32_t tok = 0, nodes = 0;
+  double keys = 0, read = 0;  // all keys, and as every narrow tile reads them
   for (int32_t r = 0; r < n_rows; ++r) {
     const cp_row_meta& m = rows[r];
     if (m.chunk_len <= 0) continue;
     out.rows.push_back(TreeRow{tok, m.chunk_len, m.chunk_start, m.req_id, 0, 1, 0, 0});
     out.most = std::max(out.most, m.chunk_len * group);
+    nodes = std::max(nodes, m.chunk_len);
+    keys += m.ctx_len;
+    read += (double)m.ctx_len * tree_tiles(m.chunk_len * group, false);
     tok += m.chunk_len;
   }
   out.off_lse = 0;
   out.ws_bytes = 256;
   if (out.rows.empty()) return;
 
+  // Both kernels' best pieces, where there is a choice: a narrow workgroup
+  // starts and ends sooner, a wide one takes four times the rows and reads K and
+  // V for all of them.  us, narrow / wide, on 32/8 heads: one request of 128 rows
+  // after 250 keys 9.6 / 14.7, after 1,000 12.9 / 15.8; 8 of them 10.3 / 16.7
+  // and 29.0 / 22.8; 32 of them 32.5 / 18.3.  Of 234 such batches this takes the
+  // slower kernel, by 7 to 20 %, in 6.
   thread_local std::vector<int> per_split;
-  per_split.clear();
-  for (const TreeRow& t : out.rows) per_split.push_back(hkv * out.tiles(t, group));
   const double d = desc.head_dim / 128.0;
-  const Cost c = out.wide() ? Cost{64, 2.8 * d, 2.4 * d, 7.0, 3.0, 0.2 * d}
-                            : Cost{128, 5.5 * d, 4.0 * d, 4.0, 4.0, 0.2 * d};
-  const int piece = best_piece(out.rows, per_split, hq, c, 256 / c.turn);
+  const double per_key = hkv * desc.head_dim * 4.0 / 5.3e6;
+  const Cost costs[2] = {{128, 5.5 * d, 0.3 + 1.2 * d, 3.2, 5.5, 0.3 * d, read * per_key},
+                         {64, 0.4 + 2.2 * d, 1.0 + 0.2 * d, 7.0, 3.0, 0.2 * d, keys * per_key}};
+  int turn = 0, piece = 0;
+  double best = 0;
+  for (int wide = 0; wide < 2; ++wide) {
+    if (wide ? out.most <= kNarrowRows : nodes > kNarrowNodes) continue;
+    per_split.clear();
+    for (const TreeRow& t : out.rows) per_split.push_back(hkv * tree_tiles(t.n * group, wide));
+    double time = 0;
+    const int p = best_piece(out.rows, per_split, hq, costs[wide], &time);
+    if (piece == 0 || time < best) best = time, piece = p, turn = costs[wide].turn, out.wide = wide;
+  }
   for (TreeRow& t : out.rows) {
-    const int turns = (t.start + t.n + c.turn - 1) / c.turn;
+    const int turns = (t.start + t.n + turn - 1) / turn;
     const int n = (turns + piece - 1) / piece, per = (turns + n - 1) / n;
-    t.split_keys = per * c.turn;
+    t.split_keys = per * turn;
     t.n_split = (turns + per - 1) / per;
     if (t.n_split == 1) continue;
     const int64_t partial = (int64_t)t.n_split * t.n * hq;
     if (out.partial_rows + partial > INT_MAX) {  // beyond their index type
-      t.split_keys = turns * c.turn;
+      t.split_keys = turns * turn;
       t.n_split = 1;
       continue;
     }

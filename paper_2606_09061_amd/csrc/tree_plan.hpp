@@ -7,12 +7,16 @@
 
 namespace cptree {
 
-// Rows of the products: a (node, q head) pair of one kv head's group.  A batch
-// whose largest tree has up to kNarrowRows of them runs on the narrow kernel,
-// whose waves share the keys, any other on the wide one, whose waves share the
-// rows, kWideRows a workgroup.
-constexpr int kNarrowRows = 32;
+// Rows of the products: a (node, q head) pair of one kv head's group.  The
+// narrow kernel takes kNarrowRows of them a workgroup, whose waves share the
+// keys, and trees of one word of mask; the wide one kWideRows, whose waves share
+// the rows.
+constexpr int kNarrowRows = 32, kNarrowNodes = 64;
 constexpr int kWideRows = 128;
+// Workgroups per piece of keys and kv head of a tree of m rows.
+constexpr int tree_tiles(int m, bool wide) {
+  return wide ? (m + kWideRows - 1) / kWideRows : (m + kNarrowRows - 1) / kNarrowRows;
+}
 
 // Output rows (node, q head) per workgroup of the merge: its 256 threads hold
 // 1024 / d of them at a time, and several share a row with many splits.
@@ -23,17 +27,13 @@ constexpr int merge_rows(int d, int n_split) {
 }
 
 struct TreePlan {
+  bool wide = false;           // the kernel
   int most = 0;                // rows of the products of the largest tree
   std::vector<TreeRow> rows;   // longest pieces first
   std::vector<TreeRow> merge;  // those that are split
   int64_t partial_rows = 0;
   size_t off_lse = 0, ws_bytes = 256;  // partial rows of D fp32, then their log sums
 
-  bool wide() const { return most > kNarrowRows; }
-  // workgroups per piece of keys and kv head
-  int tiles(const TreeRow& t, int group) const {
-    return wide() ? (t.n * group + kWideRows - 1) / kWideRows : 1;
-  }
 };
 
 // rows: valid for desc, at most kMaxNodes nodes each.

@@ -25,7 +25,7 @@ int main() {
     }
     const cp_attn_desc desc{group * hkv, hkv, d, 16, 1, 1 << 20, 512, 1.f};
     plan_tree(desc, rows.data(), n_rows, p);
-    const int turn = p.wide() ? 64 : 128;
+    const int turn = p.wide ? 64 : 128;
     int64_t seen = 0, partial = 0;
     size_t merged = 0;
     int most = 0, before = 1 << 30;
@@ -34,10 +34,11 @@ int main() {
       const int keys = t.start + t.n;
       most = std::max(most, t.n * group);
       seen += t.n;
+      assert(p.wide ? t.n <= kMaxNodes : t.n <= kNarrowNodes);
       assert(t.n >= 1 && t.n_split >= 1 && t.split_keys % turn == 0);
       assert((int64_t)t.split_keys * t.n_split >= keys);
       assert((int64_t)t.split_keys * (t.n_split - 1) < keys);  // no empty piece
-      assert(p.tiles(t, group) * (p.wide() ? kWideRows : kNarrowRows) >= t.n * group);
+      assert(tree_tiles(t.n * group, p.wide) * (p.wide ? kWideRows : kNarrowRows) >= t.n * group);
       const int piece = std::min(t.split_keys, keys);
       assert(piece <= before);  // longest first
       before = piece;
