@@ -22,22 +22,36 @@ struct Cost {
   double loaded, alone, setup, merge, partial, memory;
 };
 
+// What the pieces of a kernel are cut from: a row's turns, its workgroups per
+// piece and its partial rows per split.
+struct Work {
+  std::vector<uint32_t> turns, per_split, partial;
+
+  // workgroups, for pieces of `piece` turns
+  int64_t workgroups(uint32_t piece) const {
+    int64_t n = 0;
+    for (size_t i = 0; i < turns.size(); ++i)
+      n += (int64_t)((turns[i] + piece - 1) / piece) * per_split[i];
+    return n;
+  }
+};
+
 struct Load {
   int64_t n, work, partial;  // workgroups, their turns, partial rows
   int longest;               // turns of the longest piece
 };
 
-Load load_of(const std::vector<TreeRow>& rows, const std::vector<int>& per_split, int hq, int turn,
-             int piece) {
+Load load_of(const Work& w, uint32_t piece) {
   Load l{0, 0, 0, 0};
-  for (size_t i = 0; i < rows.size(); ++i) {
-    const int turns = (rows[i].start + rows[i].n + turn - 1) / turn;
-    const int s = (turns + piece - 1) / piece;
-    l.n += (int64_t)s * per_split[i];
-    l.work += (int64_t)turns * per_split[i];
-    l.longest = std::max(l.longest, std::min(turns, piece));
-    if (s > 1) l.partial += (int64_t)s * rows[i].n * hq;
+  uint32_t longest = 0;
+  for (size_t i = 0; i < w.turns.size(); ++i) {
+    const uint32_t turns = w.turns[i], s = (turns + piece - 1) / piece;
+    l.n += (int64_t)s * w.per_split[i];
+    l.work += (int64_t)turns * w.per_split[i];
+    longest = std::max(longest, std::min(turns, piece));
+    if (s > 1) l.partial += (int64_t)s * w.partial[i];
   }
+  l.longest = (int)longest;
   return l;
 }
 
@@ -57,16 +71,14 @@ double time_of(const Load& l, const Cost& c) {
 // The pieces' length in turns: of the whole ranges, their parts, and the
 // shortest pieces that fill the CUs, the slots once, twice and so on, the one
 // with the shortest estimated time, which is added to `time`.
-int best_piece(const std::vector<TreeRow>& rows, const std::vector<int>& per_split, int hq,
-               const Cost& c, double* time) {
+int best_piece(const Work& w, const Cost& c, double* time) {
   const int least = 256 / c.turn;
-  const auto load = [&](int piece) { return load_of(rows, per_split, hq, c.turn, piece); };
-  const Load whole = load(1 << 30);  // longer than any range
+  const Load whole = load_of(w, 1u << 30);  // longer than any range
   int best = whole.longest;
   *time = time_of(whole, c);
   const auto look = [&](int piece) {
     if (piece >= whole.longest) return;
-    const double t = time_of(load(piece), c);
+    const double t = time_of(load_of(w, piece), c);
     if (t < *time) *time = t, best = piece;
   };
   const int64_t rounds = ceil_div(whole.n, kSlots);
@@ -75,7 +87,7 @@ int best_piece(const std::vector<TreeRow>& rows, const std::vector<int>& per_spl
     int lo = least;
     while (lo < hi) {
       const int mid = (lo + hi) / 2;
-      if (load(mid).n <= workgroups) hi = mid;
+      if (w.workgroups(mid) <= workgroups) hi = mid;
       else lo = mid + 1;
     }
     look(hi);
@@ -119,7 +131,7 @@ void plan_tree(const cp_attn_desc& desc, const cp_row_meta* rows, int32_t n_rows
   // after 250 keys 9.6 / 14.7, after 1,000 12.9 / 15.8; 8 of them 10.3 / 16.7
   // and 29.0 / 22.8; 32 of them 32.5 / 18.3.  Of 234 such batches this takes the
   // slower kernel, by 7 to 20 %, in 6.
-  thread_local std::vector<int> per_split;
+  thread_local Work work;
   const double d = desc.head_dim / 128.0;
   const double per_key = hkv * desc.head_dim * 4.0 / 5.3e6;
   const Cost costs[2] = {{128, 5.5 * d, 0.3 + 1.2 * d, 3.2, 5.5, 0.3 * d, read * per_key},
@@ -128,10 +140,14 @@ void plan_tree(const cp_attn_desc& desc, const cp_row_meta* rows, int32_t n_rows
   double best = 0;
   for (int wide = 0; wide < 2; ++wide) {
     if (wide ? out.most <= kNarrowRows : nodes > kNarrowNodes) continue;
-    per_split.clear();
-    for (const TreeRow& t : out.rows) per_split.push_back(hkv * tree_tiles(t.n * group, wide));
+    work.turns.clear(), work.per_split.clear(), work.partial.clear();
+    for (const TreeRow& t : out.rows) {
+      work.turns.push_back((t.start + t.n + costs[wide].turn - 1) / costs[wide].turn);
+      work.per_split.push_back(hkv * tree_tiles(t.n * group, wide));
+      work.partial.push_back(t.n * hq);
+    }
     double time = 0;
-    const int p = best_piece(out.rows, per_split, hq, costs[wide], &time);
+    const int p = best_piece(work, costs[wide], &time);
     if (piece == 0 || time < best) best = time, piece = p, turn = costs[wide].turn, out.wide = wide;
   }
   for (TreeRow& t : out.rows) {

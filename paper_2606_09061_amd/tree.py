@@ -114,7 +114,8 @@ def _workspace(ws, nbytes, device, stream, what):
 
 
 def _nodes(rows):
-    return sum(rows[:, 2].tolist())   # (of a few rows, faster than numpy's)
+    n = rows[:, 2]
+    return int(n.sum()) if len(n) > 32 else sum(n.tolist())   # (the faster of the two)
 
 
 _I32, _I64, _BF16 = torch.int32, torch.int64, torch.bfloat16
