@@ -109,7 +109,8 @@ int cp_tree_verify(const void *logits, int64_t ld, int32_t vocab, const int32_t 
  * n_accepted[r] outside [0, max_path] is taken as the nearer bound.  Every
  * other slot is left as it was; a move whose table entry lies outside
  * [0, num_blocks) is left out.  No two rows may share a page that is written
- * to. */
+ * to, nor two layers a pool, and no other call in flight writes to such a page:
+ * those of V are read and written whole. */
 int cp_kv_compact(const cp_attn_desc *desc, void *const *k_caches, void *const *v_caches,
                   int32_t n_layers, const int32_t *block_tables, const cp_row_meta *rows,
                   int32_t n_rows, const int32_t *path, int32_t max_path,
@@ -133,7 +134,8 @@ typedef struct {
  * [0, num_reqs_in_table); every dst_req is named once, and by no fork as its
  * src_req; every used block is in [0, num_blocks) and named once; else
  * CP_ERR_BAD_META.  A page whose source entry lies outside [0, num_blocks) is
- * not copied.  Which blocks are free is the caller's to know. */
+ * not copied.  Which blocks are free is the caller's to know; a pool is named
+ * once. */
 int cp_kv_fork(const cp_attn_desc *desc, void *const *k_caches, void *const *v_caches,
                int32_t n_layers, int32_t *block_tables, const cp_fork *forks, int32_t n_forks,
                void *stream);

@@ -199,7 +199,8 @@ def verify(logits, tokens, parents, rows, target, path, n_accepted, next_token, 
 
 class KvLayers:
     """The K/V pools of a model's layers, as kv_compact and kv_fork take them:
-    checked once, and kept alive by this handle."""
+    checked once (none may share memory with another: what is moved in one
+    would move again in the next), and kept alive by this handle."""
 
     def __init__(self, desc, k_caches, v_caches):
         _want(len(k_caches) == len(v_caches) > 0, "kv_layers: one K and one V pool per layer")
@@ -211,6 +212,9 @@ class KvLayers:
             (ctypes.c_void_p * self.n)(*(_ptr(t, _BF16, (desc.num_blocks, hkv, *page), self.device,
                                               "kv_layers") for t in pools))
             for pools, page in zip(self.pools, ((b, d), (d, b))))
+        at = sorted([*self.k, *self.v])
+        _want(all(y - x >= 2 * desc.num_blocks * hkv * d * b for x, y in zip(at, at[1:])),
+              "kv_layers: no two pools share memory")
 
     def table(self, block_tables, what):
         d = self.desc

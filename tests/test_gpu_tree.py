@@ -224,6 +224,24 @@ def test_attn_batches_of_many_rows():
     c.check(c.run(), "300 rows")
 
 
+@pytest.mark.parametrize("n", [2, 70])
+def test_attn_splits_behind_a_full_launch(n):
+    """More rows than travel in one launch, the long ones, whose ranges are split
+    and merged, at its end and behind it."""
+    rng = np.random.default_rng(n)
+    rows = [(int(rng.integers(0, 40)), 1) for _ in range(118)]
+    for r, a in ((3, 5000), (111, 9000), (112, 7001), (117, 6000)):
+        rows[r] = (a, n)
+    c = Case(4, 1, 128, 16, rows, 21)
+    c.check(c.run(), "118 rows")
+
+
+@pytest.mark.parametrize("lens", [[1] * 7, [1] * 8, [1] * 9, [0, 4] * 8, [0] * 9 + [5]])
+def test_attn_numbers_of_rows_around_the_short_argument_block(lens):
+    c = Case(8, 2, 64, 16, [(11 * i, n) for i, n in enumerate(lens)], 22)
+    c.check(c.run(), f"{len(lens)} rows")
+
+
 def test_attn_mixed_tree_sizes():
     rows = [(int(a), int(n)) for a, n in zip([10, 900, 0, 333, 77, 2500, 31, 500, 64],
                                              [256, 1, 100, 16, 8, 60, 33, 2, 128])]
@@ -511,6 +529,41 @@ def test_verify_is_repeatable_on_a_stream_and_in_a_graph():
         d2.check(out, 8)
 
 
+@pytest.mark.parametrize("rows", [7, 8, 9, 256, 257])
+def test_layout_and_verify_numbers_of_rows(rows):
+    """Around the short argument block and the full one; two verifications at
+    once, on streams of their own, each with its own workspace."""
+    lens = [1 + r % 3 for r in range(rows)]
+    a, b = Drafts(lens, 40, rows), Drafts(lens[::-1], 40, rows + 1)
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for s in streams:
+        s.wait_stream(torch.cuda.current_stream())
+    outs = []
+    for x, s in zip((a, b), streams):
+        with torch.cuda.stream(s):
+            outs.append(x.run(4))
+    torch.cuda.synchronize()
+    a.check(outs[0], 4)
+    b.check(outs[1], 4)
+
+
+def test_verify_of_the_smallest_numbers():
+    """Denormal logits differ, and the smallest one is above both zeros."""
+    g = torch.zeros(4, 30, dtype=torch.int16)
+    g[0, 7] = 1                     # the smallest positive value
+    g[1, :] = -32768                # -0 ...
+    g[1, 9] = 0                     # ... equals +0: the first one wins
+    g[2, :] = -32768 + 2            # negative denormals
+    g[2, 11] = -32768 + 1
+    g[3, 4], g[3, 20] = 0x7f, 0x80  # the largest denormal, the smallest normal number
+    rows = np.array([(0, 0, 1, 1)] * 4, np.int32)
+    i32 = dict(dtype=torch.int32, device=DEV)
+    target, count, after = (torch.empty(4, **i32) for _ in range(3))
+    tree.verify(g.to(DEV).view(torch.bfloat16), torch.zeros(4, **i32), torch.full((4,), -1, **i32),
+                rows, target, torch.empty(4, 2, **i32), count, after)
+    assert target.tolist() == after.tolist() == [7, 0, 11, 20] and count.tolist() == [1] * 4
+
+
 # ---------------------------------------------------------------- the pools
 
 def _layers_of(c, n, seed):
@@ -610,6 +663,96 @@ def test_many_forks_and_pages_that_are_none():
     assert np.array_equal(bt.cpu().numpy(), want[0][2])
     _same(kd, [w[0] for w in want])
     _same(vd, [w[1] for w in want])
+
+
+@pytest.mark.parametrize("d,block", [(128, 16), (64, 32), (64, 16), (128, 32)])
+def test_compact_paths_of_more_than_a_wave(d, block):
+    """Paths of up to 256 nodes, whole, with few or many gaps, and ended by an
+    entry that does not rise at the border of two groups of 64."""
+    rows = [(0, 256), (13, 256), (100, 256), (31, 200), (1, 130), (63, 66), (5, 256)]
+    c = Case(2, 2, d, block, rows, d + block)
+    n = c.rows[:, 2]
+    path = np.full((len(rows), 256), -1, np.int32)
+    count = np.zeros(len(rows), np.int32)
+    for r, k in enumerate([256, 255, 129, 192, 128, 65, 200]):
+        path[r, :k] = np.sort(c.rng.choice(n[r], k, replace=False))
+        count[r] = k
+    path[3, 64] = path[3, 63]            # the first of the second group does not rise
+    path[4, 127] = path[4, 126] - 1      # nor does the last of it here
+    path[6, 128:] = -1                   # ends between groups, though more are counted
+    ks, vs, (kd, vd) = _layers_of(c, 2, 12)
+    tree.kv_compact(tree.kv_layers(c.desc(), kd, vd), torch.from_numpy(c.table).to(DEV), c.rows,
+                    torch.from_numpy(path).to(DEV), torch.from_numpy(count).to(DEV))
+    want = [ref.compact(k.numpy(), v.numpy(), c.table, c.rows.tolist(), path, count)
+            for k, v in zip(ks, vs)]
+    _same(kd, [w[0] for w in want])
+    _same(vd, [w[1] for w in want])
+
+
+def test_moves_and_forks_in_a_graph_and_on_two_streams():
+    """A fork and a compaction captured once and replayed on new contents, while
+    another pair of pools goes through the same calls on a stream of its own."""
+    def case(seed):
+        c = Case(2, 2, 128, 16, [(21, 40), (70, 12)], 33, spare=6)
+        src, new = int(c.rows[0, 0]), [r for r in range(4) if r not in c.rows[:, 0]]
+        forks = np.array([(src, new[0], 10, c.free[0]), (src, new[1], 16, -1)], np.int32)
+        rng = np.random.default_rng(seed)
+        path = np.full((2, 12), -1, np.int32)
+        for r, k in enumerate((12, 7)):
+            path[r, :k] = np.sort(rng.choice(int(c.rows[r, 2]), k, replace=False))
+        return c, forks, path, np.array([12, 7], np.int32), _layers_of(c, 3, seed)
+
+    def expect(c, forks, path, count, pools):
+        ks, vs, _ = pools
+        bt = ref.fork(ks[0].numpy(), vs[0].numpy(), c.table, forks.tolist())[2]
+        out = [ref.fork(k.numpy(), v.numpy(), c.table, forks.tolist())[:2] for k, v in zip(ks, vs)]
+        out = [ref.compact(k, v, bt, c.rows.tolist(), path, count) for k, v in out]
+        return bt, [o[0] for o in out], [o[1] for o in out]
+
+    c, forks, path, count, (ks, vs, (kd, vd)) = case(1)
+    handle = tree.kv_layers(c.desc(), kd, vd)
+    bt, p, n = (torch.from_numpy(x).to(DEV) for x in (c.table, path, count))
+
+    def both(handle, bt, p, n, stream=None):
+        tree.kv_fork(handle, bt, forks, stream)
+        tree.kv_compact(handle, bt, c.rows, p, n, stream)
+
+    both(handle, bt, p, n)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        both(handle, bt, p, n)
+    side = torch.cuda.Stream()
+    for i in range(4):
+        now, other = case(2 + i), case(20 + i)
+        for dst, src in zip(kd + vd, now[4][2][0] + now[4][2][1]):
+            dst.copy_(src)
+        bt.copy_(torch.from_numpy(c.table))
+        p.copy_(torch.from_numpy(now[2]))
+        n.copy_(torch.from_numpy(now[3]))
+        obt, op, on = (torch.from_numpy(x).to(DEV) for x in (c.table, other[2], other[3]))
+        oh = tree.kv_layers(c.desc(), *other[4][2])
+        torch.cuda.synchronize()
+        graph.replay()
+        both(oh, obt, op, on, side)
+        torch.cuda.synchronize()
+        for got, want in (((bt, kd, vd), expect(*now)), ((obt, *other[4][2]), expect(*other))):
+            assert np.array_equal(got[0].cpu().numpy(), want[0]), i
+            _same(got[1], want[1])
+            _same(got[2], want[2])
+
+
+def test_pools_that_share_memory_are_refused():
+    c = Case(2, 2, 64, 16, [(20, 3)], 34)
+    k = torch.zeros(2, *c.k.shape, dtype=torch.bfloat16, device=DEV)
+    v = torch.zeros(2, *c.v.shape, dtype=torch.bfloat16, device=DEV)
+    tree.kv_layers(c.desc(), list(k), list(v))
+    flat = k.view(-1)
+    shifted = flat[8:8 + k[0].numel()].view(c.k.shape)
+    for ks, vs in (([k[0], k[0]], list(v)), (list(k), [v[1], v[1]]),
+                   ([k[0], shifted], list(v)), ([k[0]], [k[0].view(c.v.shape)])):
+        with pytest.raises(cp.CpError):
+            tree.kv_layers(c.desc(), ks, vs)
 
 
 # ---------------------------------------------------------------- a round of them together
