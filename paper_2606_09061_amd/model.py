@@ -549,6 +549,10 @@ class Model:
             raise ValueError(f"batch of {T} tokens exceeds the model's {self.max_tokens}")
         if (rows[:, 2] > tree.MAX_NODES).any() or not 1 <= max_path <= tree.MAX_NODES:
             raise ValueError(f"a tree has at most {tree.MAX_NODES} nodes, and so its path")
+        for t in (tokens, parents):   # (index_select would resize its output to others)
+            if t.shape != (T,) or t.dtype != torch.int32 or t.device != self.x.device:
+                raise cp.CpError(cp.CP_ERR_INVALID_ARG,
+                                 f"verify: tokens and parents are int32 [{T}] on {self.x.device}")
         s = stream or torch.cuda.current_stream(self.dev)
         with torch.cuda.stream(s):
             i32 = dict(dtype=torch.int32, device=self.dev)

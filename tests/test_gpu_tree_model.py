@@ -143,3 +143,21 @@ def test_verify_of_empty_batches_and_its_refusals():
     bare = M.Model(CFG, max_seqs=1, max_seq_len=64, max_tokens=64, seed=1, lm_head=False)
     with pytest.raises(ValueError):
         bare.verify([(0, 0, 1, 1)], none, none)
+
+
+def test_verify_refuses_other_tokens():
+    """Before anything runs: the model's buffers and cache stay as they were."""
+    m = _model(1)
+    t = torch.zeros(3, dtype=torch.int32, device=m.dev)
+    par = torch.tensor([-1, 0, 0], dtype=torch.int32, device=m.dev)
+    m.pos.fill_(-7)
+    m.x.fill_(2)
+    before, kc = m.x.data_ptr(), [k.view(torch.int16).clone() for k in m.kc]
+    for tok, parents in ((t[:2], par), (t.repeat(2), par), (t.long(), par), (t.cpu(), par),
+                         (t[None], par), (t, par[:2]), (t, par.long()), (t, par.cpu())):
+        with pytest.raises(M.cp.CpError):
+            m.verify([(0, 0, 3, 3)], tok, parents)
+    torch.cuda.synchronize()
+    assert m.x.data_ptr() == before and m.x.shape[0] == 2048
+    assert (m.x == 2).all() and (m.pos == -7).all()
+    assert all(torch.equal(k.view(torch.int16), w) for k, w in zip(m.kc, kc))
