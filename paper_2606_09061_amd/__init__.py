@@ -5,7 +5,8 @@ path: the varlen planner, the paged KV append, the bf16-MFMA prefill-chunk
 kernel, the split-K decode kernel and the merge pass.  ``binding`` is the
 ctypes layer over its C ABI (include/cp_attn.h), re-exported here; the
 scheduler (``sched``, ``lprs``, ``serve``) and the decoder layer around the
-step (``model``) sit on top of it.
+step (``model``) sit on top of it, and ``tree`` (libcptree.so) holds
+speculative decoding and forks of requests over the same cache.
 """
 
 from .binding import (  # noqa: F401
