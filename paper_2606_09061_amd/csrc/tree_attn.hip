@@ -40,8 +40,9 @@ __device__ __forceinline__ f32x4_t mfma16x16x32(uint4 a, uint4 b, f32x4_t c) {
 // A workgroup takes 16 NC of a kv head's rows and a piece of the key range, of
 // which wave w takes tiles of 32 keys w, w + 4, ...  (With one such tile of rows
 // the stream of K and V bounds it: 32 requests of 8 nodes on 32/8 heads, 206 MB,
-// 39 us or 5.3 TB/s.)  The rows are the columns of both products (v_mfma_f32_16x16x32_bf16, NC of them
-// per operand of K or V).  Per tile and wave, lane l = 16 g + i:
+// 38 us or 5.4 TB/s.)  The rows are the columns of both products
+// (v_mfma_f32_16x16x32_bf16, NC of them per operand of K or V).  Per tile and
+// wave, lane l = 16 g + i:
 //   S^T (2 x 16 keys x 16 NC rows) = K . Q^T.  Row i of key half b is key
 //     8 (i / 4) + 4 b + i % 4, so that lane (g, i) ends up with rows i's scores
 //     of keys 8 g .. 8 g + 7, the B operand of the second product: the
@@ -416,6 +417,8 @@ hipError_t launch_narrow_t(int most, const AttnArgs& a, const TreeRows& rows, in
                            hipStream_t s) {
   static_assert(kNarrowRows == 32, "columns");
   return by_size(rows, n_rows, [&](const auto& r) {
+    // one column of rows saves registers and products: a request of 16 rows after
+    // 300 keys 7.0 us, with two columns 7.9; 32 of them after 1,000 keys 37.4 / 37.8
     if (most <= 16)
       hipLaunchKernelGGL((narrow_kernel<D, B, 1>), dim3(items), dim3(kThreads), 0, s, r, a, a.q,
                          a.k_cache, a.v_cache, a.bt, a.mask);

@@ -68,7 +68,9 @@ __device__ __forceinline__ uint64_t wave_max64(uint64_t x) {
   return x;
 }
 
-constexpr int kArgmaxWords = 4;  // 16-byte words of a thread on their way at a time
+// 16-byte words of a thread on their way at a time (1,024 nodes of 151,936
+// logits: two 40.4 us, four 39.1, eight 39.5; 32 nodes 14.4, 14.8, 15.8).
+constexpr int kArgmaxWords = 4;
 
 // best[t][piece] = the best candidate of a piece of node t's logits.  Rows may
 // start at any bf16: whole 16-byte words are read as such, the ends one value
@@ -360,6 +362,7 @@ hipError_t launch_layout(const int32_t* parents, const NodeRows& rows, int n_row
 
 int verify_pieces(int64_t n_tokens, int32_t vocab) {
   // about 2,048 workgroups (8 per CU), each of at least four words per thread
+  // (1,024 nodes of 151,936 logits 39.1 us; of 512 workgroups 42.5, of 8,192 39.8)
   const int64_t want = (2048 + n_tokens - 1) / std::max<int64_t>(n_tokens, 1);
   const int64_t most = std::max<int64_t>(vocab / (4 * 8 * kThreads), 1);
   return (int)std::max<int64_t>(std::min(want, most), 1);
