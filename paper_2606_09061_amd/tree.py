@@ -77,28 +77,33 @@ def _want(ok, what):
 
 
 def _ptr(t, dtype, shape, device, what):
-    """The address of a dense tensor of this type and shape on this device."""
-    if (t.dtype != dtype or t.shape != shape or not t.is_contiguous() or t.device != device
-            or t.is_neg()):
+    """The address of a dense tensor of this type and shape on this GPU (its
+    index: comparing device objects costs as much as the other checks)."""
+    if (t.dtype is not dtype or t.shape != shape or not t.is_contiguous()
+            or t.get_device() != device or t.is_neg()):
         raise cp.CpError(cp.CP_ERR_INVALID_ARG,
-                         f"{what}: a dense {dtype} tensor {tuple(shape)} on {device} is wanted, "
-                         f"got {t.dtype} {tuple(t.shape)} on {t.device}")
+                         f"{what}: a dense {dtype} tensor {tuple(shape)} on cuda:{device} is "
+                         f"wanted, got {t.dtype} {tuple(t.shape)} on {t.device}")
     return t.data_ptr()
 
 
 def _device(t, what):
-    _want(t.is_cuda, f"{what}: tensors on a GPU are wanted, got {t.device}")
-    return t.device
+    """The index of a tensor's GPU."""
+    index = t.get_device()
+    if index < 0:
+        raise cp.CpError(cp.CP_ERR_INVALID_ARG,
+                         f"{what}: tensors on a GPU are wanted, got {t.device}")
+    return index
 
 
 def _call(device, stream, f, *args):
     """f(*args, stream) with ``device`` current; the raw stream is looked up
     without the stream objects, which cost more than a launch."""
-    if torch._C._cuda_getDevice() != device.index:
+    if torch._C._cuda_getDevice() != device:
         with torch.cuda.device(device):
             return f(*args, cp._stream(stream))
     if stream is None:
-        return f(*args, torch._C._cuda_getCurrentRawStream(device.index))
+        return f(*args, torch._C._cuda_getCurrentRawStream(device))
     return f(*args, cp._stream(stream))
 
 
@@ -106,10 +111,11 @@ def _workspace(ws, nbytes, device, stream, what):
     """(address, bytes) of ws, allocated for the stream when None (and returned,
     to be held until the launches are enqueued)."""
     if ws is None:
-        ws = _scratch(nbytes(), device, stream)
+        ws = _scratch(nbytes(), torch.device("cuda", device), stream)
         if ws is None:
             raise cp.CpError(cp.CP_ERR_WORKSPACE, what)
-    _want(ws.device == device and ws.is_contiguous(), f"{what}: ws is dense and on {device}")
+    if ws.get_device() != device or not ws.is_contiguous():
+        raise cp.CpError(cp.CP_ERR_INVALID_ARG, f"{what}: ws is dense and on cuda:{device}")
     return ws, ws.data_ptr(), ws.numel() * ws.element_size()
 
 
@@ -159,7 +165,8 @@ def attn(desc, q, k_cache, v_cache, block_tables, mask, rows, out, ws=None, stre
     ws, ws_ptr, ws_bytes = _workspace(ws, lambda: attn_workspace_bytes(desc, rows), dev, stream,
                                       what)
     _check(_call(dev, stream, load().cp_tree_attn, ctypes.byref(desc),
-                 _ptr(q, _BF16, (T, hq, d), dev, what), _ptr(k_cache, _BF16, (nb, hkv, b, d), dev, what),
+                 _ptr(q, _BF16, (T, hq, d), dev, what),
+                 _ptr(k_cache, _BF16, (nb, hkv, b, d), dev, what),
                  _ptr(v_cache, _BF16, (nb, hkv, d, b), dev, what),
                  _ptr(block_tables, _I32, (desc.num_reqs_in_table, desc.max_blocks_per_req), dev,
                       what), _ptr(mask, _I64, (T, W), dev, what), W, rows.tobytes(),
