@@ -284,6 +284,48 @@ def test_attn_on_another_stream_and_two_at_once():
     b.check(outs[1], "stream 1")
 
 
+def test_attn_from_two_threads():
+    """The host's side of a call keeps nothing that another thread's could meet."""
+    import threading
+    cases = [Case(8, 2, 128, 16, [(3000, 20), (40, 5)], 23), Case(4, 1, 64, 32, [(900, 70)], 24),
+             Case(32, 8, 128, 16, [(60 * i, 3) for i in range(30)], 25)]
+    gpu = [c.gpu() for c in cases]
+    want = [c.run(g) for c, g in zip(cases, gpu)]
+    torch.cuda.synchronize()
+    bad = []
+
+    def work(c, g, w):
+        s = torch.cuda.Stream()
+        for _ in range(40):
+            out = torch.empty_like(g["q"])
+            c.run(g, out=out, stream=s)
+            s.synchronize()
+            if not torch.equal(out.view(torch.int16), w.view(torch.int16)):
+                bad.append(c)
+
+    threads = [threading.Thread(target=work, args=x) for x in zip(cases, gpu, want)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not bad
+
+
+@pytest.mark.parametrize("words", [1, 2, 3, 4])
+@pytest.mark.parametrize("rows", [[(700, 3), (40, 30)], [(300, 64), (90, 33), (5, 1)]])
+def test_attn_masks_wider_than_the_trees(rows, words):
+    """Narrow and wide kernels; the words behind a tree's nodes may hold anything."""
+    c = Case(8, 1, 128, 16, rows, 26)
+    mask = np.full((c.t, words), (1 << 64) - 1, np.uint64)
+    mask[:, :1] = c.mask
+    for t, n in enumerate(np.repeat(c.rows[:, 2], c.rows[:, 2]).tolist()):
+        if n < 64:
+            mask[t, 0] |= np.uint64(((1 << 64) - 1) >> n << n)
+    g = c.gpu()
+    g["mask"] = torch.from_numpy(mask.view(np.int64)).to(DEV)
+    c.check(c.run(g), f"{words} words")
+
+
 def test_attn_in_a_graph():
     """Captured once, replayed on new contents of the same buffers."""
     c, other = (Case(8, 2, 128, 16, [(2000, 30), (40, 5)], 17) for _ in range(2))
