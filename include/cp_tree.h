@@ -44,6 +44,11 @@ extern "C" {
 
 #define CP_TREE_MAX_NODES 256
 
+/* Keys (chunk_start + chunk_len) that a row of cp_tree_attn may have: more do
+ * not fit the memory with pages of their own, and the bound keeps key indexes
+ * in 32 bits when they are rounded up to pieces. */
+#define CP_TREE_MAX_KEYS (1 << 30)
+
 /* Masks and positions of drafted trees.  parents[t] is the index inside its
  * row of node t's parent; anything but an index before the node's own (-1, by
  * convention, for the root) ends the chain of ancestors.  With W = mask_words
@@ -56,7 +61,8 @@ int cp_tree_layout(const int32_t *parents, const cp_row_meta *rows, int32_t n_ro
                    uint64_t *mask, int32_t mask_words, int32_t *positions, void *stream);
 
 /* Workspace bytes cp_tree_attn needs for this batch, or 0 if desc/rows are
- * invalid or a row has more than CP_TREE_MAX_NODES nodes. */
+ * invalid or a row has more than CP_TREE_MAX_NODES nodes or CP_TREE_MAX_KEYS
+ * keys. */
 size_t cp_tree_attn_workspace_bytes(const cp_attn_desc *desc, const cp_row_meta *rows,
                                     int32_t n_rows);
 
@@ -70,7 +76,8 @@ size_t cp_tree_attn_workspace_bytes(const cp_attn_desc *desc, const cp_row_meta 
  * rounded to bf16 for the product with V and summed as rounded.  q, out
  * [T][Hq][D], mask [T][mask_words] (8-byte aligned), ws 256-byte aligned; out
  * must not overlap q.  Checks as for cp_attn_mixed; more nodes than
- * min(64 * mask_words, CP_TREE_MAX_NODES) in a row is CP_ERR_BAD_META.
+ * min(64 * mask_words, CP_TREE_MAX_NODES) in a row is CP_ERR_BAD_META, more
+ * keys than CP_TREE_MAX_KEYS CP_ERR_UNSUPPORTED.
  * Long key ranges are split and merged by a log-sum-exp pass; the result of a
  * batch does not depend on anything but its inputs. */
 int cp_tree_attn(const cp_attn_desc *desc, const void *q, const void *k_cache,

@@ -91,6 +91,16 @@ int check_geometry(const cp_attn_desc* desc, const cp_row_meta* rows, int32_t n_
   return check_rows(rows, n_rows, most, tokens);
 }
 
+// Rows that the plan of the attention can take.
+int check_attn(const cp_attn_desc* desc, const cp_row_meta* rows, int32_t n_rows, int most,
+               int64_t* tokens) {
+  const int rc = check_geometry(desc, rows, n_rows, most, tokens);
+  if (rc != CP_OK) return rc;
+  for (int32_t r = 0; r < n_rows; ++r)
+    if (rows[r].chunk_len > 0 && rows[r].ctx_len > CP_TREE_MAX_KEYS) return CP_ERR_UNSUPPORTED;
+  return CP_OK;
+}
+
 int check_pools(void* const* k_caches, void* const* v_caches, int32_t n_layers) {
   if (n_layers < 0 || (n_layers > 0 && (!k_caches || !v_caches))) return CP_ERR_INVALID_ARG;
   for (int32_t i = 0; i < n_layers; ++i)
@@ -218,7 +228,7 @@ size_t cp_tree_attn_workspace_bytes(const cp_attn_desc* desc, const cp_row_meta*
   size_t bytes = 0;
   const int rc = guarded([&] {
     int64_t tokens = 0;
-    const int e = check_geometry(desc, rows, n_rows, kMaxNodes, &tokens);
+    const int e = check_attn(desc, rows, n_rows, kMaxNodes, &tokens);
     if (e != CP_OK) return e;
     TreePlan& p = thread_plan();
     plan_tree(*desc, rows, n_rows, p);
@@ -235,7 +245,7 @@ int cp_tree_attn(const cp_attn_desc* desc, const void* q, const void* k_cache,
   return guarded([&] {
     if (mask_words < 1 || mask_words > kMaxWords) return CP_ERR_INVALID_ARG;
     int64_t tokens = 0;
-    int rc = check_geometry(desc, rows, n_rows, 64 * mask_words, &tokens);
+    int rc = check_attn(desc, rows, n_rows, 64 * mask_words, &tokens);
     if (rc != CP_OK || tokens == 0) return rc;
     if (!q || !k_cache || !v_cache || !block_tables || !mask || !out || !ws || !aligned(q, 16) ||
         !aligned(k_cache, 16) || !aligned(v_cache, 16) || !aligned(out, 16) ||

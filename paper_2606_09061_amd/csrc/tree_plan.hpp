@@ -38,7 +38,8 @@ struct TreePlan {
 
 };
 
-// rows: valid for desc, at most kMaxNodes nodes each.
+// rows: valid for desc, at most kMaxNodes nodes and CP_TREE_MAX_KEYS keys each (key
+// indexes stay in 32 bits, rounded up to pieces and a piece further).
 void plan_tree(const cp_attn_desc& desc, const cp_row_meta* rows, int32_t n_rows, TreePlan& out);
 
 }  // namespace cptree

@@ -30,7 +30,8 @@ from .model import _scratch
 _PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_PKG, "libcptree.so")
 
-MAX_NODES = 256   # CP_TREE_MAX_NODES
+MAX_NODES = 256      # CP_TREE_MAX_NODES
+MAX_KEYS = 1 << 30   # CP_TREE_MAX_KEYS
 
 _lib = None
 
@@ -146,15 +147,16 @@ def attn_workspace_bytes(desc, rows) -> int:
     n = load().cp_tree_attn_workspace_bytes(ctypes.byref(desc), rows.tobytes(), rows.shape[0])
     if n == 0:
         rc = cp.check_batch(desc, rows)
-        raise cp.CpError(rc if rc != cp.CP_OK else cp.CP_ERR_BAD_META,
-                         "cp_tree_attn_workspace_bytes")
+        if rc == cp.CP_OK:   # what the tree attention checks beyond it
+            rc = cp.CP_ERR_BAD_META if (rows[:, 2] > MAX_NODES).any() else cp.CP_ERR_UNSUPPORTED
+        raise cp.CpError(rc, "cp_tree_attn_workspace_bytes")
     return int(n)
 
 
 def attn(desc, q, k_cache, v_cache, block_tables, mask, rows, out, ws=None, stream=None):
     """out [T, Hq, D]: every drafted node over its request's committed keys and
-    the nodes that its mask (int64 [T, W]) names.  ``ws``: uint8 of at least
-    attn_workspace_bytes (allocated here when None)."""
+    the nodes that its mask (int64 [T, W]) names, MAX_KEYS keys a row at most.
+    ``ws``: uint8 of at least attn_workspace_bytes (allocated here when None)."""
     what = "cp_tree_attn"
     rows = cp._rows(rows)
     dev, T = _device(q, what), _nodes(rows)

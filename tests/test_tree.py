@@ -298,3 +298,44 @@ def test_plan_under_sanitizers(tmp_path):
                     os.path.join(csrc, "tree_plan.cpp"), "-o", exe], check=True, timeout=300)
     r = subprocess.run([exe], capture_output=True, text=True, timeout=300)
     assert r.returncode == 0 and r.stdout.startswith("ok"), r.stderr[-2000:]
+
+
+# ---------------------------------------------------------------- the longest contexts
+
+LONGEST = 1 << 30   # keys of a row
+
+
+def _far(ctx, n=3):
+    return _desc(max_blocks_per_req=(1 << 27) - 1), _rows([0, ctx - n, n, ctx])
+
+
+@pytest.mark.parametrize("ctx", [LONGEST + 1, 2147475000, 2147483521, 2147483632])
+def test_contexts_past_the_longest_are_refused(ctx):
+    """In a process of its own: the plan of such rows used to divide by zero."""
+    import subprocess
+    import sys
+    code = (f"import test_tree as t\n"
+            f"d, rows = t._far({ctx})\n"
+            f"assert t._attn(d, rows) == t.binding.CP_ERR_UNSUPPORTED\n"
+            f"try:\n    t.tree.attn_workspace_bytes(d, rows)\n"
+            f"except t.cp.CpError as e:\n    assert e.code == t.binding.CP_ERR_UNSUPPORTED\n"
+            f"else:\n    raise SystemExit('not refused')\n")
+    env = dict(os.environ, PYTHONPATH=os.pathsep.join([ROOT, os.path.join(ROOT, "tests")]))
+    r = subprocess.run([sys.executable, "-c", code], env=env, capture_output=True, text=True,
+                       timeout=300)
+    assert r.returncode == 0, (r.returncode, r.stderr[-2000:])
+
+
+def test_the_longest_context_is_planned():
+    need = tree.attn_workspace_bytes(*_far(LONGEST))
+    assert need > 1 << 20
+    assert _attn(*_far(LONGEST), ws_bytes=need - 1) == binding.CP_ERR_WORKSPACE
+
+
+def test_refusals_of_the_workspace_query_name_their_reason():
+    for d, rows, code in ((_desc(), _rows([0, 10, 257, 267]), binding.CP_ERR_BAD_META),
+                          (_desc(num_q_heads=2048, num_kv_heads=2048), GOOD,
+                           binding.CP_ERR_UNSUPPORTED)):
+        with pytest.raises(cp.CpError) as e:
+            tree.attn_workspace_bytes(d, rows)
+        assert e.value.code == code
