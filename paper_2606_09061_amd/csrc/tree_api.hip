@@ -21,7 +21,8 @@ namespace {
 constexpr int kMaxKvHeads = 1024;
 constexpr int64_t kMaxTokens = 1 << 23;
 constexpr int32_t kMaxVocab = 1 << 30;
-constexpr int kMaxItems = 1 << 22;
+static_assert(kMaxRowItems >= kMaxKvHeads * tree_tiles(8 * kMaxNodes, true) &&
+              kMaxRowItems >= kMaxKvHeads * tree_tiles(8 * kNarrowNodes, false));
 
 bool aligned(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
 
@@ -144,13 +145,13 @@ int by_node_rows(const cp_row_meta* rows, int32_t n_rows, F&& f) {
 
 // f(rows of one launch, their number, its workgroups) for rows in batches, the
 // places behind them no workgroup's; items_of(row) is the number of a row's
-// workgroups, of which a launch takes some 2^22 (2^32 threads are its limit).
+// workgroups.
 template <class Items, class F>
 int by_tree_rows(const std::vector<TreeRow>& rows, Items&& items_of, F&& f) {
   for (size_t r = 0; r < rows.size();) {
     TreeRows batch;
     int items = 0, n = 0;
-    for (; r < rows.size() && n < kTreeRows && items < kMaxItems; ++r) {
+    for (; r < rows.size() && n < kTreeRows; ++r) {
       batch.r[n] = rows[r];
       batch.r[n++].item0 = items;
       items += items_of(rows[r]);

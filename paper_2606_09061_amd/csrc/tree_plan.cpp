@@ -2,7 +2,6 @@
 #include "tree_plan.hpp"
 
 #include <algorithm>
-#include <climits>
 
 namespace cptree {
 
@@ -157,11 +156,6 @@ void plan_tree(const cp_attn_desc& desc, const cp_row_meta* rows, int32_t n_rows
     t.n_split = (turns + per - 1) / per;
     if (t.n_split == 1) continue;
     const int64_t partial = (int64_t)t.n_split * t.n * hq;
-    if (out.partial_rows + partial > INT_MAX) {  // beyond their index type
-      t.split_keys = turns * turn;
-      t.n_split = 1;
-      continue;
-    }
     t.part0 = (int32_t)out.partial_rows;
     out.partial_rows += partial;
     out.merge.push_back(t);

@@ -28,6 +28,16 @@ constexpr int merge_rows(int d, int n_split) {
   return rows;
 }
 
+// Bounds that need no check.  Rows that are split make at most kMaxSplitItems
+// workgroups: cutting brings their number to the next rounds of the GPU's 512
+// slots, 2,048 more than the rows uncut, or to 8 times at most 512, and a row
+// that is cut at least doubles its own.  An uncut row makes 16 per kv head at
+// most.  So the partial rows, 128 a workgroup, keep to 32-bit indexes, and the
+// kTreeRows rows of a launch to the 2^24 workgroups of 256 threads that it takes.
+constexpr int64_t kMaxSplitItems = 4096, kMaxPartialRows = kMaxSplitItems * kWideRows;
+constexpr int kMaxRowItems = 16 << 10;  // of 1,024 kv heads
+static_assert((int64_t)kTreeRows * kMaxRowItems + kMaxSplitItems < 1 << 24, "a launch's grid");
+
 struct TreePlan {
   bool wide = false;           // the kernel
   int most = 0;                // rows of the products of the largest tree

@@ -339,3 +339,20 @@ def test_refusals_of_the_workspace_query_name_their_reason():
         with pytest.raises(cp.CpError) as e:
             tree.attn_workspace_bytes(d, rows)
         assert e.value.code == code
+
+
+def test_plan_at_the_ends_of_its_ranges(tmp_path):
+    """Host C++: contexts of up to 2^30 keys, up to 1,024 kv heads and many rows,
+    under sanitizers (tests/native/tree_bounds.cpp)."""
+    import shutil
+    import subprocess
+    if shutil.which("g++") is None:
+        pytest.skip("needs g++")
+    csrc = os.path.join(ROOT, "paper_2606_09061_amd", "csrc")
+    exe = str(tmp_path / "tree_bounds")
+    subprocess.run(["g++", "-std=c++17", "-O1", "-g", "-fsanitize=address,undefined",
+                    "-fno-sanitize-recover=all", "-I", os.path.join(ROOT, "include"), "-I", csrc,
+                    os.path.join(ROOT, "tests", "native", "tree_bounds.cpp"),
+                    os.path.join(csrc, "tree_plan.cpp"), "-o", exe], check=True, timeout=300)
+    r = subprocess.run([exe], capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and r.stdout.startswith("ok"), r.stderr[-2000:]
