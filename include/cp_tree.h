@@ -85,8 +85,9 @@ int cp_tree_attn(const cp_attn_desc *desc, const void *q, const void *k_cache,
                  int32_t mask_words, const cp_row_meta *rows, int32_t n_rows, void *out, void *ws,
                  size_t ws_bytes, void *stream);
 
-/* Workspace bytes cp_tree_verify needs for n_tokens nodes in all, or 0 if a
- * size is out of range (n_tokens < 0, vocab < 1). */
+/* Workspace bytes cp_tree_verify needs for up to n_tokens nodes in all (one
+ * that serves a batch serves every smaller one), or 0 if a size is out of range
+ * (n_tokens < 0, vocab < 1). */
 size_t cp_tree_verify_workspace_bytes(int64_t n_tokens, int32_t vocab);
 
 /* Greedy verification.  logits: bf16 [T], rows of vocab values at a stride of

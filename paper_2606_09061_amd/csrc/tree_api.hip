@@ -300,7 +300,7 @@ int cp_tree_attn(const cp_attn_desc* desc, const void* q, const void* k_cache,
 
 size_t cp_tree_verify_workspace_bytes(int64_t n_tokens, int32_t vocab) {
   if (n_tokens < 0 || n_tokens > kMaxTokens || vocab < 1 || vocab > kMaxVocab) return 0;
-  return std::max<size_t>(256, (size_t)n_tokens * verify_pieces(n_tokens, vocab) * 8);
+  return std::max<size_t>(256, (size_t)verify_candidates(n_tokens, vocab) * 8);
 }
 
 int cp_tree_verify(const void* logits, int64_t ld, int32_t vocab, const int32_t* tokens,
@@ -319,7 +319,8 @@ int cp_tree_verify(const void* logits, int64_t ld, int32_t vocab, const int32_t*
     if (!logits || !tokens || !parents || !target || !ws || !aligned(logits, 2) ||
         !aligned(tokens, 4) || !aligned(parents, 4) || !aligned(target, 4) || !aligned(ws, 256))
       return CP_ERR_INVALID_ARG;
-    if (ws_bytes < cp_tree_verify_workspace_bytes(total, vocab)) return CP_ERR_WORKSPACE;
+    const size_t need = (size_t)total * verify_pieces(total, vocab) * 8;
+    if (ws_bytes < std::max<size_t>(256, need)) return CP_ERR_WORKSPACE;
   }
   (void)hipGetLastError();
   hipStream_t s = (hipStream_t)stream;

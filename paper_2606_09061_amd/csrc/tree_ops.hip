@@ -360,12 +360,22 @@ hipError_t launch_layout(const int32_t* parents, const NodeRows& rows, int n_row
   });
 }
 
+// about 2,048 workgroups (8 per CU), each of at least four words per thread
+// (1,024 nodes of 151,936 logits 39.1 us; of 512 workgroups 42.5, of 8,192 39.8)
+static constexpr int64_t kArgmaxGroups = 2048;
+
+static int64_t most_pieces(int32_t vocab) {
+  return std::max<int64_t>(vocab / (4 * 8 * kThreads), 1);
+}
+
 int verify_pieces(int64_t n_tokens, int32_t vocab) {
-  // about 2,048 workgroups (8 per CU), each of at least four words per thread
-  // (1,024 nodes of 151,936 logits 39.1 us; of 512 workgroups 42.5, of 8,192 39.8)
-  const int64_t want = (2048 + n_tokens - 1) / std::max<int64_t>(n_tokens, 1);
-  const int64_t most = std::max<int64_t>(vocab / (4 * 8 * kThreads), 1);
-  return (int)std::max<int64_t>(std::min(want, most), 1);
+  const int64_t want = (kArgmaxGroups + n_tokens - 1) / std::max<int64_t>(n_tokens, 1);
+  return (int)std::max<int64_t>(std::min(want, most_pieces(vocab)), 1);
+}
+
+// n ceil(2048 / n) falls here and there; 2048 + n - 1, its bound, only rises.
+int64_t verify_candidates(int64_t n_tokens, int32_t vocab) {
+  return std::min(n_tokens * most_pieces(vocab), n_tokens + kArgmaxGroups - 1);
 }
 
 hipError_t launch_argmax(const uint16_t* logits, int64_t ld, int32_t vocab, int64_t n_tokens,

@@ -12,6 +12,8 @@ hipError_t launch_layout(const int32_t* parents, const NodeRows& rows, int n_row
 
 // The vocabulary's pieces, one workgroup each, when T nodes' logits are read.
 int verify_pieces(int64_t n_tokens, int32_t vocab);
+// The most candidates, nodes times pieces, of batches of up to T nodes.
+int64_t verify_candidates(int64_t n_tokens, int32_t vocab);
 
 hipError_t launch_argmax(const uint16_t* logits, int64_t ld, int32_t vocab, int64_t n_tokens,
                          int pieces, uint64_t* best, hipStream_t s);

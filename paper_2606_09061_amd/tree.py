@@ -176,6 +176,7 @@ def attn(desc, q, k_cache, v_cache, block_tables, mask, rows, out, ws=None, stre
 
 
 def verify_workspace_bytes(n_tokens, vocab) -> int:
+    """Bytes of verify's ``ws`` for batches of up to n_tokens nodes."""
     n = load().cp_tree_verify_workspace_bytes(int(n_tokens), int(vocab))
     if n == 0:
         raise cp.CpError(cp.CP_ERR_INVALID_ARG, "cp_tree_verify_workspace_bytes")

@@ -862,3 +862,12 @@ def test_a_drafted_round():
     c.rows, c.mask = rows4, ref.layout(dr2.parents, rows4, 1)[0]
     c.q, c.k, c.v = q2.cpu(), ks[0].cpu(), vs[0].cpu()
     c.check(out2, "next round")
+
+
+def test_one_verify_workspace_for_all_batches():
+    """Sized for 2,100 nodes, it serves fewer, whose vocabulary is cut into more pieces."""
+    vocab = 20000
+    ws = torch.empty(tree.verify_workspace_bytes(2100, vocab), dtype=torch.uint8, device=DEV)
+    for lens in ([1], [7], [250] * 8, [256] * 8 + [52], [255, 256, 256, 256]):
+        d = Drafts(lens, vocab, sum(lens))
+        d.check(d.run(5, ws=ws), 5)

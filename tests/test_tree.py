@@ -356,3 +356,11 @@ def test_plan_at_the_ends_of_its_ranges(tmp_path):
                     os.path.join(csrc, "tree_plan.cpp"), "-o", exe], check=True, timeout=300)
     r = subprocess.run([exe], capture_output=True, text=True, timeout=300)
     assert r.returncode == 0 and r.stdout.startswith("ok"), r.stderr[-2000:]
+
+
+@pytest.mark.parametrize("vocab", [1, 1000, 16384, 20000, 151936, 1 << 30])
+def test_a_verify_workspace_serves_fewer_nodes_too(vocab):
+    """A server sizes its workspace once, for its largest batch."""
+    sizes = [tree.verify_workspace_bytes(n, vocab) for n in range(4200)]
+    assert all(a <= b for a, b in zip(sizes, sizes[1:]))
+    assert sizes[-1] <= 8 * (4199 + 2047)                 # and is none too large
