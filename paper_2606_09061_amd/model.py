@@ -443,7 +443,6 @@ class Model:
         self.pos = torch.zeros(T, dtype=torch.int32, device=self.dev)
         self.tokens = torch.randint(0, c.vocab, (T,), generator=gen, device=self.dev)
         self.ws = torch.empty(64 << 20, dtype=torch.uint8, device=self.dev)      # attention plan
-        self.kv = None   # the pools as verify's compaction takes them
         # split-K partials of the projections (grown on demand)
         self.ws_gemm = torch.empty(256, dtype=torch.uint8, device=self.dev)
         # an append item covers one row's tokens inside one block: at most
@@ -575,9 +574,8 @@ class Model:
                 project(h, self.lm_head, logits, None, s, self.ws_gemm)
             tree.verify(logits, tokens, parents, rows, target, path, n_accepted, after, stream=s)
             if T > 0:
-                if self.kv is None:
-                    self.kv = tree.kv_layers(self.desc, self.kc, self.vc)
-                tree.kv_compact(self.kv, self.bt, rows, path, n_accepted, s)
+                tree.kv_compact(tree.kv_layers(self.desc, self.kc, self.vc), self.bt, rows, path,
+                                n_accepted, s)
         return target, path, n_accepted, after
 
 

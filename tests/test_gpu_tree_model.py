@@ -161,3 +161,43 @@ def test_verify_refuses_other_tokens():
     assert m.x.data_ptr() == before and m.x.shape[0] == 2048
     assert (m.x == 2).all() and (m.pos == -7).all()
     assert all(torch.equal(k.view(torch.int16), w) for k, w in zip(m.kc, kc))
+
+
+def _drafted(m, seed=5):
+    """A prompt of 30 tokens, then a star-shaped tree whose last node is the one
+    that agrees: it moves over the others' slots."""
+    rng = np.random.default_rng(seed)
+    prompt = rng.integers(0, CFG.vocab, 30)
+    after = _feed(m, [(0, 0, 30, 30)], [prompt])[0][0]
+    m.verify([(0, 30, 1, 31)], torch.tensor([after], dtype=torch.int32, device=m.dev),
+             torch.tensor([-1], dtype=torch.int32, device=m.dev))
+    return after
+
+
+def _star(m, root, right):
+    tokens = torch.tensor([root, (right + 1) % CFG.vocab, (right + 2) % CFG.vocab, right],
+                          dtype=torch.int32, device=m.dev)
+    parents = torch.tensor([-1, 0, 0, 0], dtype=torch.int32, device=m.dev)
+    return m.verify([(0, 30, 4, 34)], tokens, parents)
+
+
+def test_verify_compacts_the_pools_that_the_layers_used():
+    """A layer's pools replaced between two iterations: the next one appends to,
+    attends over and compacts the new ones."""
+    a, b = _model(1), _model(1)
+    root = _drafted(a)
+    assert _drafted(b) == root
+    b.kc[1], b.vc[1] = b.kc[1].clone(), b.vc[1].clone()
+    right = int(_star(a, root, 0)[0][0])        # what the root is followed by
+    _star(b, root, 0)
+    got, want = _star(b, root, right), _star(a, root, right)
+    for x, y in zip(got, want):
+        assert torch.equal(x, y)
+    assert want[1][0, :3].tolist() == [0, 3, -1]
+    # every layer's K and V of the committed tokens
+    for x, y in zip(b.kc + b.vc, a.kc + a.vc):
+        for p in (30, 31):
+            at, slot = int(a.bt[0, p // CFG.block_size]), p % CFG.block_size
+            is_k = x.shape[3] == CFG.head_dim
+            u, w = (t[at, :, slot] if is_k else t[at, :, :, slot] for t in (x, y))
+            assert torch.equal(u.view(torch.int16), w.view(torch.int16))
