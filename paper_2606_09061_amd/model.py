@@ -549,9 +549,11 @@ class Model:
         if (rows[:, 2] > tree.MAX_NODES).any() or not 1 <= max_path <= tree.MAX_NODES:
             raise ValueError(f"a tree has at most {tree.MAX_NODES} nodes, and so its path")
         for t in (tokens, parents):   # (index_select would resize its output to others)
-            if t.shape != (T,) or t.dtype != torch.int32 or t.device != self.x.device:
-                raise cp.CpError(cp.CP_ERR_INVALID_ARG,
-                                 f"verify: tokens and parents are int32 [{T}] on {self.x.device}")
+            if (t.shape != (T,) or t.dtype != torch.int32 or t.device != self.x.device
+                    or not t.is_contiguous()):
+                raise cp.CpError(cp.CP_ERR_INVALID_ARG, "verify: tokens and parents are dense "
+                                 f"int32 [{T}] on {self.x.device}")
+        need = tree.attn_workspace_bytes(self.desc, rows) if T > 0 else 0   # (checks the rows)
         s = stream or torch.cuda.current_stream(self.dev)
         with torch.cuda.stream(s):
             i32 = dict(dtype=torch.int32, device=self.dev)
@@ -562,7 +564,6 @@ class Model:
                 words = -(-int(rows[:, 2].max()) // 64)
                 mask = torch.empty(T, words, dtype=torch.int64, device=self.dev)
                 tree.layout(parents, rows, mask, self.pos[:T], s)
-                need = tree.attn_workspace_bytes(self.desc, rows)
                 if need > self.ws.numel():
                     self.ws = torch.empty(need, dtype=torch.uint8, device=self.dev)
                 x, h = self.x[:T], self.h[:T]

@@ -201,3 +201,25 @@ def test_verify_compacts_the_pools_that_the_layers_used():
             is_k = x.shape[3] == CFG.head_dim
             u, w = (t[at, :, slot] if is_k else t[at, :, :, slot] for t in (x, y))
             assert torch.equal(u.view(torch.int16), w.view(torch.int16))
+
+
+@pytest.mark.parametrize("which", ["tokens", "parents", "table"])
+def test_verify_refuses_before_anything_runs(which):
+    """Tokens or parents that are not dense, and rows outside the table."""
+    m = _model(1)
+    tokens = torch.zeros(6, dtype=torch.int32, device=m.dev)[::2]
+    parents = torch.tensor([-1, -1, 0, 0, 0, 0], dtype=torch.int32, device=m.dev)[::2]
+    if which != "tokens":
+        tokens = tokens.contiguous()
+    if which != "parents":
+        parents = parents.contiguous()
+    rows = [(1, 0, 3, 3)] if which == "table" else [(0, 0, 3, 3)]
+    m.pos.fill_(-7)
+    m.x.fill_(2)
+    for x in m.kc + m.vc:
+        x.fill_(3)
+    with pytest.raises(M.cp.CpError):
+        m.verify(rows, tokens, parents)
+    torch.cuda.synchronize()
+    assert (m.x == 2).all() and (m.pos == -7).all()
+    assert all((x == 3).all() for x in m.kc + m.vc)
