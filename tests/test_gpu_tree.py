@@ -871,3 +871,34 @@ def test_one_verify_workspace_for_all_batches():
     for lens in ([1], [7], [250] * 8, [256] * 8 + [52], [255, 256, 256, 256]):
         d = Drafts(lens, vocab, sum(lens))
         d.check(d.run(5, ws=ws), 5)
+
+
+def test_all_calls_from_several_threads():
+    """Each thread's attention and verification, 40 times, against what the same
+    calls give alone; a worker's exception is the test's."""
+    from concurrent.futures import ThreadPoolExecutor
+    cases = [Case(8, 2, 128, 16, [(3000, 20), (40, 5)], 23), Case(4, 1, 64, 32, [(900, 70)], 24),
+             Case(32, 8, 128, 16, [(60 * i, 3) for i in range(30)], 25)]
+    work = []
+    for i, c in enumerate(cases):
+        d, g = Drafts([3, 9, 5 + i], 700 + i, i), c.gpu()
+        work.append((c, g, c.run(g), d, {k: x.clone() for k, x in d.run(4).items()}))
+    torch.cuda.synchronize()
+
+    def loop(c, g, attended, d, verified):
+        s, ends = torch.cuda.Stream(), 0
+        logits, tok, par = (torch.as_tensor(x).to(DEV) for x in (bf16(d.logits), d.tokens, d.parents))
+        torch.cuda.synchronize()
+        for _ in range(40):
+            with torch.cuda.stream(s):
+                out = c.run(g, out=torch.empty_like(g["q"]))
+                got = {k: torch.empty_like(x) for k, x in verified.items()}
+                tree.verify(logits, tok, par, d.rows, **got)
+            s.synchronize()
+            assert torch.equal(out.view(torch.int16), attended.view(torch.int16))
+            assert all(torch.equal(got[k], x) for k, x in verified.items())
+            ends += 1
+        return ends
+
+    with ThreadPoolExecutor(len(work)) as pool:
+        assert [f.result(60) for f in [pool.submit(loop, *w) for w in work]] == [40] * len(work)
