@@ -7,9 +7,13 @@
 // it, above that the matrix cores.
 //
 // Softmax runs in base 2, over one pass of the keys, with a running maximum
-// that moves lazily (a score has to exceed it by 2^8) and fp32 sums of the
-// weights as they were rounded to bf16 for the product with V.  Masks cost
-// nothing until the keys of the tree itself, the last ones of a row.
+// that moves lazily (a score has to exceed it by 2^8).  The weights are rounded
+// to bf16, the type that the matrix cores want beside V; exact products would
+// need a second one with what the rounding leaves.  fp32 sums of the weights as
+// rounded keep the rows normalised: outputs are off by 0.0022 to 0.0023 in the
+// mean square against 0.0016 to 0.0017 of their own rounding, as in the mixed
+// step.  Masks cost nothing until the keys of the tree itself, the last ones of
+// a row.
 #include "tree_attn.hpp"
 
 #include "tree_device.hpp"

@@ -127,9 +127,9 @@ void plan_tree(const cp_attn_desc& desc, const cp_row_meta* rows, int32_t n_rows
   // Both kernels' best pieces, where there is a choice: a narrow workgroup
   // starts and ends sooner, a wide one takes four times the rows and reads K and
   // V for all of them.  us, narrow / wide, on 32/8 heads: one request of 128 rows
-  // after 250 keys 9.6 / 14.7, after 1,000 12.9 / 15.8; 8 of them 10.3 / 16.7
-  // and 29.0 / 22.8; 32 of them 32.5 / 18.3.  Of 234 such batches this takes the
-  // slower kernel, by 7 to 20 %, in 6.
+  // after 250 keys 8.4 / 14.0, after 1,000 12.0 / 15.7; 8 of them 10.3 / 14.0
+  // and 22.7 / 21.0; 32 of them 32.7 / 18.2 and 85.6 / 37.6.  Of 234 such batches
+  // the choice is more than 5 % behind the faster kernel in 5, by 6 to 14 %.
   thread_local Work work;
   const double d = desc.head_dim / 128.0;
   const double per_key = hkv * desc.head_dim * 4.0 / 5.3e6;
