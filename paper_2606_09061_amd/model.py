@@ -553,7 +553,9 @@ class Model:
                     or not t.is_contiguous()):
                 raise cp.CpError(cp.CP_ERR_INVALID_ARG, "verify: tokens and parents are dense "
                                  f"int32 [{T}] on {self.x.device}")
-        need = tree.attn_workspace_bytes(self.desc, rows) if T > 0 else 0   # (checks the rows)
+        # (both check what they are given, before anything runs)
+        need = tree.attn_workspace_bytes(self.desc, rows) if T > 0 else 0
+        pools = tree.kv_layers(self.desc, self.kc, self.vc)
         s = stream or torch.cuda.current_stream(self.dev)
         with torch.cuda.stream(s):
             i32 = dict(dtype=torch.int32, device=self.dev)
@@ -575,8 +577,7 @@ class Model:
                 project(h, self.lm_head, logits, None, s, self.ws_gemm)
             tree.verify(logits, tokens, parents, rows, target, path, n_accepted, after, stream=s)
             if T > 0:
-                tree.kv_compact(tree.kv_layers(self.desc, self.kc, self.vc), self.bt, rows, path,
-                                n_accepted, s)
+                tree.kv_compact(pools, self.bt, rows, path, n_accepted, s)
         return target, path, n_accepted, after
 
 

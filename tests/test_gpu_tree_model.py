@@ -223,3 +223,23 @@ def test_verify_refuses_before_anything_runs(which):
     torch.cuda.synchronize()
     assert (m.x == 2).all() and (m.pos == -7).all()
     assert all((x == 3).all() for x in m.kc + m.vc)
+
+
+@pytest.mark.parametrize("change", ["shared", "shape", "missing"])
+def test_verify_refuses_other_pools_before_anything_runs(change):
+    m = _model(1)
+    m.x.fill_(2)
+    for x in m.kc + m.vc:
+        x.fill_(3)
+    pools = m.kc + m.vc
+    if change == "shared":
+        m.kc[2] = m.kc[1]
+    elif change == "shape":
+        m.vc[2] = m.vc[2][:-1]
+    else:
+        m.kc = m.kc[:2]
+    t = torch.zeros(3, dtype=torch.int32, device=m.dev)
+    with pytest.raises(M.cp.CpError):
+        m.verify([(0, 0, 3, 3)], t, torch.tensor([-1, 0, 0], dtype=torch.int32, device=m.dev))
+    torch.cuda.synchronize()
+    assert (m.x == 2).all() and all((x == 3).all() for x in pools)
