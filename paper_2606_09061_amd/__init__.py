@@ -6,7 +6,8 @@ kernel, the split-K decode kernel and the merge pass.  ``binding`` is the
 ctypes layer over its C ABI (include/cp_attn.h), re-exported here; the
 scheduler (``sched``, ``lprs``, ``serve``) and the decoder layer around the
 step (``model``) sit on top of it, and ``tree`` (libcptree.so) holds
-speculative decoding and forks of requests over the same cache.
+speculative decoding and forks of requests over the same cache, ``cache``
+(libcpcache.so) the operators of long and shared contexts.
 """
 
 from .binding import (  # noqa: F401

@@ -1,7 +1,7 @@
 """Builds, in-tree, libcpattn.so (the attention step: HIP kernels + C ABI,
 gfx950, hipcc), libcplayer.so (the element-wise kernels of the decoder layer
 around it, gfx950), libcptree.so (drafted trees and forks over the cache, gfx950),
-libcppeaks.so (peak-rate microbenchmarks, gfx950) and libcpsched.so (the host
+libcpcache.so (long and shared contexts over the cache, gfx950), libcppeaks.so (peak-rate microbenchmarks, gfx950) and libcpsched.so (the host
 scheduler, plain C++17, g++)."""
 
 from __future__ import annotations
@@ -22,6 +22,9 @@ LAYER_SOURCES = ["layer.hip", "gemm.hip"]
 TREE_LIB = os.path.join(PKG, "libcptree.so")
 TREE_SOURCES = ["tree_api.hip", "tree_plan.cpp", "tree_attn.hip", "tree_wide64.hip",
                 "tree_wide128.hip", "tree_ops.hip"]
+CACHE_LIB = os.path.join(PKG, "libcpcache.so")
+CACHE_SOURCES = ["cache_api.hip", "cache_plan.cpp", "cache_append.hip", "cache_select.hip",
+                 "cache_attn.hip"]
 PEAKS_LIB = os.path.join(PKG, "libcppeaks.so")
 PEAKS_SOURCES = ["peaks.hip"]
 CXX = os.environ.get("CXX", "g++")
@@ -50,14 +53,18 @@ def _compile(src: str) -> str:
 def build(jobs: int = 8) -> str:
     os.makedirs(BUILD, exist_ok=True)
     with cf.ThreadPoolExecutor(max_workers=jobs) as ex:
-        objs = list(ex.map(_compile, SOURCES + LAYER_SOURCES + TREE_SOURCES + PEAKS_SOURCES))
+        objs = list(ex.map(_compile, SOURCES + LAYER_SOURCES + TREE_SOURCES + CACHE_SOURCES
+                           + PEAKS_SOURCES))
     n1, n2 = len(SOURCES), len(SOURCES) + len(LAYER_SOURCES)
     n3 = n2 + len(TREE_SOURCES)
+    n4 = n3 + len(CACHE_SOURCES)
     _link(objs[:n1], LIB)
     _link(objs[n1:n2], LAYER_LIB)
     # the rows' checks are the attention library's own, linked in
-    _link(objs[n2:n3] + [objs[SOURCES.index("plan.cpp")]], TREE_LIB)
-    _link(objs[n3:], PEAKS_LIB)
+    checks = [objs[SOURCES.index("plan.cpp")]]
+    _link(objs[n2:n3] + checks, TREE_LIB)
+    _link(objs[n3:n4] + checks, CACHE_LIB)
+    _link(objs[n4:], PEAKS_LIB)
     build_sched()
     return LIB
 

@@ -1,0 +1,75 @@
+// Structures of libcpcache (include/cp_cache.h).
+//
+// The rows of a call travel inside the kernel arguments (at most 4 KB), a batch
+// of them per launch: no call uploads anything, so every one can be captured
+// in a graph as it is.
+#pragma once
+
+#include <limits.h>
+#include <stddef.h>
+#include <stdint.h>
+
+#include "cp_cache.h"
+
+namespace cpcache {
+
+// Rows of a launch, N at most; few of them travel in a block of kFewRows.  The
+// places behind them begin at an item that no workgroup reaches.
+template <class T, int N>
+struct RowsOf {
+  T r[N];
+};
+constexpr int kFewRows = 8;
+
+struct AppendRow {   // 24 bytes: a piece of a row of cp_qkv_append
+  int32_t tok0;      // its first token
+  int32_t item0;     // the first of the launch's (page, some kv heads) items of V
+  int32_t n, req, start, first;  // `first`: tokens of the launch before it
+};
+constexpr int kAppendRows = 144;
+using AppendRows = RowsOf<AppendRow, kAppendRows>;
+
+struct BoundsRow {   // 16 bytes: a piece of a row of cp_page_bounds
+  int32_t item0;     // the launch's pages before it
+  int32_t req, page0, ctx;
+};
+constexpr int kBoundsRows = 224;
+using BoundsRows = RowsOf<BoundsRow, kBoundsRows>;
+
+struct SelectRow {   // 32 bytes: a piece of a row of cp_page_select
+  int32_t item0;     // the launch's workgroups before it
+  int32_t tok0, n, start, req;
+  int32_t stride;    // scores per (token, kv head); 0: every page is selected
+  int64_t score0;    // its first score in the workspace
+};
+constexpr int kSelectRows = 112;
+using SelectRows = RowsOf<SelectRow, kSelectRows>;
+
+struct AttnRow {     // 32 bytes: a piece of a row of cp_page_attn or cp_prefix_attn
+  int32_t item0;     // the launch's workgroups before it
+  int32_t tok0, n, start, req;
+  int32_t group;     // the launch's group, or -1
+  int32_t n_split;   // pieces of its key range
+  int32_t part0;     // its first partial row; unused when n_split is 1
+};
+constexpr int kAttnRows = 92;
+using AttnRows = RowsOf<AttnRow, kAttnRows>;
+
+struct GroupRef {    // 24 bytes: what the rows of a group need of it
+  int32_t keys;      // those read for the whole group, whole pages
+  int32_t part0, n_split, n_rows;  // its partial rows: [kv head][split][n_rows]
+  int32_t tok0;      // its first token
+  int32_t reserved;
+};
+constexpr int kGroups = 32;
+using GroupRefs = RowsOf<GroupRef, kGroups>;
+
+struct PrefixRow {   // 32 bytes: a group's common keys
+  int32_t item0;
+  int32_t tok0, n, req;
+  int32_t keys, n_split, split_keys, part0;
+};
+constexpr int kPrefixRows = 112;
+using PrefixRows = RowsOf<PrefixRow, kPrefixRows>;
+
+}  // namespace cpcache

@@ -1,0 +1,44 @@
+// How the attention calls of libcpcache are cut into workgroups (host side, no HIP).
+#pragma once
+
+#include <vector>
+
+#include "cache.hpp"
+
+namespace cpcache {
+
+// Bounds of include/cp_cache.h: they keep launches' grids and index types in range.
+constexpr int kMaxKvHeads = 1024;
+constexpr int64_t kMaxTokens = 1 << 23, kMaxPairs = 1 << 27;
+// Workgroups of a launch: 2^24 of 256 threads are what a grid takes.
+constexpr int64_t kMaxItems = (1 << 24) - 1;
+// Tokens and pages of a piece of a row: longer rows come as several.
+constexpr int kPieceTokens = 512, kPiecePages = 2048;
+
+// Keys that the four waves of an attention workgroup take in turn.
+constexpr int kTurn = 128;
+// Most pages of a piece of a page list (its workgroup holds them in LDS).
+constexpr int kListPages = 256;
+// Most pieces of a group's keys (the factors of their merge are in LDS).
+constexpr int kMaxGroupSplits = 128;
+
+// A group's (token, q head) rows per kv head that a workgroup takes.
+constexpr int kPrefixTile = 32;
+
+struct AttnPlan {
+  std::vector<AttnRow> rows;       // the tokens' own keys
+  std::vector<PrefixRow> prefix;   // of the groups that share something
+  std::vector<GroupRef> groups;    // the same groups, by AttnRow::group
+  int piece = 0;                   // keys, or entries of a list, of a piece of the rows' ranges
+  int64_t partial_rows = 0;
+  size_t off_lse = 0, ws_bytes = 256;  // partial rows of D fp32, then their log sums
+};
+
+// rows: valid for desc, within the limits of cp_cache.h.  Both return whether the
+// partial rows fit their index type.
+bool plan_pages(const cp_attn_desc& desc, const cp_row_meta* rows, int32_t n_rows, int32_t n_pages,
+                AttnPlan& out);
+bool plan_prefix(const cp_attn_desc& desc, const cp_row_meta* rows, int32_t n_rows,
+                 const cp_prefix_group* groups, int32_t n_groups, AttnPlan& out);
+
+}  // namespace cpcache

@@ -1,0 +1,693 @@
+"""Long and shared contexts on the GPU against the 64-bit oracle (oracle/cache.py)."""
+
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2606_09061_amd as cp
+from oracle import cache as ref
+from oracle import layer as layer_ref
+from paper_2606_09061_amd import cache
+from paper_2606_09061_amd import model as M
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+NAN = float("nan")
+THETA, EPS = 1e6, 1e-6
+
+
+def bf16(x):
+    return torch.from_numpy(np.asarray(x, np.float32)).to(torch.bfloat16)
+
+
+def f64(t):
+    return t.detach().cpu().double().numpy()
+
+
+class Case:
+    """Rows [(start, len)] over randomly placed pages; every slot that no row owns,
+    and every page that none names, holds NaN.  ``groups`` [(first row, rows,
+    common)]: the rows of a group name the same full pages."""
+
+    def __init__(self, hq, hkv, d, block, rows, seed, groups=(), pages_apart=False):
+        rng = self.rng = np.random.default_rng(seed)
+        self.hq, self.hkv, self.d, self.block = hq, hkv, d, block
+        self.groups = np.array(list(groups), np.int32).reshape(-1, 3)
+        n = len(rows)
+        slots = rng.permutation(n + 2)[:n]
+        self.rows = np.array([(s, a, c, a + c) for s, (a, c) in zip(slots, rows)],
+                             np.int32).reshape(-1, 4)
+        need = [-(-(a + c) // block) for a, c in rows]
+        nb = sum(need) + 3
+        perm = rng.permutation(nb).astype(np.int32)
+        self.table = np.full((n + 2, max(need + [1]) + 1), perm[-1], np.int32)
+        at = 0
+        for i in range(n):
+            self.table[slots[i], :need[i]] = perm[at:at + need[i]]
+            at += need[i]
+        for first, count, common in self.groups.tolist():
+            lead = [r for r in range(first, first + count) if rows[r][1] > 0][:1]
+            for r in range(first, first + count):
+                if lead and rows[r][1] > 0:
+                    self.table[slots[r], :common // block] = self.table[slots[lead[0]],
+                                                                         :common // block]
+        k = np.full((nb, hkv, block, d), NAN, np.float32)
+        v = np.full((nb, hkv, d, block), NAN, np.float32)
+        for slot, _, _, ctx in self.rows.tolist():
+            for p in range(-(-ctx // block)):
+                b, held = self.table[slot, p], min(block, ctx - p * block)
+                mean = rng.standard_normal((hkv, 1, d)) if pages_apart else 0.0
+                k[b, :, :held] = rng.standard_normal((hkv, held, d)) + mean
+                v[b, :, :, :held] = rng.standard_normal((hkv, d, held))
+        self.t = int(self.rows[:, 2].sum())
+        self.q = bf16(rng.standard_normal((self.t, hq, d)))
+        self.k, self.v = bf16(k), bf16(v)
+        self.scale = 1.0 / math.sqrt(d)
+
+    def desc(self):
+        return cp.make_desc(self.hq, self.hkv, self.d, self.block, self.k.shape[0],
+                            self.table.shape[1], self.table.shape[0], self.scale)
+
+    def gpu(self):
+        return dict(q=self.q.to(DEV), k=self.k.to(DEV), v=self.v.to(DEV),
+                    bt=torch.from_numpy(self.table).to(DEV))
+
+    def new_out(self):
+        return torch.full((self.t, self.hq, self.d), 7.0, dtype=torch.bfloat16, device=DEV)
+
+    def prefix(self, g=None, ws=None, out=None, stream=None):
+        g, out = g or self.gpu(), self.new_out() if out is None else out
+        cache.prefix_attn(self.desc(), g["q"], g["k"], g["v"], g["bt"], self.rows, self.groups, out,
+                          ws, stream)
+        return out
+
+    def listed(self, pages, g=None, ws=None, out=None, stream=None):
+        g, out = g or self.gpu(), self.new_out() if out is None else out
+        pages = pages if torch.is_tensor(pages) else torch.from_numpy(pages).to(DEV)
+        cache.page_attn(self.desc(), g["q"], g["k"], g["v"], g["bt"], pages, self.rows, out, ws,
+                        stream)
+        return out
+
+    def lists(self, n_pages):
+        """Random rising lists of up to n_pages pages for every token and kv head."""
+        out = np.full((self.t, self.hkv, n_pages), -1, np.int32)
+        for t, _, p in ref.tokens(self.rows.tolist()):
+            for h in range(self.hkv):
+                n = p // self.block + 1
+                take = np.sort(self.rng.choice(n, min(n, n_pages), replace=False))
+                if self.rng.random() < 0.7:
+                    take[-1] = n - 1
+                out[t, h, :len(take)] = take
+        return out
+
+    def check(self, out, what="", pages=None):
+        """|out - o| <= 2^-8 |o| (the output's rounding) + 2^-8 (1 + 2^-7) spread (the
+        weights', summed as rounded) + the fp32 part: a score is a sum of d
+        products whose sizes add up to at most top = |q| |k| scale, so it is off
+        by (d + 8) 2^-23 top with the factors' own roundings, which moves the
+        weights by as much, relatively; sums of ctx weighted values in fp32, and
+        the exponentials' and the merge's few ulps."""
+        o, spread, size = ref.attn(f64(self.q), f64(self.k), f64(self.v), self.table,
+                                   self.rows.tolist(), self.scale, pages)
+        got = f64(out)
+        fine = np.isfinite(o)
+        assert np.array_equal(np.isfinite(got), fine), what
+        assert np.array_equal(np.isnan(got), np.isnan(o)), what
+
+        def longest(x, axis):                       # of the finite vectors along axis
+            n = np.linalg.norm(x, axis=axis)
+            return n[np.isfinite(n)].max(initial=0)
+
+        top = longest(f64(self.q), -1) * longest(f64(self.k), -1) * self.scale
+        ctx = int(self.rows[:, 3].max(initial=0))
+        tol = (2.0 ** -8 * np.abs(o) + 2.0 ** -8 * (1 + 2.0 ** -7) * spread
+               + 2 * (self.d + 8) * 2.0 ** -23 * top * spread
+               + (2 * ctx + 64) * 2.0 ** -23 * size + 1e-30)
+        with np.errstate(invalid="ignore"):
+            ratio = np.where(fine, np.abs(got - o) / tol, 0)
+        worst = ratio.max(initial=0)
+        print(f"  {what}: worst error {worst:.3f} of the bound", flush=True)
+        assert worst <= 1, (what, worst, np.argwhere(ratio > 1)[:5])
+
+
+HEADS = [(1, 1), (4, 2), (8, 2), (8, 1), (5, 5), (16, 2), (12, 3)]
+
+
+# ---------------------------------------------------------------- rotation and append
+
+class Append:
+    def __init__(self, hq, hkv, d, block, rows, seed):
+        c = self.c = Case(hq, hkv, d, block, rows, seed)
+        self.qkv = bf16(c.rng.standard_normal((c.t, (hq + 2 * hkv) * d))).to(DEV)
+        self.qw, self.kw = (bf16(1 + 0.3 * c.rng.standard_normal(d)).to(DEV) for _ in range(2))
+        self.bt = torch.from_numpy(c.table).to(DEV)
+        self.pools = [torch.from_numpy(c.rng.integers(-32768, 32768, x.shape, dtype=np.int16))
+                      .to(DEV).view(torch.bfloat16) for x in (c.k, c.v)]
+
+    def run(self, positions=None, pools=None, stream=None):
+        """(q, k pool, v pool)"""
+        k, v = pools or [p.clone() for p in self.pools]
+        q = torch.full((self.c.t, self.c.hq, self.c.d), 7.0, dtype=torch.bfloat16, device=DEV)
+        cache.qkv_append(self.c.desc(), self.qkv, self.qw, self.kw, self.c.rows, q, k, v, self.bt,
+                         THETA, EPS, positions, stream)
+        return q, k, v
+
+    def two_calls(self, positions=None):
+        """The same by model.qkv_rope and kv_append."""
+        c = self.c
+        k, v = (p.clone() for p in self.pools)
+        q, kn, vn = (torch.empty(c.t, h, c.d, dtype=torch.bfloat16, device=DEV)
+                     for h in (c.hq, c.hkv, c.hkv))
+        if positions is None:
+            positions = torch.from_numpy(M.positions_of(c.rows)).to(DEV)
+        M.qkv_rope(self.qkv, self.qw, self.kw, positions, c.hq, c.hkv, c.d, THETA, EPS, q, kn, vn)
+        ws = torch.empty(max(256, cp.workspace_bytes(c.desc(), c.rows)), dtype=torch.uint8,
+                         device=DEV)
+        cp.kv_append(c.desc(), kn, vn, k, v, self.bt, c.rows, ws)
+        return q, k, v
+
+
+def same_bits(a, b):
+    return all(torch.equal(x.view(torch.int16), y.view(torch.int16)) for x, y in zip(a, b))
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("block", [16, 32])
+@pytest.mark.parametrize("hq,hkv", HEADS + [(32, 8), (64, 8)])
+def test_append_gives_the_bits_of_the_two_calls(hq, hkv, d, block):
+    rows = [(37, 5), (0, 1), (0, 70), (64, 17), (300, 1), (5, 0), (31, 1), (15, 33), (16, 16)]
+    a = Append(hq, hkv, d, block, rows, 100 * hq + hkv + d + block)
+    assert same_bits(a.run(), a.two_calls())
+
+
+@pytest.mark.parametrize("rows", [[(0, 1)], [(15, 1)], [(16, 1)], [(0, 2500)], [(1030, 1500), (3, 2)],
+                                  [(7 * i, 1) for i in range(8)], [(7 * i, 1) for i in range(9)],
+                                  [(7 * i, 1 + i % 3) for i in range(144)],
+                                  [(3 * i, 1 + i % 2) for i in range(300)]])
+def test_append_numbers_of_rows_and_tokens(rows):
+    a = Append(8, 2, 128, 16, rows, len(rows))
+    assert same_bits(a.run(), a.two_calls())
+
+
+def test_append_at_given_positions():
+    """Nodes of a tree: the slots follow the rows, the rotation `positions`."""
+    a = Append(8, 2, 64, 16, [(37, 9), (500, 4)], 5)
+    positions = torch.from_numpy(a.c.rng.integers(0, 1 << 20, a.c.t).astype(np.int32)).to(DEV)
+    assert same_bits(a.run(positions), a.two_calls(positions))
+
+
+def test_append_matches_the_oracle_at_far_positions():
+    """Roundings: the output's 2^-8; the fp32 part as model.qkv_rope's own test has it."""
+    hq, hkv, d = 4, 2, 128
+    a = Append(hq, hkv, d, 16, [(40, 3), (0, 2), (15, 20)], 6)
+    positions = torch.from_numpy(a.c.rng.integers(0, 1 << 20, a.c.t).astype(np.int32)).to(DEV)
+    q, k, v = a.run(positions)
+    want = layer_ref.qkv_rope(f64(a.qkv), f64(a.qw), f64(a.kw), positions.cpu().numpy(), hq, hkv, d,
+                              THETA, EPS)
+    assert (np.abs(f64(q) - want[0]) <= 2.0 ** -8 * np.abs(want[0]) + 1e-4).all()
+    kk, vv = (np.nan_to_num(f64(p), nan=3.0, posinf=4.0, neginf=5.0) for p in a.pools)
+    wk, wv = ref.append(kk, vv, want[1], want[2], a.c.table, a.c.rows.tolist())
+    gk, gv = (np.nan_to_num(f64(p), nan=3.0, posinf=4.0, neginf=5.0) for p in (k, v))
+    assert np.array_equal(gv, wv)
+    new = wk != kk
+    assert new.any() and np.array_equal(gk[~new], kk[~new])
+    assert (np.abs(gk - wk)[new] <= 2.0 ** -8 * np.abs(wk[new]) + 1e-4).all()
+
+
+def test_append_leaves_out_slots_of_bad_pages():
+    a = Append(4, 2, 64, 16, [(10, 40), (0, 3), (100, 1)], 7)
+    want = list(a.run())
+    for r, p, bad in ((0, 1, -1), (1, 0, a.c.k.shape[0]), (2, 6, 1 << 30)):
+        b, slot = a.c.table[a.c.rows[r, 0], p], int(a.c.rows[r, 0])
+        for i in (1, 2):
+            want[i][b] = a.pools[i - 1][b]
+        a.bt[slot, p] = bad
+    assert same_bits(a.run(), want)
+
+
+def test_append_in_a_graph_and_on_two_streams():
+    a, b = Append(8, 2, 128, 16, [(37, 5), (64, 17)], 8), Append(4, 1, 64, 32, [(9, 70)], 9)
+    pools = [p.clone() for p in a.pools]
+    a.run(pools=[p.clone() for p in a.pools])
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        q, _, _ = a.run(pools=pools)
+    side = torch.cuda.Stream()
+    for i in range(3):
+        a.qkv.copy_(bf16(a.c.rng.standard_normal(a.qkv.shape)))
+        for p, old in zip(pools, a.pools):
+            p.copy_(old)
+        theirs = [p.clone() for p in b.pools]
+        torch.cuda.synchronize()
+        graph.replay()
+        with torch.cuda.stream(side):
+            other = b.run(pools=theirs)
+        torch.cuda.synchronize()
+        assert same_bits((q, *pools), a.two_calls()), i
+        assert same_bits(other, b.two_calls()), i
+
+
+# ---------------------------------------------------------------- bounds
+
+def run_bounds(c, g, old):
+    out = old.clone()
+    cache.page_bounds(c.desc(), g["k"], g["bt"], c.rows, out)
+    return out
+
+
+def check_bounds(c, g, old):
+    out = run_bounds(c, g, old)
+    want = ref.bounds(f64(c.k), c.table, c.rows.tolist(), f64(old))
+    assert np.array_equal(f64(out), want)
+    return out
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("block", [16, 32])
+@pytest.mark.parametrize("hkv", [1, 2, 3, 8])
+def test_bounds_match_the_oracle(hkv, d, block):
+    rows = [(37, 5), (0, 1), (0, 70), (64, 17), (300, 1), (5, 0), (31, 1), (15, 33), (16, 16), (0, 16)]
+    c = Case(hkv, hkv, d, block, rows, hkv + d + block)
+    old = torch.full((c.k.shape[0], hkv, 2, d), 9.0, dtype=torch.bfloat16, device=DEV)
+    check_bounds(c, c.gpu(), old)
+
+
+def test_bounds_of_infinities_and_nan_span_all_finite_values():
+    c = Case(2, 2, 64, 16, [(3, 40), (0, 20)], 3)
+    for i, x in enumerate([NAN, math.inf, -math.inf]):
+        c.k[c.table[c.rows[0, 0], i % 2], i % 2, i + 1, 5 * i] = x
+    old = torch.zeros(c.k.shape[0], 2, 2, 64, dtype=torch.bfloat16, device=DEV)
+    out = check_bounds(c, c.gpu(), old)
+    assert (out.float().abs() > 3.3e38).sum() == 6 and torch.isfinite(out.float()).all()
+
+
+@pytest.mark.parametrize("n", [8, 9, 224, 225, 400])
+def test_bounds_of_many_rows_and_bad_pages(n):
+    c = Case(1, 1, 64, 16, [(5 * i, 1 + i % 30) for i in range(n)], n)
+    for r in range(0, n, 7):
+        c.table[c.rows[r, 0], c.rows[r, 1] // 16] = [-1, c.k.shape[0], 1 << 30][r % 3]
+    old = torch.zeros(c.k.shape[0], 1, 2, 64, dtype=torch.bfloat16, device=DEV)
+    check_bounds(c, c.gpu(), old)
+
+
+def test_bounds_of_a_long_prompt():
+    c = Case(1, 1, 64, 16, [(9, 40000)], 4)       # more pages than a piece
+    old = torch.zeros(c.k.shape[0], 1, 2, 64, dtype=torch.bfloat16, device=DEV)
+    check_bounds(c, c.gpu(), old)
+
+
+# ---------------------------------------------------------------- selection
+
+class Select:
+    """Bounds made of the pools' keys; a case of its own for selection."""
+
+    def __init__(self, hq, hkv, d, block, rows, seed, pool=None):
+        rng = self.rng = np.random.default_rng(seed)
+        self.hq, self.hkv, self.d, self.block = hq, hkv, d, block
+        n = len(rows)
+        self.rows = np.array([(r, a, c, a + c) for r, (a, c) in enumerate(rows)], np.int32)
+        width = max(1, -(-int(self.rows[:, 3].max()) // block))
+        nb = pool or n * width
+        self.table = (rng.integers(0, nb, (n, width)) if pool
+                      else rng.permutation(nb).reshape(n, width)).astype(np.int32)
+        mid = rng.standard_normal((nb, hkv, 1, d))
+        half = np.abs(rng.standard_normal((nb, hkv, 1, d))) + 0.5
+        self.bounds = bf16(np.concatenate([mid - half, mid + half], 2))
+        self.t = int(self.rows[:, 2].sum())
+        self.q = bf16(rng.standard_normal((self.t, hq, d)))
+
+    def desc(self):
+        return cp.make_desc(self.hq, self.hkv, self.d, self.block, self.bounds.shape[0],
+                            self.table.shape[1], self.table.shape[0], 0.1)
+
+    def gpu(self):
+        return (self.q.to(DEV), self.bounds.to(DEV), torch.from_numpy(self.table).to(DEV))
+
+    def run(self, n_pages, n_first=1, n_last=1, ws=None, g=None, out=None, stream=None):
+        q, b, bt = g or self.gpu()
+        if out is None:
+            out = torch.full((self.t, self.hkv, n_pages), 77, dtype=torch.int32, device=DEV)
+        cache.page_select(self.desc(), q, b, bt, self.rows, out, n_first, n_last, ws, stream)
+        return out
+
+    def want(self, n_pages, n_first=1, n_last=1):
+        return ref.select(f64(self.q), f64(self.bounds), self.table, self.rows.tolist(), self.block,
+                          n_pages, n_first, n_last)
+
+    def check(self, n_pages, n_first=1, n_last=1, **kw):
+        got = self.run(n_pages, n_first, n_last, **kw).cpu().numpy()
+        want = self.want(n_pages, n_first, n_last)
+        assert np.array_equal(got, want), np.argwhere((got != want).any(-1))[:5]
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("block", [16, 32])
+@pytest.mark.parametrize("hq,hkv", HEADS)
+def test_select_matches_the_oracle(hq, hkv, d, block):
+    rows = [(400, 3), (0, 1), (0, 5), (1023, 2), (160, 1), (5, 0), (159, 1)]
+    Select(hq, hkv, d, block, rows, 100 * hq + hkv + d + block).check(9)
+
+
+@pytest.mark.parametrize("n_pages,n_first,n_last", [(1, 0, 0), (1, 1, 0), (1, 0, 1), (2, 1, 1),
+                                                    (7, 0, 0), (20, 3, 17), (40, 5, 2), (63, 0, 1),
+                                                    (64, 1, 1), (65, 0, 0), (300, 100, 200)])
+def test_select_budgets(n_pages, n_first, n_last):
+    s = Select(8, 2, 64, 16, [(1022, 4), (300, 1), (1007, 1)], n_pages + n_first)
+    s.check(n_pages, n_first, n_last)
+
+
+@pytest.mark.parametrize("ctx,n_pages", [(255 * 16, 20), (256 * 16, 256), (257 * 16, 255),
+                                         (513 * 16 + 1, 100), (40000, 300), (70000, 4096)])
+def test_select_of_long_contexts_with_equal_scores(ctx, n_pages):
+    """Few different pages: most scores are shared, and the lower pages win."""
+    s = Select(4, 1, 64, 16, [(ctx - 1, 1)], ctx, pool=40)
+    s.check(n_pages)
+    s = Select(4, 1, 64, 16, [(ctx - 1, 1)], ctx, pool=1)   # all equal
+    s.check(n_pages, 0, 0)
+
+
+def test_select_scores_a_hair_apart():
+    """Scores that 32 bits cannot tell apart: 2^24 and the sums of it and 1, 2, ..."""
+    s = Select(1, 1, 64, 16, [(16 * 50 - 1, 1)], 3)
+    s.q[:] = 1
+    b = np.zeros((s.bounds.shape[0], 1, 2, 64))
+    b[..., 0] = 2.0 ** 24
+    order = s.rng.permutation(s.bounds.shape[0])
+    b[:, 0, :, 1] = (order % 128)[:, None]
+    s.bounds = bf16(b)
+    s.check(10, 0, 0)
+
+
+def test_select_takes_pages_of_bad_entries_last():
+    s = Select(4, 2, 64, 16, [(16 * 40, 1), (100, 1)], 4)
+    for i, bad in enumerate([-1, s.bounds.shape[0], 1 << 30, -7]):
+        s.table[0, 3 + 5 * i] = bad
+    s.check(36)
+    s.check(40, 0, 0)
+
+
+def test_select_of_a_q_that_is_not_finite_is_a_valid_list():
+    s = Select(4, 2, 64, 16, [(16 * 40, 2)], 5)
+    s.q[0, 0, 3], s.q[1, 2, 5] = NAN, math.inf
+    got = s.run(9).cpu().numpy()
+    for t in range(2):
+        for h in range(2):
+            assert (np.diff(got[t, h]) > 0).all() and got[t, h, 0] == 0 and got[t, h, -1] == 40
+
+
+@pytest.mark.parametrize("n", [8, 9, 112, 113, 250])
+def test_select_numbers_of_rows(n):
+    Select(2, 1, 64, 16, [(int(90 + 7 * i), 1) for i in range(n)], n).check(5)
+
+
+def test_select_repeats_and_reads_no_stale_workspace():
+    s = Select(8, 2, 128, 16, [(5000, 2), (40, 1), (900, 1)], 6)
+    need, g = cache.page_select_workspace_bytes(s.desc(), s.rows, 20), s.gpu()
+    for fill in (0, 255, 127):
+        ws = torch.full((need + 512,), fill, dtype=torch.uint8, device=DEV)
+        s.check(20, ws=ws[:need], g=g)
+        assert (ws[need:] == fill).all()
+
+
+# ---------------------------------------------------------------- attention over pages
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("block", [16, 32])
+@pytest.mark.parametrize("hq,hkv", HEADS)
+def test_page_attn_matches_the_oracle(hq, hkv, d, block):
+    rows = [(400, 3), (0, 1), (0, 5), (1023, 2), (160, 1), (5, 0), (159, 1)]
+    c = Case(hq, hkv, d, block, rows, 100 * hq + hkv + d + block)
+    pages = c.lists(9)
+    c.check(c.listed(pages), f"{hq}/{hkv} d {d} block {block}", pages)
+
+
+@pytest.mark.parametrize("n_pages", [1, 2, 3, 7, 8, 9, 64, 255, 256, 257, 600])
+def test_page_attn_lengths_of_lists(n_pages):
+    c = Case(4, 1, 128, 16, [(9999, 1), (2000, 1), (40, 2)], n_pages)
+    pages = c.lists(n_pages)
+    c.check(c.listed(pages), f"{n_pages} pages", pages)
+
+
+def test_page_attn_ends_lists_at_entries_that_do_not_count():
+    c = Case(8, 2, 64, 16, [(700, 6), (0, 3)], 3)
+    pages = c.lists(20)
+    pages[0, 0, 5] = -1
+    pages[0, 1, 4] = pages[0, 1, 3]          # does not rise
+    pages[1, 0, 7] = 10 ** 6
+    pages[1, 1, 0] = -3
+    pages[2, 0, 0] = 1 << 30
+    pages[2, 1, 6] = -(1 << 31)
+    pages[2, 1, 7] = -5                      # rises from the one before, and is none
+    pages[3, 0, 2:5] = [9, 8, 7]
+    pages[4, 0] = -1
+    pages[7, 0, 0] = 1                       # past the token's own page
+    out = c.listed(pages)
+    c.check(out, "broken lists", pages)
+    for t, h in ((1, 1), (2, 0), (4, 0), (7, 0)):
+        assert (out[t, 4 * h:4 * h + 4] == 0).all()
+
+
+def test_page_attn_reads_listed_pages_only():
+    """NaN in pages that are not listed changes nothing; in those that are, it shows."""
+    c = Case(4, 2, 128, 16, [(800, 2)], 4)
+    pages = c.lists(12)
+    named = set(pages[:, :, :].reshape(-1).tolist())
+    for p in range(51):
+        if p not in named:
+            c.k[c.table[c.rows[0, 0], p]] = NAN
+            c.v[c.table[c.rows[0, 0], p]] = NAN
+    c.check(c.listed(pages), "unlisted NaN", pages)
+    c.v[c.table[c.rows[0, 0], pages[0, 1, 2]], 1, 5] = NAN
+    out = c.listed(pages)
+    assert torch.isnan(out[0, 2:, 5]).all() and not torch.isnan(out[0, :2]).any()
+
+
+@pytest.mark.parametrize("lens", [[1] * 8, [1] * 9, [1] * 92, [2, 0] * 50, [1] * 200])
+def test_page_attn_numbers_of_rows(lens):
+    c = Case(4, 2, 64, 16, [(11 * i, n) for i, n in enumerate(lens)], len(lens))
+    pages = c.lists(6)
+    c.check(c.listed(pages), f"{len(lens)} rows", pages)
+
+
+def test_page_attn_of_a_long_chunk():
+    """More tokens than a piece of a row, uncut lists."""
+    c = Case(1, 1, 64, 16, [(100, 1500)], 5)
+    pages = c.lists(4)
+    c.check(c.listed(pages), "1,500 tokens", pages)
+
+
+# ---------------------------------------------------------------- common prefixes
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("block", [16, 32])
+@pytest.mark.parametrize("hq,hkv", HEADS)
+def test_prefix_attn_matches_the_oracle(hq, hkv, d, block):
+    rows = [(100, 1), (130, 2), (96, 1), (70, 3), (5, 0), (300, 1), (200, 1), (0, 1), (900, 4)]
+    c = Case(hq, hkv, d, block, rows, 100 * hq + hkv + d + block,
+             groups=[(0, 3, 96), (4, 3, 165)])
+    c.check(c.prefix(), f"{hq}/{hkv} d {d} block {block}")
+
+
+@pytest.mark.parametrize("common", [0, 1, 15, 16, 17, 31, 32, 33, 64, 127, 128, 129, 1000, 5000])
+@pytest.mark.parametrize("n", [1, 2, 9])
+def test_prefix_attn_lengths(common, n):
+    rows = [(common + 3 * i, 1 + i % 2) for i in range(n)]
+    c = Case(8, 2, 128, 16, rows, common + n, groups=[(0, n, common)])
+    c.check(c.prefix(), f"{common} tokens in common, {n} rows")
+
+
+@pytest.mark.parametrize("n", [3, 4, 5, 7, 8, 9, 31, 33, 64, 65, 100])
+@pytest.mark.parametrize("hq,hkv,d,block", [(4, 1, 128, 16), (8, 1, 64, 32), (2, 2, 128, 32)])
+def test_prefix_attn_sizes_of_groups(n, hq, hkv, d, block):
+    rows = [(200 + 5 * (i % 7), 1) for i in range(n)] + [(50, 1)]
+    c = Case(hq, hkv, d, block, rows, n, groups=[(0, n, 200)])
+    c.check(c.prefix(), f"{n} rows of a group")
+
+
+@pytest.mark.parametrize("hq,hkv,d,block", [(4, 1, 128, 16), (8, 1, 128, 32), (1, 1, 64, 16)])
+def test_prefix_attn_of_long_prefixes_and_long_tails(hq, hkv, d, block):
+    rows = [(20000, 1), (20007, 2), (26000, 1), (12000, 1)]
+    c = Case(hq, hkv, d, block, rows, d + block, groups=[(0, 3, 20000)])
+    c.check(c.prefix(), "20,000 tokens in common")
+
+
+def test_prefix_attn_of_many_rows_and_groups():
+    rows, groups = [], []
+    for g in range(70):
+        n = 1 + g % 4
+        if g % 5:
+            groups.append((len(rows), n, 16 * (g % 9)))
+        rows += [(16 * (g % 9) + i, (g + i) % 3) for i in range(n)]
+    c = Case(4, 2, 64, 16, rows, 6, groups=groups)
+    c.check(c.prefix(), f"{len(rows)} rows, {len(groups)} groups")
+
+
+@pytest.mark.parametrize("n", [8, 9, 92, 93, 112, 113, 200])
+def test_prefix_attn_numbers_of_rows(n):
+    c = Case(2, 1, 64, 16, [(20 + i, 1) for i in range(n)], n, groups=[(n // 3, n // 2, 20)])
+    c.check(c.prefix(), f"{n} rows")
+    c = Case(2, 1, 64, 16, [(20 + i, 1) for i in range(n)], n, groups=[(i, 1, 20) for i in range(n)])
+    c.check(c.prefix(), f"{n} groups")
+
+
+def test_prefix_attn_without_groups():
+    c = Case(8, 2, 128, 16, [(500, 1), (0, 3), (70, 20)], 7)
+    c.check(c.prefix(), "no groups")
+
+
+def test_prefix_attn_what_a_token_does_not_see_does_not_touch_it():
+    """NaN in a later token's key and value, and in another row's own pages."""
+    c = Case(8, 2, 128, 16, [(100, 5), (110, 1)], 8, groups=[(0, 2, 100)])
+    b = c.table[c.rows[0, 0], 103 // 16]
+    c.k[b, 0, 103 % 16, 3], c.v[b, 1, 4, 103 % 16] = NAN, NAN
+    c.check(c.prefix(), "poisoned token")
+    assert not torch.isnan(c.prefix()[:3]).any()
+
+
+@pytest.mark.parametrize("scale", [30.0, 1e-3, 1000.0])
+def test_attn_large_scores(scale):
+    """Scores far apart: the running maximum moves, most weights vanish."""
+    c = Case(8, 2, 64, 16, [(500, 2), (530, 1)], 9, groups=[(0, 2, 500)])
+    c.scale = scale / 8
+    c.check(c.prefix(), f"scale {scale}")
+    pages = c.lists(20)
+    c.check(c.listed(pages), f"scale {scale}, pages", pages)
+
+
+def test_attn_repeats_bit_for_bit_and_reads_no_stale_workspace():
+    c = Case(8, 2, 128, 16, [(3000, 1), (3005, 2), (900, 1)], 10, groups=[(0, 2, 2990)])
+    g, pages = c.gpu(), torch.from_numpy(c.lists(60)).to(DEV)
+    needs = (cache.prefix_attn_workspace_bytes(c.desc(), c.rows, c.groups),
+             cache.page_attn_workspace_bytes(c.desc(), c.rows, 60))
+    first = [None, None]
+    for fill in (0, 255, 127):
+        for i, call in enumerate((c.prefix, lambda **kw: c.listed(pages, **kw))):
+            ws = torch.full((needs[i] + 512,), fill, dtype=torch.uint8, device=DEV)
+            big = torch.full((c.t + 4, 8, 128), 5.0, dtype=torch.bfloat16, device=DEV)
+            call(g=g, ws=ws[:needs[i]], out=big[2:2 + c.t])
+            assert (ws[needs[i]:] == fill).all() and (big[:2] == 5).all() and (big[2 + c.t:] == 5).all()
+            out = big[2:2 + c.t].view(torch.int16).clone()
+            first[i] = out if first[i] is None else first[i]
+            assert torch.equal(out, first[i])
+
+
+def test_calls_in_graphs_streams_and_threads():
+    """Captured once and replayed on new contents, beside the same calls of other
+    threads on streams of their own."""
+    from concurrent.futures import ThreadPoolExecutor
+    c = Case(8, 2, 128, 16, [(300, 1), (310, 1), (40, 2)], 11, groups=[(0, 2, 300)])
+    s = Select(8, 2, 128, 16, [(2000, 1), (300, 2)], 12)
+    g, sg, pages = c.gpu(), s.gpu(), torch.from_numpy(c.lists(7)).to(DEV)
+    out = [c.new_out(), c.new_out(), torch.zeros(3, 2, 9, dtype=torch.int32, device=DEV)]
+    ws = [torch.empty(1 << 22, dtype=torch.uint8, device=DEV) for _ in range(3)]
+
+    def all_three(out, ws):
+        c.prefix(g, ws[0], out[0])
+        c.listed(pages, g, ws[1], out[1])
+        s.run(9, ws=ws[2], g=sg, out=out[2])
+
+    all_three(out, ws)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        all_three(out, ws)
+    for i in range(3):
+        c.q = bf16(c.rng.standard_normal(c.q.shape))
+        s.q = bf16(s.rng.standard_normal(s.q.shape))
+        g["q"].copy_(c.q)
+        sg[0].copy_(s.q)
+        for x in out:
+            x.fill_(5)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        c.check(out[0], "replayed prefix")
+        c.check(out[1], "replayed pages", pages.cpu().numpy())
+        assert np.array_equal(out[2].cpu().numpy(), s.want(9))
+
+    def loop():
+        mine, ends = [torch.empty_like(x) for x in out], 0
+        side = torch.cuda.Stream()
+        with torch.cuda.stream(side):
+            for _ in range(20):
+                c.prefix(g, None, mine[0])
+                c.listed(pages, g, None, mine[1])
+                s.run(9, g=sg, out=mine[2])
+                side.synchronize()
+                assert all(torch.equal(a, b) for a, b in zip(mine, out))
+                ends += 1
+        return ends
+
+    with ThreadPoolExecutor(3) as pool:
+        assert [f.result(60) for f in [pool.submit(loop) for _ in range(3)]] == [20] * 3
+
+
+def test_debug_mode_finds_bad_entries(monkeypatch):
+    monkeypatch.setenv("CP_DEBUG", "1")
+    c = Case(4, 2, 64, 16, [(100, 1), (120, 2)], 13, groups=[(0, 2, 90)])
+    c.check(c.prefix(), "debug")
+    pages = c.lists(4)
+    c.check(c.listed(pages), "debug pages", pages)
+    a = Append(4, 2, 64, 16, [(10, 40)], 14)
+    assert same_bits(a.run(), a.two_calls())
+    keep = c.table.copy()
+    c.table[c.rows[1, 0], 2] = c.table[c.rows[1, 0], 6]      # a shared page that is not
+    with pytest.raises(cp.CpError) as e:
+        c.prefix()
+    assert e.value.code == cp.binding.CP_ERR_BAD_META
+    c.table = keep
+    c.table[c.rows[1, 0], 7] = -1
+    for call in (c.prefix, lambda: c.listed(pages)):
+        with pytest.raises(cp.CpError) as e:
+            call()
+        assert e.value.code == cp.binding.CP_ERR_BAD_META
+
+
+# ---------------------------------------------------------------- a round of them together
+
+def test_a_sparse_decode_round():
+    """A prompt is appended, its bounds taken; then each token: append, bounds of
+    its page, selection and attention over the selected pages."""
+    hq, hkv, d, block, budget = 8, 2, 128, 16, 6
+    rows = [(0, 400), (0, 95)]
+    a = Append(hq, hkv, d, block, rows, 15)
+    c = a.c
+    table = np.concatenate([c.table, np.full((len(c.table), 2), 0, np.int32)], 1)
+    desc = cp.make_desc(hq, hkv, d, block, c.k.shape[0], table.shape[1], len(table), c.scale)
+    bt = torch.from_numpy(table).to(DEV)
+    k = torch.full(c.k.shape, NAN, dtype=torch.bfloat16, device=DEV)
+    v = torch.full(c.v.shape, NAN, dtype=torch.bfloat16, device=DEV)
+    bounds = torch.full((k.shape[0], hkv, 2, d), NAN, dtype=torch.bfloat16, device=DEV)
+    free = [b for b in range(k.shape[0]) if b not in set(c.table[c.rows[:, 0]].reshape(-1))]
+    slots = c.rows[:, 0].tolist()
+    bt[slots[0], 25] = free[0]                   # 400 tokens fill 25 pages
+    table[slots[0], 25] = free[0]
+    batch = np.array([(slots[0], 0, 400, 400), (slots[1], 0, 95, 95)], np.int32)
+    q = torch.empty(495, hq, d, dtype=torch.bfloat16, device=DEV)
+    cache.qkv_append(desc, a.qkv, a.qw, a.kw, batch, q, k, v, bt, THETA, EPS)
+    cache.page_bounds(desc, k, bt, batch, bounds)
+    for step in range(3):
+        batch = np.array([(slots[0], 400 + step, 1, 401 + step), (slots[1], 95 + step, 1, 96 + step)],
+                         np.int32)
+        if step == 1:                            # token 96 begins a page
+            bt[slots[1], 6] = free[1]
+            table[slots[1], 6] = free[1]
+        qkv = bf16(c.rng.standard_normal((2, (hq + 2 * hkv) * d))).to(DEV)
+        q = torch.empty(2, hq, d, dtype=torch.bfloat16, device=DEV)
+        pages = torch.empty(2, hkv, budget, dtype=torch.int32, device=DEV)
+        out = torch.empty(2, hq, d, dtype=torch.bfloat16, device=DEV)
+        cache.qkv_append(desc, qkv, a.qw, a.kw, batch, q, k, v, bt, THETA, EPS)
+        cache.page_bounds(desc, k, bt, batch, bounds)
+        cache.page_select(desc, q, bounds, bt, batch, pages)
+        cache.page_attn(desc, q, k, v, bt, pages, batch, out)
+        kk = f64(k)
+        whole = np.array([(s, 0, n, n) for s, n in zip(slots, batch[:, 3])])
+        want = ref.bounds(kk, table, whole, np.full((k.shape[0], hkv, 2, d), NAN))
+        assert np.array_equal(f64(bounds), want, equal_nan=True)
+        chosen = ref.select(f64(q), want, table, batch.tolist(), block, budget, 1, 1)
+        assert np.array_equal(pages.cpu().numpy(), chosen)
+        c.q, c.k, c.v, c.table, c.rows = q.cpu(), k.cpu(), v.cpu(), table, batch
+        c.check(out, f"step {step}", chosen)
