@@ -24,7 +24,7 @@ TREE_SOURCES = ["tree_api.hip", "tree_plan.cpp", "tree_attn.hip", "tree_wide64.h
                 "tree_wide128.hip", "tree_ops.hip"]
 CACHE_LIB = os.path.join(PKG, "libcpcache.so")
 CACHE_SOURCES = ["cache_api.hip", "cache_plan.cpp", "cache_append.hip", "cache_select.hip",
-                 "cache_attn.hip"]
+                 "cache_attn.hip", "cache_wide64.hip", "cache_wide128.hip"]
 PEAKS_LIB = os.path.join(PKG, "libcppeaks.so")
 PEAKS_SOURCES = ["peaks.hip"]
 CXX = os.environ.get("CXX", "g++")

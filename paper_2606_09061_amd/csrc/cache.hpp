@@ -45,23 +45,25 @@ struct SelectRow {   // 32 bytes: a piece of a row of cp_page_select
 constexpr int kSelectRows = 112;
 using SelectRows = RowsOf<SelectRow, kSelectRows>;
 
-struct AttnRow {     // 32 bytes: a piece of a row of cp_page_attn or cp_prefix_attn
+// A piece of a row of cp_page_attn or cp_prefix_attn.  A launch's rows follow each
+// other: the next one's first token and item end a row, and the place behind the
+// last row holds the launch's ends.  With `own` keys (or entries of a list) of its
+// last token, a row has ceil(own / piece) pieces, and the partial rows of its
+// workgroup x are (item0 + x) G and on, behind those of the launches before.
+struct AttnRow {     // 16 bytes
   int32_t item0;     // the launch's workgroups before it
-  int32_t tok0, n, start, req;
-  int32_t group;     // the launch's group, or -1
-  int32_t n_split;   // pieces of its key range
-  int32_t part0;     // its first partial row; unused when n_split is 1
+  int32_t tok0, start, req;
 };
-constexpr int kAttnRows = 92;
-using AttnRows = RowsOf<AttnRow, kAttnRows>;
+constexpr int kAttnRows = 160;
+using AttnRows = RowsOf<AttnRow, kAttnRows + 1>;
 
-struct GroupRef {    // 24 bytes: what the rows of a group need of it
+struct GroupRef {    // 28 bytes: what the rows of a group need of it
+  int32_t row0, row1;  // the launch's rows that it holds
   int32_t keys;      // those read for the whole group, whole pages
   int32_t part0, n_split, n_rows;  // its partial rows: [kv head][split][n_rows]
   int32_t tok0;      // its first token
-  int32_t reserved;
 };
-constexpr int kGroups = 32;
+constexpr int kGroups = 36;
 using GroupRefs = RowsOf<GroupRef, kGroups>;
 
 struct PrefixRow {   // 32 bytes: a group's common keys

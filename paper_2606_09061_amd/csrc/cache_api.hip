@@ -200,62 +200,46 @@ AttnArgs attn_args(const cp_attn_desc* d, const AttnPlan& p, const void* q, cons
                   __builtin_ctz(d->num_q_heads / d->num_kv_heads),
                   n_pages,
                   p.piece,
+                  0,
+                  0,
                   d->sm_scale * cpattn::kLog2e};
 }
 
-// The groups that a launch's rows name, and the rows with the launch's indexes of
-// them; fails where there are too many.
-bool local_groups(const AttnPlan& p, AttnRows& rows, int n, GroupRefs& out) {
-  int32_t first = -1, last = -1;
-  for (int i = 0; i < n; ++i)
-    if (rows.r[i].group >= 0) {
-      if (first < 0) first = rows.r[i].group;
-      last = rows.r[i].group;
+// The launches over the tokens' rows, each with the merge of its rows that are split.
+int launch_rows(const cp_attn_desc* d, const AttnPlan& p, AttnArgs a, hipStream_t s) {
+  const int hkv = d->num_kv_heads, G = d->num_q_heads / hkv;
+  int64_t part0 = p.row_part0;
+  for (size_t r = 0; r < p.rows.size();) {
+    AttnRows batch;
+    GroupRefs groups{};
+    int64_t items = 0;
+    int n = 0, n_groups = 0, last = -1;
+    bool split = false;
+    const size_t first = r;
+    for (; r < p.rows.size() && n < kAttnRows; ++r) {
+      const TokenRow& t = p.rows[r];
+      const int64_t more = (int64_t)t.n_split * t.n * hkv;
+      if (n > 0 && items + more > kMaxItems) break;
+      if (t.group >= 0 && t.group != last) {
+        if (n_groups == kGroups) break;
+        const PrefixRow& g = p.prefix[t.group];
+        groups.r[n_groups++] = GroupRef{n, n, g.keys, g.part0, g.n_split, g.n * G, g.tok0};
+        last = t.group;
+      }
+      if (t.group >= 0) groups.r[n_groups - 1].row1 = n + 1;
+      batch.r[n++] = AttnRow{(int32_t)items, t.tok0, t.start, t.req};
+      items += more;
+      split |= t.n_split > 1;
     }
-  out = GroupRefs{};
-  if (first < 0) return true;
-  if (last - first >= kGroups) return false;
-  std::copy(p.groups.begin() + first, p.groups.begin() + last + 1, out.r);
-  for (int i = 0; i < n; ++i)
-    if (rows.r[i].group >= 0) rows.r[i].group -= first;
-  return true;
-}
-
-// The launches over the tokens' rows, and the merge of those that are split.
-int launch_rows(const cp_attn_desc* d, const AttnPlan& p, const AttnArgs& a, hipStream_t s) {
-  const int hkv = d->num_kv_heads;
-  // batches of rows whose groups fit a launch
-  std::vector<std::vector<AttnRow>> batches(1);
-  int32_t first = -1;
-  for (const AttnRow& r : p.rows) {
-    if (r.group >= 0) {
-      if (first >= 0 && r.group - first >= kGroups) batches.emplace_back(), first = -1;
-      if (first < 0) first = r.group;
-    }
-    batches.back().push_back(r);
-  }
-  for (const auto& rows : batches) {
-    int rc = by_rows<AttnRow, kAttnRows>(
-        rows, &AttnRow::item0, kMaxItems,
-        [&](const AttnRow& r) { return (int64_t)r.n_split * r.n * hkv; },
-        [&](AttnRows& batch, int n, int items, size_t) {
-          GroupRefs groups;
-          if (!local_groups(p, batch, n, groups)) return CP_ERR_UNSUPPORTED;
-          return finish(launch_tokens(d->head_dim, d->block_size, a, batch, n, groups, items, s), s);
-        });
+    const int32_t end = p.rows[r - 1].tok0 + p.rows[r - 1].n;
+    for (int i = n; i <= kAttnRows; ++i) batch.r[i] = AttnRow{INT_MAX, end, 0, 0};
+    a.part0 = (int)part0, a.n_groups = n_groups;
+    int rc = finish(launch_tokens(d->head_dim, d->block_size, a, batch, n, groups, (int)items, s), s);
+    if (rc == CP_OK && split)
+      rc = finish(launch_cache_merge(d->head_dim, d->block_size, a, batch, n, groups,
+                                     end - p.rows[first].tok0, s), s);
     if (rc != CP_OK) return rc;
-    std::vector<AttnRow> split;
-    for (const AttnRow& r : rows)
-      if (r.n_split > 1) split.push_back(r);
-    rc = by_rows<AttnRow, kAttnRows>(
-        split, &AttnRow::item0, kMaxItems,
-        [&](const AttnRow& r) { return (int64_t)merge_items(d->head_dim, r, d->num_q_heads); },
-        [&](AttnRows& batch, int n, int items, size_t) {
-          GroupRefs groups;
-          if (!local_groups(p, batch, n, groups)) return CP_ERR_UNSUPPORTED;
-          return finish(launch_cache_merge(d->head_dim, a, batch, n, groups, items, s), s);
-        });
-    if (rc != CP_OK) return rc;
+    if (p.split) part0 += items * G;
   }
   return CP_OK;
 }
@@ -516,16 +500,24 @@ int cp_prefix_attn(const cp_attn_desc* desc, const void* q, const void* k_cache,
     (void)hipGetLastError();
     const AttnArgs a =
         attn_args(desc, p, q, k_cache, v_cache, block_tables, nullptr, 0, out, ws);
-    const int G = desc->num_q_heads / desc->num_kv_heads;
-    rc = by_rows<PrefixRow, kPrefixRows>(
-        p.prefix, &PrefixRow::item0, kMaxItems,
-        [&](const PrefixRow& r) {
-          return ((int64_t)r.n * G + kPrefixTile - 1) / kPrefixTile * desc->num_kv_heads * r.n_split;
-        },
-        [&](PrefixRows& batch, int n, int items, size_t) {
-          return finish(launch_prefix(desc->head_dim, desc->block_size, a, batch, n, items, s), s);
-        });
-    if (rc != CP_OK) return rc;
+    const int G = desc->num_q_heads / desc->num_kv_heads, D = desc->head_dim;
+    for (const bool wide : {false, true}) {
+      thread_local std::vector<PrefixRow> some;
+      some.clear();
+      for (size_t i = 0; i < p.prefix.size(); ++i)
+        if (p.wide[i] == wide) some.push_back(p.prefix[i]);
+      rc = by_rows<PrefixRow, kPrefixRows>(
+          some, &PrefixRow::item0, kMaxItems,
+          [&](const PrefixRow& r) { return prefix_items(r, wide, G, desc->num_kv_heads); },
+          [&](PrefixRows& batch, int n, int items, size_t) {
+            const int B = desc->block_size;
+            return finish(!wide      ? launch_prefix_narrow(D, B, a, batch, n, items, s)
+                          : D == 128 ? launch_prefix_wide128(B, a, batch, items, s)
+                                     : launch_prefix_wide64(B, a, batch, items, s),
+                          s);
+          });
+      if (rc != CP_OK) return rc;
+    }
     return launch_rows(desc, p, a, s);
   });
 }

@@ -246,20 +246,20 @@ __device__ __forceinline__ void share(const State<D, NC>& st, Shared<16 * NC>& s
   __syncthreads();
 }
 
-// A group's rows over a piece of its common keys.  A workgroup takes kPrefixTile
+// A group's rows over a piece of its common keys.  A workgroup takes kNarrowTile
 // (token, q head) rows of one kv head.
 template <int D, int B, class Rows>
 __global__ __launch_bounds__(kThreads, 2) void prefix_kernel(
     const Rows rows, const AttnArgs a, const uint16_t* __restrict__ q,
     const uint16_t* __restrict__ k_cache, const uint16_t* __restrict__ v_cache,
     const int32_t* __restrict__ bt) {
-  constexpr int NC = kPrefixTile / 16, NKS = D / 32;
+  constexpr int NC = kNarrowTile / 16, NKS = D / 32;
   __shared__ __align__(16) uint8_t slices[kWaves][kSlice<D>];
   __shared__ Shared<16 * NC> s;
   const PrefixRow row = rows.r[row_index(rows, &PrefixRow::item0, (int)blockIdx.x)];
   const int unit = (int)blockIdx.x - row.item0;
   const int G = 1 << a.log2_group, all = row.n << a.log2_group;
-  const int tiles = (all + kPrefixTile - 1) / kPrefixTile, m0 = unit % tiles * kPrefixTile;
+  const int tiles = (all + kNarrowTile - 1) / kNarrowTile, m0 = unit % tiles * kNarrowTile;
   const int kvh = unit / tiles % a.hkv, split = unit / tiles / a.hkv;
   const int tid = threadIdx.x, lane = tid & 63, i = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -294,10 +294,36 @@ __global__ __launch_bounds__(kThreads, 2) void prefix_kernel(
     for (int w = 0; w < kWaves; ++w) s.f[w][tid] = f[w] * inv;
     if (m0 + tid < all) a.part_lse[part + tid] = L == 0.f ? -INFINITY : M + __log2f(L);
   }
-  write_rows<D, NC>(st, s.f, wave, min(kPrefixTile, all - m0), slices,
+  write_rows<D, NC>(st, s.f, wave, min(kNarrowTile, all - m0), slices,
                     [&](int r, int p, const f32x4_t& v) {
                       *reinterpret_cast<f32x4_t*>(a.part_o + (part + r) * D + 4 * p) = v;
                     });
+}
+
+// What a workgroup or a merge needs of row r of a launch.
+struct Own {
+  int32_t tok0, n, start, req, item0;
+  int n_split;
+  GroupRef group;  // of no keys and splits where the row is in none
+};
+
+template <int B, bool LIST, int N>
+__device__ __forceinline__ Own own_of(const RowsOf<AttnRow, N>& rows, const GroupRefs& groups,
+                                      const AttnArgs& a, int r) {
+  const AttnRow row = rows.r[r];
+  Own o{row.tok0, rows.r[r + 1].tok0 - row.tok0, row.start, row.req, row.item0, 1,
+        GroupRef{0, 0, 0, 0, 0, 0, 0}};
+  if constexpr (!LIST) {
+    const int lane = threadIdx.x & 63;
+    const int g = min(lane, kGroups - 1);
+    const uint64_t in = __builtin_amdgcn_ballot_w64(lane < a.n_groups && groups.r[g].row0 <= r &&
+                                                    r < groups.r[g].row1);
+    if (in) o.group = groups.r[__builtin_amdgcn_readfirstlane(__ffsll((unsigned long long)in) - 1)];
+  }
+  const int last = o.start + o.n - 1;
+  const int own = LIST ? min(a.n_pages, last / B + 1) : last + 1 - o.group.keys;
+  o.n_split = (own - 1) / a.piece + 1;
+  return o;
 }
 
 // A token's G rows over a piece of its own keys (LIST: of its page list).  Where
@@ -312,8 +338,9 @@ __global__ __launch_bounds__(kThreads, 2) void tokens_kernel(
   __shared__ __align__(16) uint8_t slices[kWaves][kSlice<D>];
   __shared__ Shared<16> s;
   __shared__ int s_blocks[LIST ? kListPages : 1], s_count;
-  __shared__ float s_g[8][LIST ? 1 : kMaxGroupSplits];  // factors of the group's pieces
-  const AttnRow row = rows.r[row_index(rows, &AttnRow::item0, (int)blockIdx.x)];
+  __shared__ float s_g[8][LIST ? 1 : kMaxGroupSplits];  // of the group's pieces: log sums, factors
+  const Own row = own_of<B, LIST>(rows, groups, a,
+                                  row_index(rows, &AttnRow::item0, (int)blockIdx.x));
   const int unit = (int)blockIdx.x - row.item0;
   const int kvh = unit % a.hkv, j = unit / a.hkv % row.n, split = unit / a.hkv / row.n;
   const int G = 1 << a.log2_group, tid = threadIdx.x, lane = tid & 63, i = lane & 15, g = lane >> 4;
@@ -327,7 +354,16 @@ __global__ __launch_bounds__(kThreads, 2) void tokens_kernel(
 #pragma unroll
     for (int ks = 0; ks < NKS; ++ks) qv[0][ks] = ld_global16(qb + ks * 32);
   }
-  GroupRef group{0, 0, 0, 0, 0, 0};
+  const int64_t part = (int64_t)a.part0 + (int64_t)blockIdx.x * G;
+  const GroupRef& group = row.group;
+  const int64_t gpart =
+      (int64_t)group.part0 + (int64_t)kvh * group.n_split * group.n_rows + (t - group.tok0) * G;
+  const bool alone = row.n_split == 1;
+  if constexpr (!LIST)
+    if (alone)
+      for (int x = tid; x < group.n_split * G; x += kThreads)
+        s_g[x & (G - 1)][x >> a.log2_group] =
+            group_lse[gpart + (int64_t)(x >> a.log2_group) * group.n_rows + (x & (G - 1))];
   State<D, 1> st;
   if constexpr (LIST) {
     // the piece's entries that count, and their blocks
@@ -351,7 +387,6 @@ __global__ __launch_bounds__(kThreads, 2) void tokens_kernel(
                     slices[wave],
                     [&](int b) { return __builtin_amdgcn_readfirstlane(s_blocks[b]); });
   } else {
-    if (row.group >= 0) group = groups.r[row.group];
     const int64_t begin = group.keys + (int64_t)split * a.piece;
     const int n_keys = (int)min((int64_t)a.piece, pos + 1 - begin);  // maybe none
     const int32_t* blocks = bt_row + begin / B;
@@ -359,36 +394,26 @@ __global__ __launch_bounds__(kThreads, 2) void tokens_kernel(
                     slices[wave], [&](int b) { return blocks[b]; });
   }
   share(st, s, wave);
-  const int64_t part = (int64_t)row.part0 + (((int64_t)j * a.hkv + kvh) * row.n_split + split) * G;
-  const int64_t gpart =
-      (int64_t)group.part0 + (int64_t)kvh * group.n_split * group.n_rows + (t - group.tok0) * G;
-  const bool alone = row.n_split == 1;
+  const int merged = !LIST && alone ? group.n_split : 0;
   if (tid < G) {
     float M = -INFINITY, L = 0.f, f[kWaves];
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) M = fmaxf(M, s.m[w][tid]);
-    if (!LIST && alone)
-      for (int e = 0; e < group.n_split; ++e) {
-        const float lse = group_lse[gpart + (int64_t)e * group.n_rows + tid];
-        s_g[tid][e] = lse;
-        M = fmaxf(M, lse);
-      }
+    for (int e = 0; e < merged; ++e) M = fmaxf(M, s_g[tid][e]);
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) {
       f[w] = s.m[w][tid] == -INFINITY ? 0.f : exp2f(s.m[w][tid] - M);
       L += f[w] * s.l[w][tid];
     }
-    if (!LIST && alone)
-      for (int e = 0; e < group.n_split; ++e) {
-        const float w = s_g[tid][e] == -INFINITY ? 0.f : exp2f(s_g[tid][e] - M);
-        s_g[tid][e] = w;
-        L += w;
-      }
+    for (int e = 0; e < merged; ++e) {
+      const float w = s_g[tid][e] == -INFINITY ? 0.f : exp2f(s_g[tid][e] - M);
+      s_g[tid][e] = w;
+      L += w;
+    }
     const float inv = L == 0.f ? 0.f : 1.f / L;
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) s.f[w][tid] = f[w] * inv;
-    if (!LIST && alone)
-      for (int e = 0; e < group.n_split; ++e) s_g[tid][e] *= inv;
+    for (int e = 0; e < merged; ++e) s_g[tid][e] *= inv;
     if (!alone) a.part_lse[part + tid] = L == 0.f ? -INFINITY : M + __log2f(L);
   }
   write_rows<D, 1>(st, s.f, wave, G, slices, [&](int r, int p, f32x4_t v) {
@@ -396,10 +421,17 @@ __global__ __launch_bounds__(kThreads, 2) void tokens_kernel(
       *reinterpret_cast<f32x4_t*>(a.part_o + (part + r) * D + 4 * p) = v;
       return;
     }
-    if constexpr (!LIST)
-      for (int e = 0; e < group.n_split; ++e)
-        v += s_g[r][e] * *reinterpret_cast<const f32x4_t*>(
-                             group_o + (gpart + (int64_t)e * group.n_rows + r) * D + 4 * p);
+    constexpr int U = 8;
+    for (int e0 = 0; e0 < merged; e0 += U) {
+      f32x4_t o[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u)  // past the last piece: it again, with weight 0
+        o[u] = *reinterpret_cast<const f32x4_t*>(
+            group_o + (gpart + (int64_t)min(e0 + u, merged - 1) * group.n_rows + r) * D + 4 * p);
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (e0 + u < merged) v += s_g[r][e0 + u] * o[u];
+    }
     *reinterpret_cast<uint2*>(a.out + (t * a.hq + kvh * G + r) * D + 4 * p) =
         make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
   });
@@ -409,18 +441,19 @@ __global__ __launch_bounds__(kThreads, 2) void tokens_kernel(
 // log2 of its weights' sum, the row's output is
 //     sum_s 2^(L_s - max L) O_s / sum_s 2^(L_s - max L),
 // over its own pieces and its group's.  A row (token, q head) takes D / 4
-// threads of 4 features.
-template <int D, class Rows>
+// threads of 4 features; a workgroup's rows are one token's.
+template <int D, int B, bool LIST, class Rows>
 __global__ __launch_bounds__(kThreads) void cache_merge_kernel(const Rows rows,
                                                                const GroupRefs groups,
-                                                               const AttnArgs a) {
+                                                               const AttnArgs a, int per_token) {
   constexpr int DQ = D / 4, PER = kThreads / DQ, U = 8;
-  const AttnRow row = rows.r[row_index(rows, &AttnRow::item0, (int)blockIdx.x)];
-  const int x = ((int)blockIdx.x - row.item0) * PER + threadIdx.x / DQ, dq = threadIdx.x % DQ;
-  if (x >= row.n * a.hq) return;
-  const int j = x / a.hq, h = x % a.hq, kvh = h >> a.log2_group, G = 1 << a.log2_group;
+  const int64_t t = (int64_t)rows.r[0].tok0 + (int)blockIdx.x / per_token;
+  const Own row = own_of<B, LIST>(rows, groups, a, row_index(rows, &AttnRow::tok0, (int)t));
+  if (row.n_split == 1) return;
+  const int h = (int)blockIdx.x % per_token * PER + threadIdx.x / DQ, dq = threadIdx.x % DQ;
+  if (h >= a.hq) return;
+  const int j = (int)(t - row.tok0), kvh = h >> a.log2_group, G = 1 << a.log2_group;
   const int e = h & (G - 1);
-  const int64_t t = (int64_t)row.tok0 + j;
   float M = -INFINITY, W = 0.f;
   f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
   const auto add = [&](int64_t first, int64_t stride, int n) {
@@ -450,12 +483,13 @@ __global__ __launch_bounds__(kThreads) void cache_merge_kernel(const Rows rows,
       }
     }
   };
-  add((int64_t)row.part0 + ((int64_t)j * a.hkv + kvh) * row.n_split * G + e, G, row.n_split);
-  if (row.group >= 0) {
-    const GroupRef g = groups.r[row.group];
+  // workgroup (split, j, kvh) of the row's launch wrote its G rows
+  const int64_t unit = (int64_t)row.item0 + (int64_t)j * a.hkv + kvh;
+  add(a.part0 + unit * G + e, (int64_t)row.n * a.hq, row.n_split);
+  const GroupRef& g = row.group;
+  if (g.n_split > 0)
     add((int64_t)g.part0 + (int64_t)kvh * g.n_split * g.n_rows + (t - g.tok0) * G + e, g.n_rows,
         g.n_split);
-  }
   const float inv = W == 0.f ? 0.f : 1.f / W;
   *reinterpret_cast<uint2*>(a.out + (t * a.hq + h) * D + dq * 4) =
       make_uint2(pack_bf16x2(acc[0] * inv, acc[1] * inv), pack_bf16x2(acc[2] * inv, acc[3] * inv));
@@ -483,10 +517,24 @@ hipError_t launch_tokens_t(const AttnArgs& a, const AttnRows& rows, int n_rows,
   });
 }
 
+template <int D, int B>
+hipError_t launch_merge_t(const AttnArgs& a, const AttnRows& rows, int n_rows,
+                          const GroupRefs& groups, int n_tokens, hipStream_t s) {
+  const int per_token = (a.hq * (D / 4) + kThreads - 1) / kThreads;
+  return by_size(rows, n_rows, [&](const auto& r) {
+    if (a.pages)
+      hipLaunchKernelGGL((cache_merge_kernel<D, B, true>), dim3(n_tokens * per_token),
+                         dim3(kThreads), 0, s, r, groups, a, per_token);
+    else
+      hipLaunchKernelGGL((cache_merge_kernel<D, B, false>), dim3(n_tokens * per_token),
+                         dim3(kThreads), 0, s, r, groups, a, per_token);
+  });
+}
+
 }  // namespace
 
-hipError_t launch_prefix(int d, int block, const AttnArgs& a, const PrefixRows& rows, int n_rows,
-                         int items, hipStream_t s) {
+hipError_t launch_prefix_narrow(int d, int block, const AttnArgs& a, const PrefixRows& rows,
+                                int n_rows, int items, hipStream_t s) {
   auto f = d == 128 ? (block == 16 ? launch_prefix_t<128, 16> : launch_prefix_t<128, 32>)
                     : (block == 16 ? launch_prefix_t<64, 16> : launch_prefix_t<64, 32>);
   return f(a, rows, n_rows, items, s);
@@ -499,19 +547,11 @@ hipError_t launch_tokens(int d, int block, const AttnArgs& a, const AttnRows& ro
   return f(a, rows, n_rows, groups, items, s);
 }
 
-int merge_items(int d, const AttnRow& row, int hq) {
-  const int per = kThreads / (d / 4);
-  return (int)(((int64_t)row.n * hq + per - 1) / per);
-}
-
-hipError_t launch_cache_merge(int d, const AttnArgs& a, const AttnRows& rows, int n_rows,
-                              const GroupRefs& groups, int items, hipStream_t s) {
-  return by_size(rows, n_rows, [&](const auto& r) {
-    if (d == 128)
-      hipLaunchKernelGGL(cache_merge_kernel<128>, dim3(items), dim3(kThreads), 0, s, r, groups, a);
-    else
-      hipLaunchKernelGGL(cache_merge_kernel<64>, dim3(items), dim3(kThreads), 0, s, r, groups, a);
-  });
+hipError_t launch_cache_merge(int d, int block, const AttnArgs& a, const AttnRows& rows, int n_rows,
+                              const GroupRefs& groups, int n_tokens, hipStream_t s) {
+  auto f = d == 128 ? (block == 16 ? launch_merge_t<128, 16> : launch_merge_t<128, 32>)
+                    : (block == 16 ? launch_merge_t<64, 16> : launch_merge_t<64, 32>);
+  return f(a, rows, n_rows, groups, n_tokens, s);
 }
 
 }  // namespace cpcache

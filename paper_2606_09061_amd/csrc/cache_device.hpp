@@ -11,8 +11,8 @@ namespace cpcache {
 template <class T, int N, class F>
 hipError_t by_size(const RowsOf<T, N>& rows, int n, F&& launch) {
   if (n <= kFewRows) {
-    RowsOf<T, kFewRows> few;
-    for (int i = 0; i < kFewRows; ++i) few.r[i] = rows.r[i];  // with the places behind the rows
+    RowsOf<T, kFewRows + 1> few;
+    for (int i = 0; i <= kFewRows; ++i) few.r[i] = rows.r[i];  // with the places behind the rows
     launch(few);
   } else {
     launch(rows);

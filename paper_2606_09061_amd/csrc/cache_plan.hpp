@@ -15,21 +15,32 @@ constexpr int64_t kMaxItems = (1 << 24) - 1;
 // Tokens and pages of a piece of a row: longer rows come as several.
 constexpr int kPieceTokens = 512, kPiecePages = 2048;
 
-// Keys that the four waves of an attention workgroup take in turn.
-constexpr int kTurn = 128;
+// Keys that the four waves of a narrow attention workgroup take in turn, and those
+// of a wide one's step.
+constexpr int kTurn = 128, kWideTurn = 64;
 // Most pages of a piece of a page list (its workgroup holds them in LDS).
 constexpr int kListPages = 256;
 // Most pieces of a group's keys (the factors of their merge are in LDS).
 constexpr int kMaxGroupSplits = 128;
 
-// A group's (token, q head) rows per kv head that a workgroup takes.
-constexpr int kPrefixTile = 32;
+// A group's (token, q head) rows per kv head that a workgroup takes: the narrow
+// kernel's waves share the keys, the wide one's the rows.
+constexpr int kNarrowTile = 32, kWideTile = 128;
+
+struct TokenRow {    // a piece of a row's tokens
+  int32_t tok0, n, start, req;
+  int32_t group;     // AttnPlan::prefix's, or -1
+  int32_t n_split;   // pieces of its key range
+};
 
 struct AttnPlan {
-  std::vector<AttnRow> rows;       // the tokens' own keys
-  std::vector<PrefixRow> prefix;   // of the groups that share something
-  std::vector<GroupRef> groups;    // the same groups, by AttnRow::group
-  int piece = 0;                   // keys, or entries of a list, of a piece of the rows' ranges
+  std::vector<TokenRow> rows;       // in the order of their tokens
+  std::vector<PrefixRow> prefix;    // of the groups that share something
+  std::vector<uint8_t> wide;        // their kernels
+  std::vector<int32_t> group_rows;  // index of each group's first of `rows`
+  int piece = 0;                    // keys, or entries of a list, of a piece of the rows' ranges
+  bool split = false;               // some row is, and all have partial rows
+  int32_t row_part0 = 0;            // the first of them; the groups' come before
   int64_t partial_rows = 0;
   size_t off_lse = 0, ws_bytes = 256;  // partial rows of D fp32, then their log sums
 };
@@ -40,5 +51,11 @@ bool plan_pages(const cp_attn_desc& desc, const cp_row_meta* rows, int32_t n_row
                 AttnPlan& out);
 bool plan_prefix(const cp_attn_desc& desc, const cp_row_meta* rows, int32_t n_rows,
                  const cp_prefix_group* groups, int32_t n_groups, AttnPlan& out);
+
+// Workgroups of a group's common keys.
+inline int64_t prefix_items(const PrefixRow& p, bool wide, int group, int hkv) {
+  const int tile = wide ? kWideTile : kNarrowTile;
+  return ((int64_t)p.n * group + tile - 1) / tile * hkv * p.n_split;
+}
 
 }  // namespace cpcache

@@ -62,54 +62,55 @@ void check(const cp_attn_desc& d, const std::vector<cp_row_meta>& rows,
     CHECK(p.ws_bytes >= 256 && p.off_lse + (size_t)p.partial_rows * 4 <= p.ws_bytes);
     CHECK(p.off_lse == (size_t)p.partial_rows * d.head_dim * 4);
     CHECK(p.piece >= 1 && (which || p.piece <= kListPages));
-    CHECK(p.groups.size() == p.prefix.size());
+    CHECK(p.wide.size() == p.prefix.size() && p.group_rows.size() == p.prefix.size());
     std::vector<Range> parts;
     for (size_t i = 0; i < p.prefix.size(); ++i) {
       const PrefixRow& g = p.prefix[i];
+      const int64_t turn = p.wide[i] ? kWideTurn : kTurn;
       CHECK(g.n >= 1 && g.keys >= B && g.keys % B == 0 && g.split_keys >= 1);
       CHECK(g.n_split >= 1 && g.n_split <= kMaxGroupSplits);
       CHECK((int64_t)g.n_split * g.split_keys >= g.keys && (int64_t)(g.n_split - 1) * g.split_keys < g.keys);
-      CHECK(g.n_split == 1 || g.split_keys % B == 0);
+      CHECK(g.n_split == 1 || g.split_keys % turn == 0);
       CHECK(g.part0 >= 0);
       parts.push_back({g.part0, (int64_t)g.n_split * g.n * hq});
-      const GroupRef& r = p.groups[i];
-      CHECK(r.keys == g.keys && r.part0 == g.part0 && r.n_split == g.n_split && r.tok0 == g.tok0);
-      CHECK(r.n_rows == g.n * (hq / hkv));
-      const int64_t items = ((int64_t)g.n * (hq / hkv) + kPrefixTile - 1) / kPrefixTile * hkv * g.n_split;
-      CHECK(items <= kMaxItems);
+      CHECK(p.rows[p.group_rows[i]].tok0 == g.tok0 && p.rows[p.group_rows[i]].group == (int)i);
+      CHECK(prefix_items(g, p.wide[i], hq / hkv, hkv) <= kMaxItems);
     }
     size_t at = 0;
-    int32_t tok = 0;
+    int32_t tok = 0, group = -1;
+    int64_t own_parts = 0;
+    bool split = false;
     for (const cp_row_meta& m : rows) {
       for (int32_t j = 0; j < m.chunk_len;) {
         CHECK(at < p.rows.size());
-        const AttnRow& r = p.rows[at++];
+        const TokenRow& r = p.rows[at++];
         CHECK(r.tok0 == tok + j && r.start == m.chunk_start + j && r.req == m.req_id);
         CHECK(r.n >= 1 && r.n <= kPieceTokens && j + r.n <= m.chunk_len && r.n_split >= 1);
-        CHECK(r.group >= -1 && r.group < (int64_t)p.groups.size());
+        CHECK(r.group >= -1 && r.group < (int64_t)p.prefix.size());
         int64_t own = std::min<int64_t>(n_pages, (r.start + r.n - 1) / B + 1);
         if (which) {
           own = (int64_t)r.start + r.n;
           if (r.group >= 0) {
-            const GroupRef& g = p.groups[r.group];
-            CHECK(g.keys <= r.start && r.tok0 >= g.tok0);
-            CHECK(r.tok0 + r.n <= g.tok0 + g.n_rows / (hq / hkv));
+            CHECK(r.group >= group);  // rising
+            group = r.group;
+            const PrefixRow& g = p.prefix[r.group];
+            CHECK(g.keys <= r.start && r.tok0 >= g.tok0 && r.tok0 + r.n <= g.tok0 + g.n);
             own -= g.keys;
           }
         } else {
           CHECK(r.group == -1);
         }
-        CHECK((int64_t)r.n_split * p.piece >= own);
+        CHECK(own >= 1 && r.n_split == (own - 1) / p.piece + 1);  // as the kernels have it
         CHECK((int64_t)r.n_split * r.n * hkv <= kMaxItems);
-        if (r.n_split > 1) {
-          CHECK(r.part0 >= 0 && (!which || p.piece % B == 0));
-          parts.push_back({r.part0, (int64_t)r.n_split * r.n * hq});
-        }
+        CHECK(r.n_split == 1 || !which || p.piece % B == 0);
+        own_parts += (int64_t)r.n_split * r.n * hq;
+        split |= r.n_split > 1;
         j += r.n;
       }
       tok += m.chunk_len;
     }
-    CHECK(at == p.rows.size());
+    CHECK(at == p.rows.size() && split == p.split);
+    if (split) parts.push_back({p.row_part0, own_parts});
     no_overlap(parts, p.partial_rows);
   }
 }
