@@ -46,32 +46,31 @@ constexpr int kSelectRows = 112;
 using SelectRows = RowsOf<SelectRow, kSelectRows>;
 
 // A piece of a row of cp_page_attn or cp_prefix_attn.  A launch's rows follow each
-// other: the next one's first token and item end a row, and the place behind the
-// last row holds the launch's ends.  With `own` keys (or entries of a list) of its
-// last token, a row has ceil(own / piece) pieces, and the partial rows of its
+// other: the next one's first token ends a row, and the place behind the last row
+// holds the launch's end.  With `own` keys (or entries of a list) of its last
+// token, a row has ceil(own / piece) pieces, and the partial rows of its
 // workgroup x are (item0 + x) G and on, behind those of the launches before.
 struct AttnRow {     // 16 bytes
-  int32_t item0;     // the launch's workgroups before it
+  int32_t item0;     // the launch's workgroups of rows before it
   int32_t tok0, start, req;
 };
-constexpr int kAttnRows = 160;
-using AttnRows = RowsOf<AttnRow, kAttnRows + 1>;
 
-struct GroupRef {    // 28 bytes: what the rows of a group need of it
-  int32_t row0, row1;  // the launch's rows that it holds
-  int32_t keys;      // those read for the whole group, whole pages
-  int32_t part0, n_split, n_rows;  // its partial rows: [kv head][split][n_rows]
-  int32_t tok0;      // its first token
+struct PrefixRow {   // 44 bytes: a group's common keys
+  int32_t item0;     // the launch's workgroups of groups before it
+  int32_t tok0, n, req;      // its first token, its tokens, a table row that has the keys
+  int32_t keys;              // whole pages, read once for the group
+  int32_t n_split, split_keys, part0;  // partial rows: [kv head][split][n G]
+  int32_t wide;              // its kernel
+  int32_t row0, row1;        // the launch's rows that are its
 };
-constexpr int kGroups = 36;
-using GroupRefs = RowsOf<GroupRef, kGroups>;
 
-struct PrefixRow {   // 32 bytes: a group's common keys
-  int32_t item0;
-  int32_t tok0, n, req;
-  int32_t keys, n_split, split_keys, part0;
+constexpr int kAttnRows = 150, kGroups = 24;
+template <int NG, int NR>
+struct AttnBatchOf {
+  PrefixRow g[NG];
+  AttnRow r[NR + 1];
 };
-constexpr int kPrefixRows = 112;
-using PrefixRows = RowsOf<PrefixRow, kPrefixRows>;
+using AttnBatch = AttnBatchOf<kGroups, kAttnRows>;
+using FewAttnBatch = AttnBatchOf<4, kFewRows>;
 
 }  // namespace cpcache

@@ -202,44 +202,58 @@ AttnArgs attn_args(const cp_attn_desc* d, const AttnPlan& p, const void* q, cons
                   p.piece,
                   0,
                   0,
+                  0,
                   d->sm_scale * cpattn::kLog2e};
 }
 
-// The launches over the tokens' rows, each with the merge of its rows that are split.
-int launch_rows(const cp_attn_desc* d, const AttnPlan& p, AttnArgs a, hipStream_t s) {
-  const int hkv = d->num_kv_heads, G = d->num_q_heads / hkv;
+// The launches of a plan, each with some of the rows, the groups that begin among
+// them, and the merge of what has several pieces.
+int launch_plan(const cp_attn_desc* d, const AttnPlan& p, AttnArgs a, hipStream_t s) {
+  const int hkv = d->num_kv_heads, G = d->num_q_heads / hkv, D = d->head_dim, B = d->block_size;
   int64_t part0 = p.row_part0;
+  int begun = 0;  // groups whose workgroups have been launched
   for (size_t r = 0; r < p.rows.size();) {
-    AttnRows batch;
-    GroupRefs groups{};
-    int64_t items = 0;
+    AttnBatch b;
+    int64_t items = 0, group_items = 0;
     int n = 0, n_groups = 0, last = -1;
-    bool split = false;
+    bool merge = false, wide = false;
     const size_t first = r;
     for (; r < p.rows.size() && n < kAttnRows; ++r) {
       const TokenRow& t = p.rows[r];
       const int64_t more = (int64_t)t.n_split * t.n * hkv;
-      if (n > 0 && items + more > kMaxItems) break;
-      if (t.group >= 0 && t.group != last) {
+      const bool other = t.group >= 0 && t.group != last, fresh = other && t.group == begun;
+      const int64_t shared = fresh ? prefix_items(p.prefix[t.group], G, hkv) : 0;
+      if (n > 0 && items + group_items + more + shared > kMaxItems) break;
+      if (other) {
         if (n_groups == kGroups) break;
-        const PrefixRow& g = p.prefix[t.group];
-        groups.r[n_groups++] = GroupRef{n, n, g.keys, g.part0, g.n_split, g.n * G, g.tok0};
+        b.g[n_groups] = p.prefix[t.group];
+        b.g[n_groups].row0 = n;
+        // (of a group that began in an earlier launch: no item, it is this one's first)
+        b.g[n_groups++].item0 = (int32_t)group_items;
+        wide |= fresh && p.prefix[t.group].wide;
+        group_items += shared;
         last = t.group;
+        if (fresh) ++begun;
       }
-      if (t.group >= 0) groups.r[n_groups - 1].row1 = n + 1;
-      batch.r[n++] = AttnRow{(int32_t)items, t.tok0, t.start, t.req};
+      if (t.group >= 0) b.g[n_groups - 1].row1 = n + 1;
+      b.r[n++] = AttnRow{(int32_t)items, t.tok0, t.start, t.req};
       items += more;
-      split |= t.n_split > 1;
+      merge |= t.n_split > 1 || t.group >= 0;
     }
     const int32_t end = p.rows[r - 1].tok0 + p.rows[r - 1].n;
-    for (int i = n; i <= kAttnRows; ++i) batch.r[i] = AttnRow{INT_MAX, end, 0, 0};
-    a.part0 = (int)part0, a.n_groups = n_groups;
-    int rc = finish(launch_tokens(d->head_dim, d->block_size, a, batch, n, groups, (int)items, s), s);
-    if (rc == CP_OK && split)
-      rc = finish(launch_cache_merge(d->head_dim, d->block_size, a, batch, n, groups,
-                                     end - p.rows[first].tok0, s), s);
+    for (int i = n_groups; i < kGroups; ++i) b.g[i] = PrefixRow{}, b.g[i].item0 = INT_MAX;
+    for (int i = n; i <= kAttnRows; ++i) b.r[i] = AttnRow{INT_MAX, end, 0, 0};
+    a.part0 = (int)part0, a.n_groups = n_groups, a.group_items = (int)group_items;
+    const int all = (int)(items + group_items);
+    const hipError_t e = a.pages    ? launch_pages(D, B, a, b, n, all, s)
+                         : !wide    ? launch_shared(D, B, a, b, n, all, s)
+                         : D == 128 ? launch_shared_wide128(B, a, b, all, s)
+                                    : launch_shared_wide64(B, a, b, all, s);
+    int rc = finish(e, s);
+    if (rc == CP_OK && merge)
+      rc = finish(launch_cache_merge(D, B, a, b, n, end - p.rows[first].tok0, s), s);
     if (rc != CP_OK) return rc;
-    if (p.split) part0 += items * G;
+    if (p.parts) part0 += items * G;
   }
   return CP_OK;
 }
@@ -456,7 +470,7 @@ int cp_page_attn(const cp_attn_desc* desc, const void* q, const void* k_cache, c
     rc = check_tables(desc, block_tables, rows, n_rows, false, s);
     if (rc != CP_OK) return rc;
     (void)hipGetLastError();
-    return launch_rows(desc, p,
+    return launch_plan(desc, p,
                        attn_args(desc, p, q, k_cache, v_cache, block_tables, pages, n_pages, out, ws),
                        s);
   });
@@ -498,27 +512,8 @@ int cp_prefix_attn(const cp_attn_desc* desc, const void* q, const void* k_cache,
     if (rc == CP_OK) rc = check_shared(desc, block_tables, rows, groups, n_groups, s);
     if (rc != CP_OK) return rc;
     (void)hipGetLastError();
-    const AttnArgs a =
-        attn_args(desc, p, q, k_cache, v_cache, block_tables, nullptr, 0, out, ws);
-    const int G = desc->num_q_heads / desc->num_kv_heads, D = desc->head_dim;
-    for (const bool wide : {false, true}) {
-      thread_local std::vector<PrefixRow> some;
-      some.clear();
-      for (size_t i = 0; i < p.prefix.size(); ++i)
-        if (p.wide[i] == wide) some.push_back(p.prefix[i]);
-      rc = by_rows<PrefixRow, kPrefixRows>(
-          some, &PrefixRow::item0, kMaxItems,
-          [&](const PrefixRow& r) { return prefix_items(r, wide, G, desc->num_kv_heads); },
-          [&](PrefixRows& batch, int n, int items, size_t) {
-            const int B = desc->block_size;
-            return finish(!wide      ? launch_prefix_narrow(D, B, a, batch, n, items, s)
-                          : D == 128 ? launch_prefix_wide128(B, a, batch, items, s)
-                                     : launch_prefix_wide64(B, a, batch, items, s),
-                          s);
-          });
-      if (rc != CP_OK) return rc;
-    }
-    return launch_rows(desc, p, a, s);
+    return launch_plan(
+        desc, p, attn_args(desc, p, q, k_cache, v_cache, block_tables, nullptr, 0, out, ws), s);
   });
 }
 

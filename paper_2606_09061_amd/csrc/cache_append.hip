@@ -58,7 +58,7 @@ __global__ __launch_bounds__(kThreads) void append_kernel(
     const int64_t w = (int64_t)blockIdx.x * kWaves + wave;
     if (w >= (int64_t)tokens * parts) return;
     const int x = (int)(w / parts), part = (int)(w % parts);
-    const AppendRow row = rows.r[row_index(rows, &AppendRow::first, x)];
+    const AppendRow row = rows.r[row_index(rows.r, &AppendRow::first, x)];
     const int64_t t = (int64_t)row.tok0 + x - row.first;
     const int slot = row.start + x - row.first;
     const int64_t blk = bt[(int64_t)row.req * a.mbr + slot / B];
@@ -129,7 +129,7 @@ __global__ __launch_bounds__(kThreads) void append_kernel(
   using V = VGeom<D, B>;
   const int64_t item = (int64_t)((int)blockIdx.x - rope_blocks) * kWaves + wave;
   if (item >= v_items) return;
-  const AppendRow row = rows.r[row_index(rows, &AppendRow::item0, (int)item)];
+  const AppendRow row = rows.r[row_index(rows.r, &AppendRow::item0, (int)item)];
   const int per = (hkv + V::HEADS - 1) / V::HEADS;  // items per page
   const int y = (int)item - row.item0, lb = row.start / B + y / per;
   const int h = y % per * V::HEADS + lane / V::LANES;
@@ -182,7 +182,7 @@ __global__ __launch_bounds__(kThreads) void bounds_kernel(const Rows rows, const
   const int64_t item = (int64_t)blockIdx.x * kWaves + wave;
   if (item >= items) return;
   const int x = (int)(item / a.hkv), h = (int)(item % a.hkv);
-  const BoundsRow row = rows.r[row_index(rows, &BoundsRow::item0, x)];
+  const BoundsRow row = rows.r[row_index(rows.r, &BoundsRow::item0, x)];
   const int lb = row.page0 + x - row.item0, held = min(B, row.ctx - lb * B);
   const int64_t blk = bt[(int64_t)row.req * a.mbr + lb];
   if (blk < 0 || blk >= a.num_blocks) return;

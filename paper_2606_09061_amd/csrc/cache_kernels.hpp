@@ -49,8 +49,9 @@ struct AttnArgs {
   float* part_o;         // [partial rows][D], normalised
   float* part_lse;       // [partial rows], log2 of the weights' sum
   int hq, hkv, mbr, log2_group, n_pages, piece;
-  int part0;             // the partial rows of the launch's first workgroup
+  int part0;             // the partial rows of the launch's first workgroup of rows
   int n_groups;          // of the launch
+  int group_items;       // its first workgroups, which are the groups'
   float scale_log2;      // sm_scale * log2(e)
 };
 
@@ -64,18 +65,19 @@ hipError_t launch_score(int d, const SelectArgs& a, const SelectRows& rows, int 
                         hipStream_t s);
 hipError_t launch_choose(const SelectArgs& a, const SelectRows& rows, int n_rows, int items,
                          hipStream_t s);
-// groups' rows over their common keys: partial rows
-hipError_t launch_prefix_narrow(int d, int block, const AttnArgs& a, const PrefixRows& rows,
-                                int n_rows, int items, hipStream_t s);
-hipError_t launch_prefix_wide64(int block, const AttnArgs& a, const PrefixRows& rows, int items,
+// tokens over their page lists
+hipError_t launch_pages(int d, int block, const AttnArgs& a, const AttnBatch& b, int n_rows,
+                        int items, hipStream_t s);
+// groups over their common keys, and tokens over their own
+hipError_t launch_shared(int d, int block, const AttnArgs& a, const AttnBatch& b, int n_rows,
+                         int items, hipStream_t s);
+// the same where some group is wide
+hipError_t launch_shared_wide64(int block, const AttnArgs& a, const AttnBatch& b, int items,
                                 hipStream_t s);
-hipError_t launch_prefix_wide128(int block, const AttnArgs& a, const PrefixRows& rows, int items,
+hipError_t launch_shared_wide128(int block, const AttnArgs& a, const AttnBatch& b, int items,
                                  hipStream_t s);
-// tokens over their own keys or their page lists
-hipError_t launch_tokens(int d, int block, const AttnArgs& a, const AttnRows& rows, int n_rows,
-                         const GroupRefs& groups, int items, hipStream_t s);
-// the merge of the same launch's rows that are split, of n_tokens tokens
-hipError_t launch_cache_merge(int d, int block, const AttnArgs& a, const AttnRows& rows, int n_rows,
-                              const GroupRefs& groups, int n_tokens, hipStream_t s);
+// the merge of the same batch's rows that have several pieces, of n_tokens tokens
+hipError_t launch_cache_merge(int d, int block, const AttnArgs& a, const AttnBatch& b, int n_rows,
+                              int n_tokens, hipStream_t s);
 
 }  // namespace cpcache

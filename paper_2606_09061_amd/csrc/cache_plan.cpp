@@ -35,8 +35,8 @@ void add_row(AttnPlan& out, int32_t tok0, const cp_row_meta& m, int32_t group) {
 }
 
 void reset(AttnPlan& out) {
-  out.rows.clear(), out.prefix.clear(), out.wide.clear(), out.group_rows.clear();
-  out.piece = 1, out.split = false, out.row_part0 = 0;
+  out.rows.clear(), out.prefix.clear();
+  out.piece = 1, out.parts = false, out.row_part0 = 0;
   out.partial_rows = 0, out.off_lse = 0, out.ws_bytes = 256;
 }
 
@@ -62,11 +62,11 @@ bool cut_rows(AttnPlan& out, const cp_attn_desc& d, double keys, int per_turn, i
   int64_t partial = 0;
   for (TokenRow& r : out.rows) {
     r.n_split = (int)ceil_div(own(r), out.piece);
-    out.split |= r.n_split > 1;
+    out.parts |= r.n_split > 1 || r.group >= 0;
     partial += (int64_t)r.n_split * r.n * d.num_q_heads;
   }
   out.row_part0 = (int32_t)std::min<int64_t>(out.partial_rows, INT32_MAX);
-  if (out.split) out.partial_rows += partial;
+  if (out.parts) out.partial_rows += partial;
   if (out.partial_rows > INT32_MAX) return false;
   out.off_lse = (size_t)out.partial_rows * d.head_dim * 4;
   out.ws_bytes = std::max<size_t>(256, out.off_lse + (size_t)out.partial_rows * 4);
@@ -81,8 +81,8 @@ void cut_groups(AttnPlan& out, const cp_attn_desc& d, bool wide) {
   int64_t uncut = 0;
   double keys = 0;
   for (size_t i = 0; i < out.prefix.size(); ++i)
-    if (out.wide[i] == wide) {
-      uncut += prefix_items(out.prefix[i], wide, G, d.num_kv_heads);
+    if (out.prefix[i].wide == wide) {
+      uncut += prefix_items(out.prefix[i], G, d.num_kv_heads);
       keys += out.prefix[i].keys;
     }
   if (uncut == 0) return;
@@ -90,9 +90,9 @@ void cut_groups(AttnPlan& out, const cp_attn_desc& d, bool wide) {
   if (uncut < kUncut) {
     for (size_t i = 0; i < out.prefix.size(); ++i) {
       const PrefixRow& p = out.prefix[i];
-      if (out.wide[i] != wide) continue;
+      if (out.prefix[i].wide != wide) continue;
       work.turns.push_back((uint32_t)ceil_div(p.keys, turn));
-      work.per_split.push_back((uint32_t)prefix_items(p, wide, G, d.num_kv_heads));
+      work.per_split.push_back((uint32_t)prefix_items(p, G, d.num_kv_heads));
       work.partial.push_back((uint32_t)((int64_t)p.n * d.num_q_heads));
     }
     double time = 0;
@@ -100,7 +100,7 @@ void cut_groups(AttnPlan& out, const cp_attn_desc& d, bool wide) {
   }
   for (size_t i = 0; i < out.prefix.size(); ++i) {
     PrefixRow& p = out.prefix[i];
-    if (out.wide[i] != wide) continue;
+    if (out.prefix[i].wide != wide) continue;
     const int64_t turns = ceil_div(p.keys, turn);
     const int64_t per = ceil_div(turns, std::min<int64_t>(kMaxGroupSplits, ceil_div(turns, piece)));
     p.n_split = (int32_t)ceil_div(turns, per);
@@ -138,8 +138,7 @@ bool plan_prefix(const cp_attn_desc& desc, const cp_row_meta* rows, int32_t n_ro
     if (g < n_groups && i >= groups[g].first_row && groups[g].common >= B && rows[i].chunk_len > 0) {
       if (last != g) {
         const int32_t keys = groups[g].common / B * B;
-        out.prefix.push_back(PrefixRow{0, tok, 0, rows[i].req_id, keys, 1, keys, 0});
-        out.group_rows.push_back((int32_t)out.rows.size());
+        out.prefix.push_back(PrefixRow{0, tok, 0, rows[i].req_id, keys, 1, keys, 0, 0, 0, 0});
         last = g;
       }
       ref = (int32_t)out.prefix.size() - 1;
@@ -148,7 +147,7 @@ bool plan_prefix(const cp_attn_desc& desc, const cp_row_meta* rows, int32_t n_ro
     add_row(out, tok, rows[i], ref);
     tok += rows[i].chunk_len;
   }
-  for (const PrefixRow& p : out.prefix) out.wide.push_back((int64_t)p.n * G > kNarrowTile);
+  for (PrefixRow& p : out.prefix) p.wide = (int64_t)p.n * G > kNarrowTile;
   cut_groups(out, desc, false);
   cut_groups(out, desc, true);
   for (PrefixRow& p : out.prefix) {

@@ -36,10 +36,8 @@ struct TokenRow {    // a piece of a row's tokens
 struct AttnPlan {
   std::vector<TokenRow> rows;       // in the order of their tokens
   std::vector<PrefixRow> prefix;    // of the groups that share something
-  std::vector<uint8_t> wide;        // their kernels
-  std::vector<int32_t> group_rows;  // index of each group's first of `rows`
   int piece = 0;                    // keys, or entries of a list, of a piece of the rows' ranges
-  bool split = false;               // some row is, and all have partial rows
+  bool parts = false;               // some row has several, and all have partial rows
   int32_t row_part0 = 0;            // the first of them; the groups' come before
   int64_t partial_rows = 0;
   size_t off_lse = 0, ws_bytes = 256;  // partial rows of D fp32, then their log sums
@@ -53,8 +51,8 @@ bool plan_prefix(const cp_attn_desc& desc, const cp_row_meta* rows, int32_t n_ro
                  const cp_prefix_group* groups, int32_t n_groups, AttnPlan& out);
 
 // Workgroups of a group's common keys.
-inline int64_t prefix_items(const PrefixRow& p, bool wide, int group, int hkv) {
-  const int tile = wide ? kWideTile : kNarrowTile;
+inline int64_t prefix_items(const PrefixRow& p, int group, int hkv) {
+  const int tile = p.wide ? kWideTile : kNarrowTile;
   return ((int64_t)p.n * group + tile - 1) / tile * hkv * p.n_split;
 }
 

@@ -68,7 +68,7 @@ __global__ __launch_bounds__(kThreads) void score_kernel(const Rows rows, const 
   constexpr int L = D / 8, PPW = 64 / L, U = 4;  // pages per load, loads in flight
   const int lane = threadIdx.x & 63, sub = lane % L;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const SelectRow row = rows.r[row_index(rows, &SelectRow::item0, (int)blockIdx.x)];
+  const SelectRow row = rows.r[row_index(rows.r, &SelectRow::item0, (int)blockIdx.x)];
   const int chunks = (row.stride + kScorePages - 1) / kScorePages;
   const int x = (int)blockIdx.x - row.item0;
   const int chunk = x % chunks, h = x / chunks % a.hkv, j = x / chunks / a.hkv;
@@ -165,7 +165,7 @@ __global__ __launch_bounds__(kThreads) void choose_kernel(const Rows rows, const
   __shared__ int s_hist[256];
   __shared__ int s_wave[kWaves];
   __shared__ int s_digit, s_left;
-  const SelectRow row = rows.r[row_index(rows, &SelectRow::item0, (int)blockIdx.x)];
+  const SelectRow row = rows.r[row_index(rows.r, &SelectRow::item0, (int)blockIdx.x)];
   const int x = (int)blockIdx.x - row.item0, h = x % a.hkv, j = x / a.hkv;
   const int64_t t = (int64_t)row.tok0 + j;
   int32_t* dst = a.pages + (t * a.hkv + h) * a.n_pages;

@@ -1,0 +1,403 @@
+// Attention over selected pages and behind common prefixes (include/cp_cache.h).
+//
+// A decode token has G = Hq / Hkv rows per kv head for each key that is read, G
+// flop a byte: its kernels are bound by the stream of K and V.  Tokens that
+// share their keys bring G rows each.  No row ever sees only a part of what its
+// workgroup reads, but for the end of the range: there are no masks.
+//
+// Softmax runs in base 2, over one pass of the keys, with a running maximum
+// that moves lazily (a score has to exceed it by 2^8).  The weights are rounded
+// to bf16, the type that the matrix cores want beside V, and summed as rounded,
+// in fp32.
+#pragma once
+
+#include "cache_device.hpp"
+#include "cache_plan.hpp"
+
+namespace cpcache {
+
+using cpattn::bf16x8_t;
+using cpattn::dot2_bf16;
+using cpattn::f32x4_t;
+using cpattn::kRescaleThreshold;
+using cpattn::ld_global16;
+using cpattn::ld_global16_nt;
+using cpattn::pack_bf16x2;
+using cpattn::shfl_xor_f;
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kWaves = kThreads / 64;
+
+__device__ __forceinline__ f32x4_t mfma16x16x32(uint4 a, uint4 b, f32x4_t c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a),
+                                                 __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
+}
+
+template <int D>
+constexpr int kSlice = 16 * D * 4;  // bytes of LDS per wave: 32 keys' rows, then 16 rows' output
+
+// A wave's state over 16 NC rows, the columns of both products
+// (v_mfma_f32_16x16x32_bf16), lane l = 16 g + i:
+//   S^T (2 x 16 keys x 16 NC rows) = K . Q^T.  Row i of key half b is key
+//     8 (i / 4) + 4 b + i % 4, so that lane (g, i) ends up with rows i's scores
+//     of keys 8 g .. 8 g + 7, the B operand of the second product: the
+//     weights never leave the lane.
+//   O^T (D x 16 NC rows) += V^T . P^T: lane (g, i) reads 8 consecutive keys of
+//     feature rows 16 dt + i, the A operand as the [D][B] blocks store it.
+template <int D, int NC>
+struct State {
+  float m[NC], l[NC];
+  f32x4_t o[NC][D / 16];
+};
+
+// Attends the wave's rows qv to keys [0, n_keys) of consecutive blocks, of which
+// wave w takes tiles of 32 keys w, w + 4, ...; block_of(i) is the i-th block's
+// place in the pool, for i below the blocks that n_keys fill.  K and V are
+// loaded as they lie in memory, K's rows passing through `slice`, LDS that only
+// this wave uses.  K of the next tile is on its way from there on, V from the
+// end of a tile to the product with it in the next.
+template <int D, int B, int NC, class BlockOf>
+__device__ __forceinline__ void attend(State<D, NC>& st, const uint4 (&qv)[NC][D / 32], int n_keys,
+                                       int wave, int kvh, int hkv, float scale_log2,
+                                       const uint16_t* __restrict__ k_cache,
+                                       const uint16_t* __restrict__ v_cache, uint8_t* slice,
+                                       BlockOf&& block_of) {
+  constexpr int TK = 32;         // keys per tile
+  constexpr int NKS = D / 32;    // k-steps of a score
+  constexpr int NDT = D / 16;    // 16-feature blocks of the output
+  const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
+#pragma unroll
+  for (int c = 0; c < NC; ++c) {
+    st.m[c] = -INFINITY, st.l[c] = 0.f;
+#pragma unroll
+    for (int dt = 0; dt < NDT; ++dt) st.o[c][dt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  }
+  if (n_keys <= 0) return;
+  const int64_t head_elems = (int64_t)B * D;
+  const int n_tiles = (n_keys + TK - 1) / TK, last_block = (n_keys - 1) / B;
+  const int voff = i * B + (8 * g) % B;
+  const bool v_second = 8 * g >= B;
+  constexpr int CH = D / 8, KPL = 64 / CH;  // 16-byte chunks per K row, rows per load
+  constexpr int NKL = 16 / KPL;             // loads per half
+  const int krow = lane / CH, kchunk = lane % CH;
+  const int koff = (8 * (krow >> 2) + (krow & 3)) * D + kchunk * 8;
+  auto slot = [](int r, int chunk) {
+    return r * (D * 2) + ((chunk ^ (CH == 16 ? r & 15 : (r >> 1) & 7)) * 16);
+  };
+  // Each byte of K and V is read by one wave of the workgroup: streamed past the
+  // caches.  Past the range its last block comes again: those keys are not seen.
+  auto block_at = [&](int t, int second) {
+    return ((int64_t)block_of(min(t * (TK / B) + second, last_block)) * hkv + kvh) * head_elems;
+  };
+  uint4 kr[2][NKL], vr[NDT];
+  auto load_k = [&](int t) {
+    const int64_t b0 = block_at(t, 0), b1 = B < TK ? block_at(t, 1) : b0;
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int j = 0; j < NKL; ++j) {
+        const int key0 = 2 * KPL * j + 4 * b;  // the load's first key
+        kr[b][j] = ld_global16_nt(k_cache + (key0 < B ? b0 : b1) + (key0 % B) * D + koff);
+      }
+  };
+  auto load_v = [&](int t) {
+    const int64_t b0 = block_at(t, 0), b1 = B < TK ? block_at(t, 1) : b0;
+    const uint16_t* vp = v_cache + (v_second ? b1 : b0) + voff;
+#pragma unroll
+    for (int dt = 0; dt < NDT; ++dt) vr[dt] = ld_global16_nt(vp + dt * 16 * B);
+  };
+
+  // tile t, with K of tile next requested on the way and V of it at the end
+  auto step = [&](int t, int next) {
+    f32x4_t s[NC][2];
+#pragma unroll
+    for (int c = 0; c < NC; ++c) s[c][0] = s[c][1] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    // a wave's LDS accesses complete in order: no wait but for the data
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int j = 0; j < NKL; ++j)
+        *reinterpret_cast<uint4*>(slice + b * 16 * D * 2 + slot(KPL * j + krow, kchunk)) =
+            kr[b][j];
+    load_k(next);
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+#pragma unroll
+    for (int ks = 0; ks < NKS; ++ks)
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        const uint4 k =
+            *reinterpret_cast<const uint4*>(slice + b * 16 * D * 2 + slot(i, 4 * ks + g));
+#pragma unroll
+        for (int c = 0; c < NC; ++c) s[c][b] = mfma16x16x32(k, qv[c][ks], s[c][b]);
+      }
+    __builtin_amdgcn_wave_barrier();
+    const int left = n_keys - t * TK;  // keys of the tile (wave-uniform)
+    if (left < TK) {  // those past the range may be anything, V included
+      const int mine = left - 8 * g;
+#pragma unroll
+      for (int c = 0; c < NC; ++c)
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (e >= mine) s[c][e >> 2][e & 3] = -INFINITY;
+#pragma unroll
+      for (int dt = 0; dt < NDT; ++dt) {
+        uint32_t* w = reinterpret_cast<uint32_t*>(&vr[dt]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          w[e] &= (2 * e < mine ? 0x0000ffffu : 0u) | (2 * e + 1 < mine ? 0xffff0000u : 0u);
+      }
+    }
+    uint4 pv[NC];
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      float x = fmaxf(fmaxf(fmaxf(s[c][0][0], s[c][0][1]), fmaxf(s[c][0][2], s[c][0][3])),
+                      fmaxf(fmaxf(s[c][1][0], s[c][1][1]), fmaxf(s[c][1][2], s[c][1][3]))) *
+                scale_log2;
+      if (__builtin_amdgcn_ballot_w64(x > st.m[c] + kRescaleThreshold)) {
+        // the four lanes of a row share its maximum
+        x = fmaxf(x, shfl_xor_f(x, 16));
+        x = fmaxf(x, shfl_xor_f(x, 32));
+        const float mnew = fmaxf(st.m[c], x);
+        const float alpha = st.m[c] == -INFINITY ? 0.f : exp2f(st.m[c] - mnew);
+        st.m[c] = mnew;
+        st.l[c] *= alpha;
+#pragma unroll
+        for (int dt = 0; dt < NDT; ++dt) st.o[c][dt] *= alpha;
+      }
+      const float neg_m = st.m[c] == -INFINITY ? 0.f : -st.m[c];  // nothing seen yet
+      uint32_t p[4];  // keys 8 g + 2 e, + 1
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float p0 = __builtin_amdgcn_exp2f(
+            __builtin_fmaf(s[c][e >> 1][2 * (e & 1)], scale_log2, neg_m));
+        const float p1 = __builtin_amdgcn_exp2f(
+            __builtin_fmaf(s[c][e >> 1][2 * (e & 1) + 1], scale_log2, neg_m));
+        p[e] = pack_bf16x2(p0, p1);
+        st.l[c] = dot2_bf16(p[e], 0x3f803f80u, st.l[c]);  // the rounded weights
+      }
+      pv[c] = make_uint4(p[0], p[1], p[2], p[3]);
+    }
+#pragma unroll
+    for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+      for (int c = 0; c < NC; ++c) st.o[c][dt] = mfma16x16x32(vr[dt], pv[c], st.o[c][dt]);
+    load_v(next);
+  };
+
+  // The requests are unconditional (past the range its last tile again, which
+  // is unused), so that the waits on them stay exact.
+  const int last = n_tiles - 1;
+  load_k(min(wave, last));
+  load_v(min(wave, last));
+  for (int t = wave; t < n_tiles; t += kWaves) step(t, min(t + kWaves, last));
+}
+
+// The waves' states of up to kNarrowTile rows in LDS: row r of wave w counts with
+// factor f[w][r] = 2^(m_w - max m) / (sum of all weights so scaled).
+struct Shared {
+  float m[kWaves][kNarrowTile], l[kWaves][kNarrowTile], f[kWaves][kNarrowTile];
+};
+
+// The waves' maxima and sums, and of both the rows' factors: `log_sum(row, x)` gets
+// the log2 of the sum of each row's weights.
+template <int D, int NC, class LogSum>
+__device__ __forceinline__ void join_waves(const State<D, NC>& st, Shared& s, int wave,
+                                           LogSum&& log_sum) {
+  const int tid = threadIdx.x, lane = tid & 63, i = lane & 15, g = lane >> 4;
+#pragma unroll
+  for (int c = 0; c < NC; ++c) {
+    float l = st.l[c];
+    l += shfl_xor_f(l, 16);
+    l += shfl_xor_f(l, 32);
+    if (g == 0) s.m[wave][16 * c + i] = st.m[c], s.l[wave][16 * c + i] = l;
+  }
+  __syncthreads();
+  if (tid < 16 * NC) {
+    float M = -INFINITY, L = 0.f, f[kWaves];
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) M = fmaxf(M, s.m[w][tid]);
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      f[w] = s.m[w][tid] == -INFINITY ? 0.f : exp2f(s.m[w][tid] - M);
+      L += f[w] * s.l[w][tid];
+    }
+    const float inv = L == 0.f ? 0.f : 1.f / L;  // L == 0: it saw no key
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) s.f[w][tid] = f[w] * inv;
+    log_sum(tid, L == 0.f ? -INFINITY : M + __log2f(L));
+  }
+}
+
+// Writes the sums of the waves' outputs, 16 rows at a time: put(row, p, v) gets
+// features 4 p .. 4 p + 3 of each row below m_rows.  slice(w) is wave w's LDS.
+template <int D, int NC, class Slice, class Put>
+__device__ __forceinline__ void write_rows(const State<D, NC>& st, const Shared& s, int wave,
+                                           int m_rows, Slice&& slice, Put&& put) {
+  constexpr int NDT = D / 16;
+  const int tid = threadIdx.x, lane = tid & 63, i = lane & 15, g = lane >> 4;
+#pragma unroll
+  for (int c = 0; c < NC; ++c) {
+    if (16 * c >= m_rows) break;  // uniform
+    __syncthreads();
+    // lane (g, i) holds features 16 dt + 4 g .. + 3 of row i; 16-byte piece p
+    // of row r lies at p ^ r, so that neither side meets a bank twice
+    float* own = reinterpret_cast<float*>(slice(wave));
+#pragma unroll
+    for (int dt = 0; dt < NDT; ++dt)
+      *reinterpret_cast<f32x4_t*>(own + i * D + ((4 * dt + g) ^ i) * 4) = st.o[c][dt];
+    __syncthreads();
+    for (int x = tid; x < 16 * (D / 4); x += kThreads) {
+      const int p = x % (D / 4), r = x / (D / 4);
+      if (16 * c + r >= m_rows) break;  // a thread's rows come in increasing order
+      f32x4_t v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w)
+        v += s.f[w][16 * c + r] *
+             *reinterpret_cast<const f32x4_t*>(reinterpret_cast<const float*>(slice(w)) + r * D +
+                                               (p ^ r) * 4);
+      put(16 * c + r, p, v);
+    }
+  }
+}
+
+// A group's rows over a piece of its common keys.  A workgroup takes kNarrowTile
+// (token, q head) rows of one kv head.
+template <int D, int B, class Slice>
+__device__ __forceinline__ void group_unit(const PrefixRow& row, int unit, const AttnArgs& a,
+                                           const uint16_t* __restrict__ q,
+                                           const uint16_t* __restrict__ k_cache,
+                                           const uint16_t* __restrict__ v_cache,
+                                           const int32_t* __restrict__ bt, Shared& s,
+                                           Slice&& slice) {
+  constexpr int NC = kNarrowTile / 16, NKS = D / 32;
+  const int G = 1 << a.log2_group, all = row.n << a.log2_group;
+  const int tiles = (all + kNarrowTile - 1) / kNarrowTile, m0 = unit % tiles * kNarrowTile;
+  const int kvh = unit / tiles % a.hkv, split = unit / tiles / a.hkv;
+  const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int begin = split * row.split_keys;
+  const int n_keys = min(row.keys - begin, row.split_keys);
+  uint4 qv[NC][NKS];
+#pragma unroll
+  for (int c = 0; c < NC; ++c) {  // past the last row that again (not stored)
+    const int x = min(m0 + 16 * c + i, all - 1);
+    const uint16_t* qb =
+        q + (((int64_t)row.tok0 + (x >> a.log2_group)) * a.hq + kvh * G + (x & (G - 1))) * D + g * 8;
+#pragma unroll
+    for (int ks = 0; ks < NKS; ++ks) qv[c][ks] = ld_global16(qb + ks * 32);
+  }
+  const int32_t* blocks = bt + (int64_t)row.req * a.mbr + begin / B;
+  State<D, NC> st;
+  attend<D, B, NC>(st, qv, n_keys, wave, kvh, a.hkv, a.scale_log2, k_cache, v_cache, slice(wave),
+                   [&](int b) { return blocks[b]; });
+  const int64_t part = (int64_t)row.part0 + ((int64_t)kvh * row.n_split + split) * all + m0;
+  join_waves(st, s, wave, [&](int r, float x) {
+    if (m0 + r < all) a.part_lse[part + r] = x;
+  });
+  write_rows(st, s, wave, min(kNarrowTile, all - m0), slice, [&](int r, int p, const f32x4_t& v) {
+    *reinterpret_cast<f32x4_t*>(a.part_o + (part + r) * D + 4 * p) = v;
+  });
+}
+
+// What a workgroup or a merge needs of row r of a launch.
+struct Own {
+  int32_t tok0, n, start, req, item0;
+  int group;    // the launch's, or -1
+  int keys;     // that are read for the group
+  int n_split;
+  bool alone;   // one piece in all: its workgroup writes the output
+};
+
+template <int B, bool LIST, class Batch>
+__device__ __forceinline__ Own own_of(const Batch& b, const AttnArgs& a, int r) {
+  const AttnRow row = b.r[r];
+  Own o{row.tok0, b.r[r + 1].tok0 - row.tok0, row.start, row.req, row.item0, -1, 0, 1, true};
+  if constexpr (!LIST) {
+    constexpr int NG = sizeof(b.g) / sizeof(PrefixRow);
+    static_assert(NG <= 64, "a group per lane");
+    const int lane = threadIdx.x & 63, g = min(lane, NG - 1);
+    const uint64_t in = __builtin_amdgcn_ballot_w64(lane < a.n_groups && b.g[g].row0 <= r &&
+                                                    r < b.g[g].row1);
+    if (in) {
+      o.group = __builtin_amdgcn_readfirstlane(__ffsll((unsigned long long)in) - 1);
+      o.keys = b.g[o.group].keys;
+    }
+  }
+  const int last = o.start + o.n - 1;
+  const int own = LIST ? min(a.n_pages, last / B + 1) : last + 1 - o.keys;
+  o.n_split = (own - 1) / a.piece + 1;
+  o.alone = o.n_split == 1 && o.group < 0;
+  return o;
+}
+
+// A token's G rows over a piece of its own keys, or (LIST) of its page list, whose
+// blocks of the piece come to s_blocks[kListPages], their number to s_count.
+template <int D, int B, bool LIST, class Slice>
+__device__ __forceinline__ void token_unit(const Own& row, int unit, const AttnArgs& a,
+                                           const uint16_t* __restrict__ q,
+                                           const uint16_t* __restrict__ k_cache,
+                                           const uint16_t* __restrict__ v_cache,
+                                           const int32_t* __restrict__ bt,
+                                           const int32_t* __restrict__ pages, Shared& s,
+                                           int* s_blocks, int* s_count, Slice&& slice) {
+  constexpr int NKS = D / 32;
+  const int kvh = unit % a.hkv, j = unit / a.hkv % row.n, split = unit / a.hkv / row.n;
+  const int G = 1 << a.log2_group, tid = threadIdx.x, lane = tid & 63, i = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int64_t t = (int64_t)row.tok0 + j;
+  const int pos = row.start + j;
+  const int32_t* bt_row = bt + (int64_t)row.req * a.mbr;
+  uint4 qv[1][NKS];
+  {  // past the last row that again (not stored)
+    const uint16_t* qb = q + (t * a.hq + kvh * G + min(i, G - 1)) * D + g * 8;
+#pragma unroll
+    for (int ks = 0; ks < NKS; ++ks) qv[0][ks] = ld_global16(qb + ks * 32);
+  }
+  State<D, 1> st;
+  if constexpr (LIST) {
+    // the piece's entries that count, and their blocks
+    const int e0 = split * a.piece, e1 = min(a.n_pages, e0 + a.piece), top = pos / B;
+    const int32_t* list = pages + (t * a.hkv + kvh) * a.n_pages;
+    if (tid == 0) *s_count = e1;
+    __syncthreads();
+    for (int e = tid; e < e1; e += kThreads) {
+      const int page = list[e], before = e > 0 ? list[e - 1] : -1;
+      if (page < 0 || page <= before || page > top) atomicMin(s_count, e);
+      else if (e >= e0) s_blocks[e - e0] = bt_row[page];
+    }
+    __syncthreads();
+    const int count = *s_count - e0;
+    int n_keys = 0;
+    if (count > 0) {  // only the last entry's page can be p's own
+      n_keys = count * B;
+      if (list[*s_count - 1] == top) n_keys -= B - 1 - pos % B;
+    }
+    attend<D, B, 1>(st, qv, n_keys, wave, kvh, a.hkv, a.scale_log2, k_cache, v_cache, slice(wave),
+                    [&](int b) { return __builtin_amdgcn_readfirstlane(s_blocks[b]); });
+  } else {
+    const int64_t begin = row.keys + (int64_t)split * a.piece;
+    const int n_keys = (int)min((int64_t)a.piece, pos + 1 - begin);  // maybe none
+    const int32_t* blocks = bt_row + begin / B;
+    attend<D, B, 1>(st, qv, n_keys, wave, kvh, a.hkv, a.scale_log2, k_cache, v_cache, slice(wave),
+                    [&](int b) { return blocks[b]; });
+  }
+  const int64_t part = (int64_t)a.part0 + ((int64_t)row.item0 + unit) * G;
+  join_waves(st, s, wave, [&](int r, float x) {
+    if (!row.alone && r < G) a.part_lse[part + r] = x;
+  });
+  write_rows(st, s, wave, G, slice, [&](int r, int p, const f32x4_t& v) {
+    if (row.alone)
+      *reinterpret_cast<uint2*>(a.out + (t * a.hq + kvh * G + r) * D + 4 * p) =
+          make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+    else
+      *reinterpret_cast<f32x4_t*>(a.part_o + (part + r) * D + 4 * p) = v;
+  });
+}
+
+}  // namespace
+
+}  // namespace cpcache

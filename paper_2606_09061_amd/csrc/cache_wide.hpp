@@ -3,11 +3,11 @@
 //
 // A workgroup takes 128 of a kv head's rows, 32 a wave, and a piece of the common
 // keys, 64 at a time, K and V copied straight into LDS.  Every row sees all of
-// them, but for the end of the range.
+// them, but for the end of the range.  Groups of few rows and the tokens' own keys
+// have workgroups of their own (cache_units.hpp) in the same launch.
 #pragma once
 
-#include "cache_device.hpp"
-#include "cache_plan.hpp"
+#include "cache_units.hpp"
 #include "kernels.hpp"
 #include "prefill_tile.hpp"
 
@@ -46,8 +46,8 @@ using cpcache::AttnArgs;  // not cpattn's
 // The pointers come as arguments of their own, which may be restrict: the table's
 // entries are then scalar loads, and no wait for one drains the copies on their way.
 template <int D, int B, int G>
-__global__ __launch_bounds__(2 * kWideTile, 2) void prefix_wide_kernel(
-    const PrefixRows rows, const AttnArgs a, const uint16_t* __restrict__ q,
+__global__ __launch_bounds__(2 * kWideTile, 2) void shared_wide_kernel(
+    const AttnBatch b, const AttnArgs a, const uint16_t* __restrict__ q,
     const uint16_t* __restrict__ k_cache, const uint16_t* __restrict__ v_cache,
     const int32_t* __restrict__ bt, uint16_t* __restrict__ out, float* __restrict__ part_o,
     float* __restrict__ part_lse) {
@@ -64,7 +64,24 @@ __global__ __launch_bounds__(2 * kWideTile, 2) void prefix_wide_kernel(
   __shared__ __attribute__((aligned(1024))) uint8_t vb0[C::TILE_BYTES];
   __shared__ __attribute__((aligned(1024))) uint8_t vb1[C::TILE_BYTES];
 
-  const PrefixRow row = rows.r[row_index(rows, &PrefixRow::item0, (int)blockIdx.x)];
+  __shared__ Shared s;
+  // a wave's slice, half a tile
+  const auto slice = [&](int w) {
+    static_assert(2 * kSlice<D> == C::TILE_BYTES, "slices");
+    return (w < 2 ? kb0 : kb1) + (w & 1) * kSlice<D>;
+  };
+  const int token_item = (int)blockIdx.x - a.group_items;
+  if (token_item >= 0) {
+    const Own own = own_of<B, false>(b, a, row_index(b.r, &AttnRow::item0, token_item));
+    token_unit<D, B, false>(own, token_item - own.item0, a, q, k_cache, v_cache, bt, nullptr, s,
+                            nullptr, nullptr, slice);
+    return;
+  }
+  const PrefixRow& row = b.g[row_index(b.g, &PrefixRow::item0, (int)blockIdx.x)];
+  if (!row.wide) {
+    group_unit<D, B>(row, (int)blockIdx.x - row.item0, a, q, k_cache, v_cache, bt, s, slice);
+    return;
+  }
   constexpr int kTokens = kWideTile / G;  // per tile
   const int tiles = (row.n + kTokens - 1) / kTokens, units = row.n_split * a.hkv;
   // tiles of the same keys go to the same XCD: eight units at a time, tile by tile
@@ -90,13 +107,13 @@ __global__ __launch_bounds__(2 * kWideTile, 2) void prefix_wide_kernel(
 }
 
 template <int D, int B>
-hipError_t launch_prefix_wide_g(const AttnArgs& a, const PrefixRows& rows, int items,
+hipError_t launch_shared_wide_g(const AttnArgs& a, const AttnBatch& b, int items,
                                 hipStream_t s) {
-  auto kern = a.log2_group == 0   ? prefix_wide_kernel<D, B, 1>
-              : a.log2_group == 1 ? prefix_wide_kernel<D, B, 2>
-              : a.log2_group == 2 ? prefix_wide_kernel<D, B, 4>
-                                  : prefix_wide_kernel<D, B, 8>;
-  hipLaunchKernelGGL(kern, dim3(items), dim3(2 * kWideTile), 0, s, rows, a, a.q, a.k_cache,
+  auto kern = a.log2_group == 0   ? shared_wide_kernel<D, B, 1>
+              : a.log2_group == 1 ? shared_wide_kernel<D, B, 2>
+              : a.log2_group == 2 ? shared_wide_kernel<D, B, 4>
+                                  : shared_wide_kernel<D, B, 8>;
+  hipLaunchKernelGGL(kern, dim3(items), dim3(2 * kWideTile), 0, s, b, a, a.q, a.k_cache,
                      a.v_cache, a.bt, a.out, a.part_o, a.part_lse);
   return hipGetLastError();
 }

@@ -62,19 +62,17 @@ void check(const cp_attn_desc& d, const std::vector<cp_row_meta>& rows,
     CHECK(p.ws_bytes >= 256 && p.off_lse + (size_t)p.partial_rows * 4 <= p.ws_bytes);
     CHECK(p.off_lse == (size_t)p.partial_rows * d.head_dim * 4);
     CHECK(p.piece >= 1 && (which || p.piece <= kListPages));
-    CHECK(p.wide.size() == p.prefix.size() && p.group_rows.size() == p.prefix.size());
     std::vector<Range> parts;
     for (size_t i = 0; i < p.prefix.size(); ++i) {
       const PrefixRow& g = p.prefix[i];
-      const int64_t turn = p.wide[i] ? kWideTurn : kTurn;
+      const int64_t turn = p.prefix[i].wide ? kWideTurn : kTurn;
       CHECK(g.n >= 1 && g.keys >= B && g.keys % B == 0 && g.split_keys >= 1);
       CHECK(g.n_split >= 1 && g.n_split <= kMaxGroupSplits);
       CHECK((int64_t)g.n_split * g.split_keys >= g.keys && (int64_t)(g.n_split - 1) * g.split_keys < g.keys);
       CHECK(g.n_split == 1 || g.split_keys % turn == 0);
       CHECK(g.part0 >= 0);
       parts.push_back({g.part0, (int64_t)g.n_split * g.n * hq});
-      CHECK(p.rows[p.group_rows[i]].tok0 == g.tok0 && p.rows[p.group_rows[i]].group == (int)i);
-      CHECK(prefix_items(g, p.wide[i], hq / hkv, hkv) <= kMaxItems);
+      CHECK(prefix_items(g, hq / hkv, hkv) <= kMaxItems);
     }
     size_t at = 0;
     int32_t tok = 0, group = -1;
@@ -91,7 +89,7 @@ void check(const cp_attn_desc& d, const std::vector<cp_row_meta>& rows,
         if (which) {
           own = (int64_t)r.start + r.n;
           if (r.group >= 0) {
-            CHECK(r.group >= group);  // rising
+            CHECK(r.group == group || (r.group == group + 1 && r.tok0 == p.prefix[r.group].tok0));
             group = r.group;
             const PrefixRow& g = p.prefix[r.group];
             CHECK(g.keys <= r.start && r.tok0 >= g.tok0 && r.tok0 + r.n <= g.tok0 + g.n);
@@ -104,12 +102,12 @@ void check(const cp_attn_desc& d, const std::vector<cp_row_meta>& rows,
         CHECK((int64_t)r.n_split * r.n * hkv <= kMaxItems);
         CHECK(r.n_split == 1 || !which || p.piece % B == 0);
         own_parts += (int64_t)r.n_split * r.n * hq;
-        split |= r.n_split > 1;
+        split |= r.n_split > 1 || r.group >= 0;
         j += r.n;
       }
       tok += m.chunk_len;
     }
-    CHECK(at == p.rows.size() && split == p.split);
+    CHECK(at == p.rows.size() && split == p.parts);
     if (split) parts.push_back({p.row_part0, own_parts});
     no_overlap(parts, p.partial_rows);
   }

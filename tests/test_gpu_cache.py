@@ -533,6 +533,20 @@ def test_prefix_attn_numbers_of_rows(n):
     c.check(c.prefix(), f"{n} groups")
 
 
+@pytest.mark.parametrize("hq,hkv,d,block", [(4, 2, 64, 16), (8, 1, 128, 16)])
+def test_prefix_attn_of_groups_over_several_launches(hq, hkv, d, block):
+    """A group of more rows than a launch has, wide and narrow ones behind it, and
+    more groups than a launch has."""
+    rows = [(90 + i % 7, 1) for i in range(170)] + [(40 + i, 1) for i in range(2)]
+    groups = [(0, 170, 90), (170, 2, 35)]
+    for g in range(60):
+        n = [1, 3, 40][g % 3]
+        groups.append((len(rows), n, 16 + 5 * (g % 8)))
+        rows += [(60 + g, 1 + g % 2) for _ in range(n)]
+    c = Case(hq, hkv, d, block, rows, d, groups=groups)
+    c.check(c.prefix(), f"{len(rows)} rows, {len(groups)} groups")
+
+
 def test_prefix_attn_without_groups():
     c = Case(8, 2, 128, 16, [(500, 1), (0, 3), (70, 20)], 7)
     c.check(c.prefix(), "no groups")
