@@ -48,10 +48,11 @@ using SelectRows = RowsOf<SelectRow, kSelectRows>;
 // A piece of a row of cp_page_attn or cp_prefix_attn.  A launch's rows follow each
 // other: the next one's first token ends a row, and the place behind the last row
 // holds the launch's end.  With `own` keys (or entries of a list) of its last
-// token, a row has ceil(own / piece) pieces, and the partial rows of its
-// workgroup x are (item0 + x) G and on, behind those of the launches before.
+// token, a row has ceil(own / piece) pieces, and the partial rows of its item x,
+// (piece, token, kv head), are (item0 + x) G and on, behind those of the launches
+// before.
 struct AttnRow {     // 16 bytes
-  int32_t item0;     // the launch's workgroups of rows before it
+  int32_t item0;     // the launch's items of rows before it
   int32_t tok0, start, req;
 };
 

@@ -202,6 +202,8 @@ AttnArgs attn_args(const cp_attn_desc* d, const AttnPlan& p, const void* q, cons
                   p.piece,
                   0,
                   0,
+                  p.unit_waves,
+                  0,
                   0,
                   d->sm_scale * cpattn::kLog2e};
 }
@@ -215,7 +217,7 @@ int launch_plan(const cp_attn_desc* d, const AttnPlan& p, AttnArgs a, hipStream_
   for (size_t r = 0; r < p.rows.size();) {
     AttnBatch b;
     int64_t items = 0, group_items = 0;
-    int n = 0, n_groups = 0, last = -1;
+    int n = 0, n_groups = 0, last = -1, most = 1;
     bool merge = false, wide = false;
     const size_t first = r;
     for (; r < p.rows.size() && n < kAttnRows; ++r) {
@@ -238,20 +240,23 @@ int launch_plan(const cp_attn_desc* d, const AttnPlan& p, AttnArgs a, hipStream_
       if (t.group >= 0) b.g[n_groups - 1].row1 = n + 1;
       b.r[n++] = AttnRow{(int32_t)items, t.tok0, t.start, t.req};
       items += more;
+      const int pieces = t.n_split + (t.group >= 0 ? p.prefix[t.group].n_split : 0);
       merge |= t.n_split > 1 || t.group >= 0;
+      most = std::max(most, pieces);
     }
     const int32_t end = p.rows[r - 1].tok0 + p.rows[r - 1].n;
     for (int i = n_groups; i < kGroups; ++i) b.g[i] = PrefixRow{}, b.g[i].item0 = INT_MAX;
     for (int i = n; i <= kAttnRows; ++i) b.r[i] = AttnRow{INT_MAX, end, 0, 0};
     a.part0 = (int)part0, a.n_groups = n_groups, a.group_items = (int)group_items;
-    const int all = (int)(items + group_items);
+    a.items = (int)items;
+    const int per = 4 / p.unit_waves, all = (int)(group_items + (items + per - 1) / per);
     const hipError_t e = a.pages    ? launch_pages(D, B, a, b, n, all, s)
                          : !wide    ? launch_shared(D, B, a, b, n, all, s)
                          : D == 128 ? launch_shared_wide128(B, a, b, all, s)
                                     : launch_shared_wide64(B, a, b, all, s);
     int rc = finish(e, s);
     if (rc == CP_OK && merge)
-      rc = finish(launch_cache_merge(D, B, a, b, n, end - p.rows[first].tok0, s), s);
+      rc = finish(launch_cache_merge(D, B, a, b, n, end - p.rows[first].tok0, most, s), s);
     if (rc != CP_OK) return rc;
     if (p.parts) part0 += items * G;
   }

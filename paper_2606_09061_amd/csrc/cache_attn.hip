@@ -13,10 +13,9 @@ __global__ __launch_bounds__(kThreads, 2) void pages_kernel(
     const int32_t* __restrict__ bt, const int32_t* __restrict__ pages) {
   __shared__ __align__(16) uint8_t slices[kWaves][kSlice<D>];
   __shared__ Shared s;
-  __shared__ int s_blocks[kListPages], s_count;
-  const Own row = own_of<B, true>(b, a, row_index(b.r, &AttnRow::item0, (int)blockIdx.x));
-  token_unit<D, B, true>(row, (int)blockIdx.x - row.item0, a, q, k_cache, v_cache, bt, pages, s,
-                         s_blocks, &s_count, [&](int w) { return slices[w]; });
+  __shared__ int s_blocks[kWaves][kListPages], s_count[kWaves];
+  token_units<D, B, true>(b, (int)blockIdx.x, a, q, k_cache, v_cache, bt, pages, s, s_blocks,
+                          s_count, [&](int w) { return slices[w]; });
 }
 
 // The groups' workgroups come first, the tokens' behind them.
@@ -34,39 +33,53 @@ __global__ __launch_bounds__(kThreads, 2) void shared_kernel(
     group_unit<D, B>(row, (int)blockIdx.x - row.item0, a, q, k_cache, v_cache, bt, s, slice);
     return;
   }
-  const Own row = own_of<B, false>(b, a, row_index(b.r, &AttnRow::item0, x));
-  token_unit<D, B, false>(row, x - row.item0, a, q, k_cache, v_cache, bt, nullptr, s, nullptr,
-                          nullptr, slice);
+  token_units<D, B, false>(b, x, a, q, k_cache, v_cache, bt, nullptr, s, nullptr, nullptr, slice);
 }
 
 // Merge of several pieces: with O_s and L_s, a piece's normalised output and the
 // log2 of its weights' sum, the row's output is
 //     sum_s 2^(L_s - max L) O_s / sum_s 2^(L_s - max L),
-// over its own pieces and its group's.  A row (token, q head) takes D / 4
-// threads of 4 features; a workgroup's rows are one token's.
+// over its own pieces and its group's.  A row (token, q head) takes `share` times
+// D / 4 threads of 4 features, each of which takes every share-th piece; they meet
+// in LDS.  A workgroup's rows are one token's.
 template <int D, int B, bool LIST, class Batch>
 __global__ __launch_bounds__(kThreads) void cache_merge_kernel(const Batch b, const AttnArgs a,
-                                                               int per_token) {
-  constexpr int DQ = D / 4, PER = kThreads / DQ, U = 8;
+                                                               int per_token, int share) {
+  constexpr int DQ = D / 4, SLOTS = kThreads / DQ, U = 8;
+  __shared__ f32x4_t s_acc[SLOTS][DQ];
+  __shared__ float s_m[SLOTS], s_w[SLOTS];
   const int64_t t = (int64_t)b.r[0].tok0 + (int)blockIdx.x / per_token;
   const Own row = own_of<B, LIST>(b, a, row_index(b.r, &AttnRow::tok0, (int)t));
   if (row.alone) return;
-  const int h = (int)blockIdx.x % per_token * PER + threadIdx.x / DQ, dq = threadIdx.x % DQ;
-  if (h >= a.hq) return;
+  const int slot = threadIdx.x / DQ, dq = threadIdx.x % DQ, per = SLOTS / share, p = slot / per;
+  const int h = (int)blockIdx.x % per_token * per + slot % per;
   const int j = (int)(t - row.tok0), kvh = h >> a.log2_group, G = 1 << a.log2_group;
   const int e = h & (G - 1);
   float M = -INFINITY, W = 0.f;
   f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
-  const auto add = [&](int64_t first, int64_t stride, int n) {
-    for (int s0 = 0; s0 < n; s0 += U) {
+  if (h < a.hq) {
+    // workgroup (split, j, kvh) of the row's launch wrote its G rows; pieces
+    // [0, own) are the row's, those behind them the group's
+    const int64_t first = a.part0 + ((int64_t)row.item0 + (int64_t)j * a.hkv + kvh) * G + e;
+    const int64_t stride = (int64_t)row.n * a.hq;
+    int own = row.n_split, n = own;
+    int64_t gfirst = 0, gstride = 0;
+    if (row.group >= 0) {
+      const PrefixRow& g = b.g[row.group];
+      gstride = (int64_t)g.n * G;
+      gfirst = g.part0 + kvh * g.n_split * gstride + (t - g.tok0) * G + e;
+      n += g.n_split;
+    }
+    for (int s0 = p; s0 < n; s0 += share * U) {
       float ls[U];
       f32x4_t o[U];
 #pragma unroll
       for (int u = 0; u < U; ++u) {  // past the last piece: it again, weight 0
-        const int64_t pr = first + min(s0 + u, n - 1) * stride;
+        const int s = min(s0 + u * share, n - 1);
+        const int64_t pr = s < own ? first + s * stride : gfirst + (s - own) * gstride;
         ls[u] = a.part_lse[pr];
         o[u] = *reinterpret_cast<const f32x4_t*>(a.part_o + pr * D + dq * 4);
-        if (s0 + u >= n) ls[u] = -INFINITY;
+        if (s0 + u * share >= n) ls[u] = -INFINITY;
       }
       float m = M;
 #pragma unroll
@@ -83,15 +96,24 @@ __global__ __launch_bounds__(kThreads) void cache_merge_kernel(const Batch b, co
         acc += w * o[u];
       }
     }
-  };
-  // workgroup (split, j, kvh) of the row's launch wrote its G rows
-  const int64_t unit = (int64_t)row.item0 + (int64_t)j * a.hkv + kvh;
-  add(a.part0 + unit * G + e, (int64_t)row.n * a.hq, row.n_split);
-  if (row.group >= 0) {
-    const PrefixRow& g = b.g[row.group];
-    const int64_t all = (int64_t)g.n * G;
-    add(g.part0 + kvh * g.n_split * all + (t - g.tok0) * G + e, all, g.n_split);
   }
+  if (share > 1) {  // uniform
+    s_acc[slot][dq] = acc;
+    if (dq == 0) s_m[slot] = M, s_w[slot] = W;
+    __syncthreads();
+    if (p > 0) return;
+    for (int k = 1; k < share; ++k) M = fmaxf(M, s_m[k * per + slot]);
+    W = 0.f;
+    acc = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    for (int k = 0; k < share; ++k) {
+      const float wk = s_w[k * per + slot];
+      if (wk == 0.f) continue;
+      const float w = exp2f(s_m[k * per + slot] - M);
+      W += w * wk;
+      acc += w * s_acc[k * per + slot][dq];
+    }
+  }
+  if (h >= a.hq) return;
   const float inv = W == 0.f ? 0.f : 1.f / W;
   *reinterpret_cast<uint2*>(a.out + (t * a.hq + h) * D + dq * 4) =
       make_uint2(pack_bf16x2(acc[0] * inv, acc[1] * inv), pack_bf16x2(acc[2] * inv, acc[3] * inv));
@@ -117,15 +139,20 @@ hipError_t launch_shared_t(const AttnArgs& a, const AttnBatch& b, int n_rows, in
 
 template <int D, int B>
 hipError_t launch_merge_t(const AttnArgs& a, const AttnBatch& b, int n_rows, int n_tokens,
-                          hipStream_t s) {
-  const int per_token = (a.hq * (D / 4) + kThreads - 1) / kThreads;
+                          int most, hipStream_t s) {
+  constexpr int SLOTS = kThreads / (D / 4);
+  int share = 1;  // of eight pieces each, which a thread loads at once
+  while (share < SLOTS && share * 8 < most &&
+         (int64_t)n_tokens * a.hq * 2 * share / SLOTS < kMaxItems / 2)
+    share *= 2;
+  const int per = SLOTS / share, per_token = (a.hq + per - 1) / per;
   return by_size(b, a.n_groups, n_rows, [&](const auto& x) {
     if (a.pages)
       hipLaunchKernelGGL((cache_merge_kernel<D, B, true>), dim3(n_tokens * per_token),
-                         dim3(kThreads), 0, s, x, a, per_token);
+                         dim3(kThreads), 0, s, x, a, per_token, share);
     else
       hipLaunchKernelGGL((cache_merge_kernel<D, B, false>), dim3(n_tokens * per_token),
-                         dim3(kThreads), 0, s, x, a, per_token);
+                         dim3(kThreads), 0, s, x, a, per_token, share);
   });
 }
 
@@ -146,10 +173,10 @@ hipError_t launch_shared(int d, int block, const AttnArgs& a, const AttnBatch& b
 }
 
 hipError_t launch_cache_merge(int d, int block, const AttnArgs& a, const AttnBatch& b, int n_rows,
-                              int n_tokens, hipStream_t s) {
+                              int n_tokens, int most, hipStream_t s) {
   auto f = d == 128 ? (block == 16 ? launch_merge_t<128, 16> : launch_merge_t<128, 32>)
                     : (block == 16 ? launch_merge_t<64, 16> : launch_merge_t<64, 32>);
-  return f(a, b, n_rows, n_tokens, s);
+  return f(a, b, n_rows, n_tokens, most, s);
 }
 
 }  // namespace cpcache

@@ -49,7 +49,8 @@ struct AttnArgs {
   float* part_o;         // [partial rows][D], normalised
   float* part_lse;       // [partial rows], log2 of the weights' sum
   int hq, hkv, mbr, log2_group, n_pages, piece;
-  int part0;             // the partial rows of the launch's first workgroup of rows
+  int part0;             // the partial rows of the launch's first item of rows
+  int items, unit_waves; // the launch's (token, kv head, piece) items, and waves of each
   int n_groups;          // of the launch
   int group_items;       // its first workgroups, which are the groups'
   float scale_log2;      // sm_scale * log2(e)
@@ -76,8 +77,9 @@ hipError_t launch_shared_wide64(int block, const AttnArgs& a, const AttnBatch& b
                                 hipStream_t s);
 hipError_t launch_shared_wide128(int block, const AttnArgs& a, const AttnBatch& b, int items,
                                  hipStream_t s);
-// the merge of the same batch's rows that have several pieces, of n_tokens tokens
+// the merge of the same batch's rows that have several pieces, `most` at most, of
+// n_tokens tokens
 hipError_t launch_cache_merge(int d, int block, const AttnArgs& a, const AttnBatch& b, int n_rows,
-                              int n_tokens, hipStream_t s);
+                              int n_tokens, int most, hipStream_t s);
 
 }  // namespace cpcache

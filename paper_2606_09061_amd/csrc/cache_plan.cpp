@@ -15,6 +15,9 @@ using cptree::ceil_div;
 // Work beyond so many workgroups is not cut: they fill the GPU eight times.
 constexpr int64_t kUncut = 8 * cptree::kSlots;
 
+// Items up to which four waves share one, and two.
+constexpr int64_t kUnitWaves4 = 512, kUnitWaves2 = 768;
+
 // Times of the attention kernels (pieces.hpp), in us.
 cptree::Cost cost_of(int d, bool wide, double memory) {
   const double x = d / 128.0;
@@ -59,12 +62,14 @@ bool cut_rows(AttnPlan& out, const cp_attn_desc& d, double keys, int per_turn, i
     const int turns = cptree::best_piece(work, cost_of(d.head_dim, false, memory_us(d, keys)), &time);
     out.piece = (int)std::min<int64_t>(most, (int64_t)std::max(1, turns) * per_turn);
   }
-  int64_t partial = 0;
+  int64_t partial = 0, items = 0;
   for (TokenRow& r : out.rows) {
     r.n_split = (int)ceil_div(own(r), out.piece);
     out.parts |= r.n_split > 1 || r.group >= 0;
     partial += (int64_t)r.n_split * r.n * d.num_q_heads;
+    items += (int64_t)r.n_split * r.n * d.num_kv_heads;
   }
+  out.unit_waves = items <= kUnitWaves4 ? 4 : items <= kUnitWaves2 ? 2 : 1;
   out.row_part0 = (int32_t)std::min<int64_t>(out.partial_rows, INT32_MAX);
   if (out.parts) out.partial_rows += partial;
   if (out.partial_rows > INT32_MAX) return false;

@@ -36,6 +36,7 @@ struct TokenRow {    // a piece of a row's tokens
 struct AttnPlan {
   std::vector<TokenRow> rows;       // in the order of their tokens
   std::vector<PrefixRow> prefix;    // of the groups that share something
+  int unit_waves = 4;               // waves of a (token, kv head, piece) item: 1, 2 or 4
   int piece = 0;                    // keys, or entries of a list, of a piece of the rows' ranges
   bool parts = false;               // some row has several, and all have partial rows
   int32_t row_part0 = 0;            // the first of them; the groups' come before

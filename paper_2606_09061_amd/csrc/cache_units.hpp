@@ -52,15 +52,15 @@ struct State {
   f32x4_t o[NC][D / 16];
 };
 
-// Attends the wave's rows qv to keys [0, n_keys) of consecutive blocks, of which
-// wave w takes tiles of 32 keys w, w + 4, ...; block_of(i) is the i-th block's
+// Attends the wave's rows qv to keys [0, n_keys) of consecutive blocks, of which it
+// takes tiles of 32 keys first, first + stride, ...; block_of(i) is the i-th block's
 // place in the pool, for i below the blocks that n_keys fill.  K and V are
 // loaded as they lie in memory, K's rows passing through `slice`, LDS that only
 // this wave uses.  K of the next tile is on its way from there on, V from the
 // end of a tile to the product with it in the next.
 template <int D, int B, int NC, class BlockOf>
 __device__ __forceinline__ void attend(State<D, NC>& st, const uint4 (&qv)[NC][D / 32], int n_keys,
-                                       int wave, int kvh, int hkv, float scale_log2,
+                                       int first, int stride, int kvh, int hkv, float scale_log2,
                                        const uint16_t* __restrict__ k_cache,
                                        const uint16_t* __restrict__ v_cache, uint8_t* slice,
                                        BlockOf&& block_of) {
@@ -191,9 +191,9 @@ __device__ __forceinline__ void attend(State<D, NC>& st, const uint4 (&qv)[NC][D
   // The requests are unconditional (past the range its last tile again, which
   // is unused), so that the waits on them stay exact.
   const int last = n_tiles - 1;
-  load_k(min(wave, last));
-  load_v(min(wave, last));
-  for (int t = wave; t < n_tiles; t += kWaves) step(t, min(t + kWaves, last));
+  load_k(min(first, last));
+  load_v(min(first, last));
+  for (int t = first; t < n_tiles; t += stride) step(t, min(t + stride, last));
 }
 
 // The waves' states of up to kNarrowTile rows in LDS: row r of wave w counts with
@@ -202,12 +202,13 @@ struct Shared {
   float m[kWaves][kNarrowTile], l[kWaves][kNarrowTile], f[kWaves][kNarrowTile];
 };
 
-// The waves' maxima and sums, and of both the rows' factors: `log_sum(row, x)` gets
-// the log2 of the sum of each row's weights.
+// The maxima and sums of `waves` waves from wave w0 on, which share 16 NC rows, and
+// from them the rows' factors; x counts the threads of those waves.
+// log_sum(row, y) gets the log2 of the sum of each row's weights.
 template <int D, int NC, class LogSum>
-__device__ __forceinline__ void join_waves(const State<D, NC>& st, Shared& s, int wave,
-                                           LogSum&& log_sum) {
-  const int tid = threadIdx.x, lane = tid & 63, i = lane & 15, g = lane >> 4;
+__device__ __forceinline__ void join_waves(const State<D, NC>& st, Shared& s, int wave, int w0,
+                                           int waves, int x, LogSum&& log_sum) {
+  const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
 #pragma unroll
   for (int c = 0; c < NC; ++c) {
     float l = st.l[c];
@@ -216,29 +217,28 @@ __device__ __forceinline__ void join_waves(const State<D, NC>& st, Shared& s, in
     if (g == 0) s.m[wave][16 * c + i] = st.m[c], s.l[wave][16 * c + i] = l;
   }
   __syncthreads();
-  if (tid < 16 * NC) {
-    float M = -INFINITY, L = 0.f, f[kWaves];
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) M = fmaxf(M, s.m[w][tid]);
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-      f[w] = s.m[w][tid] == -INFINITY ? 0.f : exp2f(s.m[w][tid] - M);
-      L += f[w] * s.l[w][tid];
+  if (x < 16 * NC) {
+    float M = -INFINITY, L = 0.f;
+    for (int w = w0; w < w0 + waves; ++w) M = fmaxf(M, s.m[w][x]);
+    for (int w = w0; w < w0 + waves; ++w) {
+      const float f = s.m[w][x] == -INFINITY ? 0.f : exp2f(s.m[w][x] - M);
+      s.f[w][x] = f;
+      L += f * s.l[w][x];
     }
     const float inv = L == 0.f ? 0.f : 1.f / L;  // L == 0: it saw no key
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) s.f[w][tid] = f[w] * inv;
-    log_sum(tid, L == 0.f ? -INFINITY : M + __log2f(L));
+    for (int w = w0; w < w0 + waves; ++w) s.f[w][x] *= inv;
+    log_sum(x, L == 0.f ? -INFINITY : M + __log2f(L));
   }
 }
 
-// Writes the sums of the waves' outputs, 16 rows at a time: put(row, p, v) gets
+// Writes the sums of those waves' outputs, 16 rows at a time: put(row, p, v) gets
 // features 4 p .. 4 p + 3 of each row below m_rows.  slice(w) is wave w's LDS.
 template <int D, int NC, class Slice, class Put>
 __device__ __forceinline__ void write_rows(const State<D, NC>& st, const Shared& s, int wave,
-                                           int m_rows, Slice&& slice, Put&& put) {
+                                           int w0, int waves, int x0, int m_rows, Slice&& slice,
+                                           Put&& put) {
   constexpr int NDT = D / 16;
-  const int tid = threadIdx.x, lane = tid & 63, i = lane & 15, g = lane >> 4;
+  const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
 #pragma unroll
   for (int c = 0; c < NC; ++c) {
     if (16 * c >= m_rows) break;  // uniform
@@ -246,16 +246,16 @@ __device__ __forceinline__ void write_rows(const State<D, NC>& st, const Shared&
     // lane (g, i) holds features 16 dt + 4 g .. + 3 of row i; 16-byte piece p
     // of row r lies at p ^ r, so that neither side meets a bank twice
     float* own = reinterpret_cast<float*>(slice(wave));
+    if (16 * c + i < m_rows)
 #pragma unroll
-    for (int dt = 0; dt < NDT; ++dt)
-      *reinterpret_cast<f32x4_t*>(own + i * D + ((4 * dt + g) ^ i) * 4) = st.o[c][dt];
+      for (int dt = 0; dt < NDT; ++dt)
+        *reinterpret_cast<f32x4_t*>(own + i * D + ((4 * dt + g) ^ i) * 4) = st.o[c][dt];
     __syncthreads();
-    for (int x = tid; x < 16 * (D / 4); x += kThreads) {
+    for (int x = x0; x < 16 * (D / 4); x += 64 * waves) {
       const int p = x % (D / 4), r = x / (D / 4);
       if (16 * c + r >= m_rows) break;  // a thread's rows come in increasing order
       f32x4_t v = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int w = 0; w < kWaves; ++w)
+      for (int w = w0; w < w0 + waves; ++w)
         v += s.f[w][16 * c + r] *
              *reinterpret_cast<const f32x4_t*>(reinterpret_cast<const float*>(slice(w)) + r * D +
                                                (p ^ r) * 4);
@@ -292,15 +292,16 @@ __device__ __forceinline__ void group_unit(const PrefixRow& row, int unit, const
   }
   const int32_t* blocks = bt + (int64_t)row.req * a.mbr + begin / B;
   State<D, NC> st;
-  attend<D, B, NC>(st, qv, n_keys, wave, kvh, a.hkv, a.scale_log2, k_cache, v_cache, slice(wave),
-                   [&](int b) { return blocks[b]; });
+  attend<D, B, NC>(st, qv, n_keys, wave, kWaves, kvh, a.hkv, a.scale_log2, k_cache, v_cache,
+                   slice(wave), [&](int b) { return blocks[b]; });
   const int64_t part = (int64_t)row.part0 + ((int64_t)kvh * row.n_split + split) * all + m0;
-  join_waves(st, s, wave, [&](int r, float x) {
+  join_waves(st, s, wave, 0, kWaves, threadIdx.x, [&](int r, float x) {
     if (m0 + r < all) a.part_lse[part + r] = x;
   });
-  write_rows(st, s, wave, min(kNarrowTile, all - m0), slice, [&](int r, int p, const f32x4_t& v) {
-    *reinterpret_cast<f32x4_t*>(a.part_o + (part + r) * D + 4 * p) = v;
-  });
+  write_rows(st, s, wave, 0, kWaves, threadIdx.x, min(kNarrowTile, all - m0), slice,
+             [&](int r, int p, const f32x4_t& v) {
+               *reinterpret_cast<f32x4_t*>(a.part_o + (part + r) * D + 4 * p) = v;
+             });
 }
 
 // What a workgroup or a merge needs of row r of a launch.
@@ -334,20 +335,28 @@ __device__ __forceinline__ Own own_of(const Batch& b, const AttnArgs& a, int r) 
   return o;
 }
 
-// A token's G rows over a piece of its own keys, or (LIST) of its page list, whose
-// blocks of the piece come to s_blocks[kListPages], their number to s_count.
-template <int D, int B, bool LIST, class Slice>
-__device__ __forceinline__ void token_unit(const Own& row, int unit, const AttnArgs& a,
-                                           const uint16_t* __restrict__ q,
-                                           const uint16_t* __restrict__ k_cache,
-                                           const uint16_t* __restrict__ v_cache,
-                                           const int32_t* __restrict__ bt,
-                                           const int32_t* __restrict__ pages, Shared& s,
-                                           int* s_blocks, int* s_count, Slice&& slice) {
+// A workgroup of tokens: each of its units, taken by a.unit_waves waves, is a token's
+// G rows over a piece of its own keys, or (LIST) of its page list, whose blocks of
+// the piece come to s_blocks, their number to s_count.
+template <int D, int B, bool LIST, class Batch, class Slice>
+__device__ __forceinline__ void token_units(const Batch& b, int block, const AttnArgs& a,
+                                            const uint16_t* __restrict__ q,
+                                            const uint16_t* __restrict__ k_cache,
+                                            const uint16_t* __restrict__ v_cache,
+                                            const int32_t* __restrict__ bt,
+                                            const int32_t* __restrict__ pages, Shared& s,
+                                            int (*s_blocks)[kListPages], int* s_count,
+                                            Slice&& slice) {
   constexpr int NKS = D / 32;
-  const int kvh = unit % a.hkv, j = unit / a.hkv % row.n, split = unit / a.hkv / row.n;
-  const int G = 1 << a.log2_group, tid = threadIdx.x, lane = tid & 63, i = lane & 15, g = lane >> 4;
+  const int tid = threadIdx.x, lane = tid & 63, i = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int W = a.unit_waves, mine = wave / W, w0 = mine * W, x = tid - 64 * w0;
+  const int item = block * (kWaves / W) + mine;
+  const bool real = item < a.items;  // the last workgroup may have fewer units
+  const Own row = own_of<B, LIST>(b, a, row_index(b.r, &AttnRow::item0, min(item, a.items - 1)));
+  const int unit = min(item, a.items - 1) - row.item0;
+  const int kvh = unit % a.hkv, j = unit / a.hkv % row.n, split = unit / a.hkv / row.n;
+  const int G = 1 << a.log2_group;
   const int64_t t = (int64_t)row.tok0 + j;
   const int pos = row.start + j;
   const int32_t* bt_row = bt + (int64_t)row.req * a.mbr;
@@ -358,38 +367,41 @@ __device__ __forceinline__ void token_unit(const Own& row, int unit, const AttnA
     for (int ks = 0; ks < NKS; ++ks) qv[0][ks] = ld_global16(qb + ks * 32);
   }
   State<D, 1> st;
+  int n_keys = 0;
   if constexpr (LIST) {
     // the piece's entries that count, and their blocks
     const int e0 = split * a.piece, e1 = min(a.n_pages, e0 + a.piece), top = pos / B;
     const int32_t* list = pages + (t * a.hkv + kvh) * a.n_pages;
-    if (tid == 0) *s_count = e1;
+    if (x == 0) s_count[mine] = e1;
     __syncthreads();
-    for (int e = tid; e < e1; e += kThreads) {
+    for (int e = x; e < e1; e += 64 * W) {
       const int page = list[e], before = e > 0 ? list[e - 1] : -1;
-      if (page < 0 || page <= before || page > top) atomicMin(s_count, e);
-      else if (e >= e0) s_blocks[e - e0] = bt_row[page];
+      if (page < 0 || page <= before || page > top) atomicMin(&s_count[mine], e);
+      else if (e >= e0) s_blocks[mine][e - e0] = bt_row[page];
     }
     __syncthreads();
-    const int count = *s_count - e0;
-    int n_keys = 0;
+    const int end = s_count[mine], count = end - e0;
     if (count > 0) {  // only the last entry's page can be p's own
       n_keys = count * B;
-      if (list[*s_count - 1] == top) n_keys -= B - 1 - pos % B;
+      if (list[end - 1] == top) n_keys -= B - 1 - pos % B;
     }
-    attend<D, B, 1>(st, qv, n_keys, wave, kvh, a.hkv, a.scale_log2, k_cache, v_cache, slice(wave),
-                    [&](int b) { return __builtin_amdgcn_readfirstlane(s_blocks[b]); });
+    const int* blocks = s_blocks[mine];
+    attend<D, B, 1>(st, qv, real ? n_keys : 0, wave - w0, W, kvh, a.hkv, a.scale_log2, k_cache,
+                    v_cache, slice(wave),
+                    [&](int b) { return __builtin_amdgcn_readfirstlane(blocks[b]); });
   } else {
     const int64_t begin = row.keys + (int64_t)split * a.piece;
-    const int n_keys = (int)min((int64_t)a.piece, pos + 1 - begin);  // maybe none
+    n_keys = (int)min((int64_t)a.piece, pos + 1 - begin);  // maybe none
     const int32_t* blocks = bt_row + begin / B;
-    attend<D, B, 1>(st, qv, n_keys, wave, kvh, a.hkv, a.scale_log2, k_cache, v_cache, slice(wave),
-                    [&](int b) { return blocks[b]; });
+    attend<D, B, 1>(st, qv, real ? n_keys : 0, wave - w0, W, kvh, a.hkv, a.scale_log2, k_cache,
+                    v_cache, slice(wave), [&](int b) { return blocks[b]; });
   }
   const int64_t part = (int64_t)a.part0 + ((int64_t)row.item0 + unit) * G;
-  join_waves(st, s, wave, [&](int r, float x) {
-    if (!row.alone && r < G) a.part_lse[part + r] = x;
+  join_waves(st, s, wave, w0, W, x, [&](int r, float y) {
+    if (real && !row.alone && r < G) a.part_lse[part + r] = y;
   });
-  write_rows(st, s, wave, G, slice, [&](int r, int p, const f32x4_t& v) {
+  write_rows(st, s, wave, w0, W, x, G, slice, [&](int r, int p, const f32x4_t& v) {
+    if (!real) return;
     if (row.alone)
       *reinterpret_cast<uint2*>(a.out + (t * a.hq + kvh * G + r) * D + 4 * p) =
           make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));

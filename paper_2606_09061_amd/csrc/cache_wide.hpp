@@ -72,9 +72,8 @@ __global__ __launch_bounds__(2 * kWideTile, 2) void shared_wide_kernel(
   };
   const int token_item = (int)blockIdx.x - a.group_items;
   if (token_item >= 0) {
-    const Own own = own_of<B, false>(b, a, row_index(b.r, &AttnRow::item0, token_item));
-    token_unit<D, B, false>(own, token_item - own.item0, a, q, k_cache, v_cache, bt, nullptr, s,
-                            nullptr, nullptr, slice);
+    token_units<D, B, false>(b, token_item, a, q, k_cache, v_cache, bt, nullptr, s, nullptr,
+                             nullptr, slice);
     return;
   }
   const PrefixRow& row = b.g[row_index(b.g, &PrefixRow::item0, (int)blockIdx.x)];
