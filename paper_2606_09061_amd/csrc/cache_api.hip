@@ -143,6 +143,11 @@ int by_rows(const std::vector<R>& rows, int32_t R::*item0, int64_t most, Items&&
   return CP_OK;
 }
 
+// Pages that a workgroup scores: a turn of its waves (64 pages of head_dim 128), and
+// as many more as leave kScoreItems workgroups.
+constexpr int kLeastChunk = 64, kMostChunk = 512;
+constexpr int64_t kScoreItems = 2048;
+
 // The scores that cp_page_select keeps: rows whose tokens may have to choose.
 int64_t plan_select(const cp_attn_desc& d, const cp_row_meta* rows, int32_t n_rows, int32_t n_pages,
                     std::vector<SelectRow>& out) {
@@ -154,7 +159,7 @@ int64_t plan_select(const cp_attn_desc& d, const cp_row_meta* rows, int32_t n_ro
     const int32_t held = m.chunk_len == 0 ? 0 : (m.ctx_len - 1) / d.block_size + 1;
     const int32_t stride = held > n_pages ? held : 0;
     // a piece's workgroups of the scores fit a launch
-    const int64_t chunks = std::max(1, (stride + kScorePages - 1) / kScorePages);
+    const int64_t chunks = std::max(1, (stride + kLeastChunk - 1) / kLeastChunk);
     const int32_t step =
         (int32_t)std::max<int64_t>(1, std::min<int64_t>(kPieceTokens, kMaxItems / 2 / (chunks * d.num_kv_heads)));
     for (int32_t j = 0; j < m.chunk_len; j += step) {
@@ -202,7 +207,7 @@ AttnArgs attn_args(const cp_attn_desc* d, const AttnPlan& p, const void* q, cons
                   p.piece,
                   0,
                   0,
-                  p.unit_waves,
+                  __builtin_ctz(p.unit_waves),
                   0,
                   0,
                   d->sm_scale * cpattn::kLog2e};
@@ -405,6 +410,10 @@ int cp_page_select(const cp_attn_desc* desc, const void* q, const void* bounds,
     rc = check_tables(desc, block_tables, rows, n_rows, false, s);
     if (rc != CP_OK) return rc;
     (void)hipGetLastError();
+    const int hkv = desc->num_kv_heads;
+    int chunk = kLeastChunk, most = 0;
+    while (chunk < kMostChunk && scores > 2 * chunk * kScoreItems) chunk *= 2;
+    for (const SelectRow& r : plan) most = std::max(most, (r.start + r.n - 1) / desc->block_size + 1);
     const SelectArgs a{static_cast<const uint16_t*>(q),
                        static_cast<const uint16_t*>(bounds),
                        block_tables,
@@ -417,15 +426,15 @@ int cp_page_select(const cp_attn_desc* desc, const void* q, const void* bounds,
                        desc->block_size,
                        n_pages,
                        n_first,
-                       n_last};
-    const int hkv = desc->num_kv_heads;
+                       n_last,
+                       chunk};
     scored.clear();
     for (const SelectRow& r : plan)
       if (r.stride > 0) scored.push_back(r);
     rc = by_rows<SelectRow, kSelectRows>(
         scored, &SelectRow::item0, kMaxItems,
         [&](const SelectRow& r) {
-          return (int64_t)r.n * hkv * ((r.stride + kScorePages - 1) / kScorePages);
+          return (int64_t)r.n * hkv * ((r.stride + chunk - 1) / chunk);
         },
         [&](SelectRows& batch, int n, int items, size_t) {
           return finish(launch_score(desc->head_dim, a, batch, n, items, s), s);
@@ -434,7 +443,7 @@ int cp_page_select(const cp_attn_desc* desc, const void* q, const void* bounds,
     return by_rows<SelectRow, kSelectRows>(
         plan, &SelectRow::item0, kMaxItems, [&](const SelectRow& r) { return (int64_t)r.n * hkv; },
         [&](SelectRows& batch, int n, int items, size_t) {
-          return finish(launch_choose(a, batch, n, items, s), s);
+          return finish(launch_choose(a, batch, n, items, most, s), s);
         });
   });
 }

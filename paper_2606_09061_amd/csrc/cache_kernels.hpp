@@ -35,9 +35,8 @@ struct SelectArgs {
   int32_t* pages;
   uint64_t* scores;
   int hq, hkv, mbr, num_blocks, block, n_pages, n_first, n_last;
+  int chunk;  // pages that a workgroup scores
 };
-// Pages that a workgroup scores.
-constexpr int kScorePages = 256;
 
 struct AttnArgs {
   const uint16_t* q;
@@ -50,7 +49,7 @@ struct AttnArgs {
   float* part_lse;       // [partial rows], log2 of the weights' sum
   int hq, hkv, mbr, log2_group, n_pages, piece;
   int part0;             // the partial rows of the launch's first item of rows
-  int items, unit_waves; // the launch's (token, kv head, piece) items, and waves of each
+  int items, log2_waves; // the launch's (token, kv head, piece) items, and waves of each
   int n_groups;          // of the launch
   int group_items;       // its first workgroups, which are the groups'
   float scale_log2;      // sm_scale * log2(e)
@@ -64,8 +63,9 @@ hipError_t launch_bounds(int d, int block, const BoundsArgs& a, const BoundsRows
                          int pages, hipStream_t s);
 hipError_t launch_score(int d, const SelectArgs& a, const SelectRows& rows, int n_rows, int items,
                         hipStream_t s);
+// most: the largest number of pages of a token
 hipError_t launch_choose(const SelectArgs& a, const SelectRows& rows, int n_rows, int items,
-                         hipStream_t s);
+                         int most, hipStream_t s);
 // tokens over their page lists
 hipError_t launch_pages(int d, int block, const AttnArgs& a, const AttnBatch& b, int n_rows,
                         int items, hipStream_t s);

@@ -15,8 +15,17 @@ using cptree::ceil_div;
 // Work beyond so many workgroups is not cut: they fill the GPU eight times.
 constexpr int64_t kUncut = 8 * cptree::kSlots;
 
-// Items up to which four waves share one, and two.
-constexpr int64_t kUnitWaves4 = 512, kUnitWaves2 = 768;
+// Waves of an item, of which the longest takes `turns`: four where the items alone
+// do not fill the CUs' slots; one, which starts and ends once for all its keys,
+// where they do, unless long items would end far apart.  us, 1 / 2 / 4 waves, lists
+// of 64 pages on 32/8 heads: 256 items 48 / 31 / 29, 384 48 / 41 / 44, 512 52 / 54 /
+// 56, 768 65 / 85 / 81, 1,024 95 / 104 / 106, 2,048 198 / 223 / 219; of 256 pages: 384
+// 173 / 123 / 130, 512 186 / 165 / 165, 768 262 / 257 / 261, 2,048 739 / 681 / 667.
+int unit_waves(int64_t items, int64_t turns) {
+  if (items <= 320) return 4;
+  if (items <= 512) return turns > 8 ? 2 : 1;
+  return items <= 1536 || turns <= 16 ? 1 : 4;
+}
 
 // Times of the attention kernels (pieces.hpp), in us.
 cptree::Cost cost_of(int d, bool wide, double memory) {
@@ -62,14 +71,15 @@ bool cut_rows(AttnPlan& out, const cp_attn_desc& d, double keys, int per_turn, i
     const int turns = cptree::best_piece(work, cost_of(d.head_dim, false, memory_us(d, keys)), &time);
     out.piece = (int)std::min<int64_t>(most, (int64_t)std::max(1, turns) * per_turn);
   }
-  int64_t partial = 0, items = 0;
+  int64_t partial = 0, items = 0, longest = 0;
   for (TokenRow& r : out.rows) {
     r.n_split = (int)ceil_div(own(r), out.piece);
     out.parts |= r.n_split > 1 || r.group >= 0;
     partial += (int64_t)r.n_split * r.n * d.num_q_heads;
     items += (int64_t)r.n_split * r.n * d.num_kv_heads;
+    longest = std::max<int64_t>(longest, ceil_div(std::min<int64_t>(own(r), out.piece), per_turn));
   }
-  out.unit_waves = items <= kUnitWaves4 ? 4 : items <= kUnitWaves2 ? 2 : 1;
+  out.unit_waves = unit_waves(items, longest);
   out.row_part0 = (int32_t)std::min<int64_t>(out.partial_rows, INT32_MAX);
   if (out.parts) out.partial_rows += partial;
   if (out.partial_rows > INT32_MAX) return false;

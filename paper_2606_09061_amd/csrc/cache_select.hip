@@ -23,59 +23,78 @@ __device__ __forceinline__ uint64_t key_of(double x) {
   return b >> 63 ? ~b : b | 1ull << 63;
 }
 
-template <int Bit>
-__device__ __forceinline__ uint64_t partner64(uint64_t x) {
-  const float lo = cpattn::lane_partner<Bit>(__uint_as_float((uint32_t)x));
-  const float hi = cpattn::lane_partner<Bit>(__uint_as_float((uint32_t)(x >> 32)));
+template <int Ctrl>
+__device__ __forceinline__ uint64_t dpp64(uint64_t x) {
+  const float lo = cpattn::dpp<Ctrl>(__uint_as_float((uint32_t)x));
+  const float hi = cpattn::dpp<Ctrl>(__uint_as_float((uint32_t)(x >> 32)));
   return (uint64_t)__float_as_uint(lo) | (uint64_t)__float_as_uint(hi) << 32;
 }
 
-// One step of a sum over lanes that differ in `Bit`: while a lane holds more than
-// one head's sum, each side keeps half of them and gives away the others.
-template <int Bit, int N, int G>
-__device__ __forceinline__ void sum_step(double (&u)[G], int lane) {
+// The value of the lane whose index differs in bit Bit alone (1, 2, 4 or 8).
+template <int Bit>
+__device__ __forceinline__ uint64_t partner64(uint64_t x) {
+  if constexpr (Bit == 4) return dpp64<0x1B>(dpp64<cpattn::kMirror8>(x));  // 7 - i, then i ^ 3
+  else return dpp64<Bit == 1 ? cpattn::kXor1 : Bit == 2 ? cpattn::kXor2 : cpattn::kXor8>(x);
+}
+// The same but for Bit 4, where the bits below differ, too.
+template <int Bit>
+__device__ __forceinline__ uint64_t mirror64(uint64_t x) {
+  if constexpr (Bit == 4) return dpp64<cpattn::kMirror8>(x);
+  else return partner64<Bit>(x);
+}
+
+// One step of a sum over lanes that differ in `Bit`: of N sums a lane keeps one
+// half, by its side, and gives away the other; the last one both sides keep.
+template <int Bit, int N>
+__device__ __forceinline__ void sum_step(double* u, int lane) {
+  const auto add = [](double keep, double give) {
+    return keep + __longlong_as_double(
+                      (long long)mirror64<Bit>((uint64_t)__double_as_longlong(give)));
+  };
   if constexpr (N > 1) {
     const bool up = lane & Bit;
 #pragma unroll
-    for (int e = 0; e < N / 2; ++e) {
-      const double keep = up ? u[e + N / 2] : u[e], give = up ? u[e] : u[e + N / 2];
-      u[e] = keep + __longlong_as_double((long long)partner64<Bit>(
-                        (uint64_t)__double_as_longlong(give)));
-    }
+    for (int e = 0; e < N / 2; ++e)
+      u[e] = add(up ? u[e + N / 2] : u[e], up ? u[e] : u[e + N / 2]);
   } else {
-    u[0] += __longlong_as_double((long long)partner64<Bit>((uint64_t)__double_as_longlong(u[0])));
+    u[0] = add(u[0], u[0]);
   }
 }
 
-template <int Bit>
-__device__ __forceinline__ uint64_t max_step(uint64_t k) {
-  const uint64_t o = partner64<Bit>(k);
-  return o > k ? o : k;
-}
-
-// Scores.  A workgroup takes kScorePages pages of one (token, kv head), its waves
+// Scores.  A workgroup takes a.chunk pages of one (token, kv head), its waves
 // 64 / L of them at a time, L = D / 8 lanes a page with 8 features each.  With
 // lo + hi and hi - lo of a feature, 2 max(q lo, q hi) = q (lo + hi) + |q| (hi - lo):
-// two fp64 multiply-adds per head and feature, which with the conversions are
-// 14 fp64-rate operations per 4 bytes of bounds at 4 heads a group; the bounds'
-// stream is as long.
+// two fp64 multiply-adds per head and feature.  Sums over a page's lanes are split
+// by head first, then by the U pages that the lanes have in hand.  At 4 heads a
+// group that is some 170 vector operations per 2 KB of bounds.
 template <int D, int G, class Rows>
-__global__ __launch_bounds__(kThreads) void score_kernel(const Rows rows, const SelectArgs a,
-                                                         const uint16_t* __restrict__ q,
-                                                         const uint4* __restrict__ bounds,
-                                                         const int32_t* __restrict__ bt,
-                                                         uint64_t* __restrict__ scores) {
+__global__ __launch_bounds__(kThreads, G <= 4 ? 4 : 2) void score_kernel(
+    const Rows rows, const SelectArgs a, const uint16_t* __restrict__ q,
+    const uint4* __restrict__ bounds, const int32_t* __restrict__ bt,
+    uint64_t* __restrict__ scores) {
   constexpr int L = D / 8, PPW = 64 / L, U = 4;  // pages per load, loads in flight
+  // heads per lane behind the steps over lane bits 4 and 8
+  constexpr int H4 = G > 1 ? G / 2 : 1, H = L == 16 && H4 > 1 ? H4 / 2 : H4;
   const int lane = threadIdx.x & 63, sub = lane % L;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const SelectRow row = rows.r[row_index(rows.r, &SelectRow::item0, (int)blockIdx.x)];
-  const int chunks = (row.stride + kScorePages - 1) / kScorePages;
+  const int chunks = (row.stride + a.chunk - 1) / a.chunk;
   const int x = (int)blockIdx.x - row.item0;
   const int chunk = x % chunks, h = x / chunks % a.hkv, j = x / chunks / a.hkv;
   const int n_pages = (row.start + j) / a.block + 1;  // of this token
-  const int p0 = chunk * kScorePages, p1 = min(n_pages, p0 + kScorePages);
+  const int p0 = chunk * a.chunk, p1 = min(n_pages, p0 + a.chunk);
   if (p0 >= p1) return;
   const int64_t t = (int64_t)row.tok0 + j;
+  const int32_t* bt_row = bt + (int64_t)row.req * a.mbr;
+  uint64_t* dst = scores + row.score0 + ((int64_t)j * a.hkv + h) * row.stride;
+  const int group = lane / L;
+  constexpr int STEP = kWaves * PPW * U;
+  int32_t blk[U];
+  const auto load_entries = [&](int b) {  // past the last page that one again
+#pragma unroll
+    for (int u = 0; u < U; ++u) blk[u] = bt_row[min(b + u * PPW + group, p1 - 1)];
+  };
+  load_entries(p0 + wave * PPW * U);
   double qd[G][8];
 #pragma unroll
   for (int e = 0; e < G; ++e) {
@@ -84,21 +103,18 @@ __global__ __launch_bounds__(kThreads) void score_kernel(const Rows rows, const 
 #pragma unroll
     for (int i = 0; i < 8; ++i) qd[e][i] = (double)(i & 1 ? bf16hi(w[i / 2]) : bf16lo(w[i / 2]));
   }
-  const int32_t* bt_row = bt + (int64_t)row.req * a.mbr;
-  uint64_t* dst = scores + row.score0 + ((int64_t)j * a.hkv + h) * row.stride;
-  const int group = lane / L;
-  for (int b = p0 + wave * PPW * U; b < p1; b += kWaves * PPW * U) {
+  for (int b = p0 + wave * PPW * U; b < p1; b += STEP) {
     uint4 lo[U], hi[U];
     bool there[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int page = min(b + u * PPW + group, p1 - 1);  // past the last page that one again
-      const int blk = bt_row[page];
-      there[u] = blk >= 0 && blk < a.num_blocks;
-      const uint4* src = bounds + ((int64_t)(there[u] ? blk : 0) * a.hkv + h) * 2 * L + sub;
-      lo[u] = cpattn::ld_global16(src);
-      hi[u] = cpattn::ld_global16(src + L);
+      there[u] = blk[u] >= 0 && blk[u] < a.num_blocks;
+      const uint4* src = bounds + ((int64_t)(there[u] ? blk[u] : 0) * a.hkv + h) * 2 * L + sub;
+      lo[u] = cpattn::ld_global16_nt(src);
+      hi[u] = cpattn::ld_global16_nt(src + L);
     }
+    load_entries(min(b + STEP, p1 - 1));
+    double sum[U * H];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const uint32_t lw[4] = {lo[u].x, lo[u].y, lo[u].z, lo[u].w};
@@ -115,22 +131,228 @@ __global__ __launch_bounds__(kThreads) void score_kernel(const Rows rows, const 
         for (int e = 0; e < G; ++e)
           s[e] = __builtin_fma(fabs(qd[e][i]), width, __builtin_fma(qd[e][i], both, s[e]));
       }
-      // sums over the L lanes, then the largest of the heads
-      constexpr int N1 = L == 16 ? (G > 1 ? G / 2 : 1) : G, N2 = N1 > 1 ? N1 / 2 : 1,
-                    N3 = N2 > 1 ? N2 / 2 : 1;
-      if constexpr (L == 16) sum_step<8, G>(s, lane);
-      sum_step<4, N1>(s, lane);
-      sum_step<2, N2>(s, lane);
-      sum_step<1, N3>(s, lane);
-      static_assert(N3 <= 2, "one head's sum is left");
-      uint64_t k = key_of(s[0]);
-      if constexpr (N3 > 1) k = max_step<1>(k);
-      if constexpr (N2 > 1) k = max_step<2>(k);
-      if constexpr (N1 > 1) k = max_step<4>(k);
-      if constexpr (L == 16 && G > 1) k = max_step<8>(k);
-      const int page = b + u * PPW + group;
-      if (sub == 0 && page < p1) dst[page] = there[u] ? k : 0;
+      sum_step<4, G>(s, lane);
+      if constexpr (L == 16) sum_step<8, H4>(s, lane);
+#pragma unroll
+      for (int e = 0; e < H; ++e) sum[u * H + e] = s[e];
     }
+    static_assert(U == 4, "two lane bits");
+    sum_step<2, U * H>(sum, lane);
+    sum_step<1, U / 2 * H>(sum, lane);
+    // lane bits 1 and 0 name the page, bits 8 and 4 the heads
+    uint64_t k = key_of(sum[0]);
+#pragma unroll
+    for (int e = 1; e < H; ++e) k = max(k, key_of(sum[e]));
+    if constexpr (G > 1) k = max(k, partner64<4>(k));
+    if constexpr (L == 16 && H4 > 1) k = max(k, partner64<8>(k));
+    const int u = lane & 3, page = b + u * PPW + group;
+    const bool found = u == 0 ? there[0] : u == 1 ? there[1] : u == 2 ? there[2] : there[3];
+    if (sub < U && page < p1) dst[page] = found ? k : 0;
+  }
+}
+
+// Inclusive sum of x over the lanes of a wave.
+__device__ __forceinline__ int wave_scan(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);  // row_shr:1
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);  // row_bcast:15
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);  // row_bcast:31
+  return x;
+}
+
+// The largest of x over groups of 16 lanes, and over the wave.
+__device__ __forceinline__ uint64_t max16(uint64_t x) {
+  x = max(x, partner64<1>(x));
+  x = max(x, partner64<2>(x));
+  x = max(x, mirror64<4>(x));
+  return max(x, partner64<8>(x));
+}
+__device__ __forceinline__ uint64_t max64(uint64_t x) {
+  x = max16(x);
+  x = max(x, (uint64_t)__shfl_xor((unsigned long long)x, 16, 64));
+  return max(x, (uint64_t)__shfl_xor((unsigned long long)x, 32, 64));
+}
+
+// Where the selected pages of a (token, kv head) go, and how many it has to choose
+// from.
+struct Choice {
+  int n;
+  const uint64_t* src;
+  int32_t* dst;
+};
+
+template <class Rows>
+__device__ __forceinline__ Choice choice_of(const Rows& rows, const SelectArgs& a,
+                                            const uint64_t* scores) {
+  const SelectRow row = rows.r[row_index(rows.r, &SelectRow::item0, (int)blockIdx.x)];
+  const int x = (int)blockIdx.x - row.item0, h = x % a.hkv, j = x / a.hkv;
+  const int64_t t = (int64_t)row.tok0 + j;
+  return Choice{(row.start + j) / a.block + 1,
+                scores + row.score0 + ((int64_t)j * a.hkv + h) * row.stride,
+                a.pages + (t * a.hkv + h) * a.n_pages};
+}
+
+// The choice: one workgroup of NT threads per (token, kv head), which holds up to
+// NT NU keys in registers.  The fixed pages aside, the place of the threshold
+// is found eight bits at a time from the highest one in which the keys differ,
+// by a histogram of the keys that agree with the bits known so far.  Once few keys
+// are left, or all of them are selected, each counts those before it.  The
+// selected pages are written in order, by the ballots of the waves.
+template <int NT, int NU, class Rows>
+__global__ __launch_bounds__(NT) void choose_kernel(const Rows rows, const SelectArgs a,
+                                                    const uint64_t* __restrict__ scores) {
+  constexpr int NW = NT / 64, kFew = 128, NC = NU * NW, CPL = NC > 64 ? NC / 64 : 1;
+  static_assert(NW <= 16 && NT % kFew == 0 && (NC <= 64 || NC == 64 * CPL), "geometry");
+  __shared__ __align__(16) int s_hist[2][256];
+  __shared__ int s_count[2][CPL * 64];
+  __shared__ uint64_t s_max[16], s_not_min[16], s_key[kFew];
+  __shared__ int s_page[kFew], s_digit, s_left, s_in, s_few;
+  __shared__ unsigned long long s_take[NC];
+  const Choice c = choice_of(rows, a, scores);
+  const int n = c.n, P = a.n_pages, tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  if (n <= P) {  // all of them
+    for (int i = tid; i < P; i += NT) c.dst[i] = i < n ? i : -1;
+    return;
+  }
+  // n > P >= fixed pages: those are apart
+  const int first = a.n_first, last = n - a.n_last;  // chosen from: [first, last)
+  uint64_t key[NU];
+#pragma unroll
+  for (int u = 0; u < NU; ++u) {
+    const int i = u * NT + tid;
+    key[u] = i >= first && i < last ? c.src[i] : 0;
+  }
+  for (int x = tid; x < 512; x += NT) s_hist[x >> 8][x & 255] = 0;
+  if (tid < 2 * CPL * 64) s_count[0][tid] = 0;  // (NT >= 2 CPL 64)
+  static_assert(NT >= 2 * CPL * 64 && NT >= NC, "one word a thread");
+  if (tid < NC) s_take[tid] = 0;
+  if (tid == 0) s_few = 0;
+  uint64_t most = 0, not_least = 0;
+#pragma unroll
+  for (int u = 0; u < NU; ++u) {
+    const int i = u * NT + tid;
+    if (i >= first && i < last) most = max(most, key[u]), not_least = max(not_least, ~key[u]);
+  }
+  most = max64(most), not_least = max64(not_least);
+  if (lane == 0) s_max[wave] = most, s_not_min[wave] = not_least;
+  __syncthreads();
+  most = max16(s_max[min(lane & 15, NW - 1)]);
+  const uint64_t least = ~max16(s_not_min[min(lane & 15, NW - 1)]);
+  int left = P - a.n_first - a.n_last;  // still to be chosen, of `in` keys that agree with
+  int in = last - first;                // `known` in the bits from `shift` on
+  int shift = 64 - __clzll((long long)(most ^ least));  // (of equal ones: 0)
+  uint64_t known = shift < 64 ? most >> shift : 0;
+  for (int pass = 0; in > kFew && in > left && left > 0 && shift > 0; pass ^= 1) {
+    const int low = max(0, shift - 8), bits = shift - low;
+#pragma unroll
+    for (int u = 0; u < NU; ++u) {
+      const int i = u * NT + tid;
+      if (i >= first && i < last && (shift >= 64 || key[u] >> shift == known))
+        atomicAdd(&s_hist[pass][(int)(key[u] >> low) & ((1 << bits) - 1)], 1);
+    }
+    __syncthreads();
+    if (wave == 0) {  // lane l: digits 255 - 4 l and the three below
+      const int4 d = *reinterpret_cast<const int4*>(&s_hist[pass][252 - 4 * lane]);
+      const int upto = wave_scan(d.x + d.y + d.z + d.w);
+      const int c3 = upto - d.x - d.y - d.z - d.w;  // above digit 255 - 4 l
+      const int c2 = c3 + d.w, c1 = c2 + d.z, c0 = c1 + d.y;
+      if (c3 < left && upto >= left) {
+        const int x = c2 >= left ? 3 : c1 >= left ? 2 : c0 >= left ? 1 : 0;
+        s_digit = 252 - 4 * lane + x;
+        s_left = left - (x == 3 ? c3 : x == 2 ? c2 : x == 1 ? c1 : c0);
+        s_in = x == 3 ? d.w : x == 2 ? d.z : x == 1 ? d.y : d.x;
+      }
+    } else {
+      for (int x = tid - 64; x < 256; x += NT - 64) s_hist[pass ^ 1][x] = 0;
+    }
+    __syncthreads();
+    known = (shift < 64 ? known << bits : 0) | (uint64_t)s_digit;
+    left = s_left, in = s_in, shift = low;
+  }
+  // above the agreeing keys: chosen; of those, all, none, or the `left` first by
+  // (key, page)
+  uint32_t chosen = 0, agree = 0;  // a bit per u
+#pragma unroll
+  for (int u = 0; u < NU; ++u) {
+    const int i = u * NT + tid;
+    const uint64_t top = shift < 64 ? key[u] >> shift : 0;
+    const bool fixed = i < first || (i >= last && i < n);
+    if (fixed || (i < last && top > known)) chosen |= 1u << u;
+    else if (i < last && top == known) agree |= 1u << u;
+  }
+  // word x of a wave's counts (u, wave) of the keys before
+  const auto count = [&](uint32_t bits, int buffer, int (&before)[CPL]) {
+#pragma unroll
+    for (int u = 0; u < NU; ++u) {
+      const uint64_t b = __builtin_amdgcn_ballot_w64(bits >> u & 1);
+      if (lane == 0) s_count[buffer][u * NW + wave] = __popcll(b);
+    }
+    __syncthreads();
+    int sum = 0;
+#pragma unroll
+    for (int x = 0; x < CPL; ++x) {
+      before[x] = sum;
+      sum += s_count[buffer][CPL * lane + x];
+    }
+    const int lanes_before = wave_scan(sum) - sum;
+#pragma unroll
+    for (int x = 0; x < CPL; ++x) before[x] += lanes_before;
+  };
+  const auto position = [&](uint32_t bits, int u, const int (&before)[CPL]) {
+    const uint64_t b = __builtin_amdgcn_ballot_w64(bits >> u & 1);
+    const int word = u * NW + wave;
+    int at = 0;
+#pragma unroll
+    for (int x = 0; x < CPL; ++x)
+      if (word % CPL == x) at = __builtin_amdgcn_readlane(before[x], word / CPL);
+    return at + __popcll(b & ((1ull << lane) - 1));
+  };
+  if (in <= left) {
+    chosen |= agree;
+  } else if (left > 0 && in <= kFew) {
+#pragma unroll
+    for (int u = 0; u < NU; ++u)
+      if (agree >> u & 1) {
+        const int at = atomicAdd(&s_few, 1);
+        s_key[at] = key[u], s_page[at] = u * NT + tid;
+      }
+    __syncthreads();
+    // SH threads count the keys before one (whatever their order here)
+    constexpr int SH = NT / kFew >= 8 ? 8 : 2;
+    if (tid < kFew * SH) {
+      const int e0 = tid % SH, x = min(tid / SH, in - 1);
+      const uint64_t k = s_key[x];
+      const int page = s_page[x];
+      int before = 0;
+#pragma unroll 4
+      for (int e = e0; e < in; e += SH)
+        before += s_key[e] > k || (s_key[e] == k && s_page[e] < page);
+#pragma unroll
+      for (int m = 1; m < SH; m <<= 1) before += __shfl_xor(before, m, 64);
+      if (e0 == 0 && tid / SH < in && before < left)
+        atomicOr(&s_take[page >> 6], 1ull << (page & 63));
+    }
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < NU; ++u) chosen |= (uint32_t)(s_take[u * NW + wave] >> lane & 1) << u;
+  } else if (left > 0) {  // more equal keys: the first `left`
+    int before[CPL];
+    count(agree, 1, before);
+#pragma unroll
+    for (int u = 0; u < NU; ++u) {
+      const int at = position(agree, u, before);
+      if ((agree >> u & 1) && at < left) chosen |= 1u << u;
+    }
+  }
+  int before[CPL];
+  count(chosen, 0, before);
+#pragma unroll
+  for (int u = 0; u < NU; ++u) {
+    const int at = position(chosen, u, before);
+    if (chosen >> u & 1) c.dst[at] = u * NT + tid;
   }
 }
 
@@ -155,27 +377,22 @@ __device__ __forceinline__ int scan(int x, int* s_wave, int* total) {
   return before + sum - x;
 }
 
-// The choice: one workgroup per (token, kv head).  The n_pages-th largest key is
-// found eight bits at a time, from a histogram of the keys that agree with the
-// bits known so far; then the pages are written in order, those above it and
-// as many equal ones as there is room for, the lower first.
+// The same for more keys than a workgroup holds, which are read again in each pass.
 template <class Rows>
-__global__ __launch_bounds__(kThreads) void choose_kernel(const Rows rows, const SelectArgs a,
-                                                          const uint64_t* __restrict__ scores) {
+__global__ __launch_bounds__(kThreads) void choose_long_kernel(const Rows rows, const SelectArgs a,
+                                                               const uint64_t* __restrict__ scores) {
   __shared__ int s_hist[256];
   __shared__ int s_wave[kWaves];
   __shared__ int s_digit, s_left;
-  const SelectRow row = rows.r[row_index(rows.r, &SelectRow::item0, (int)blockIdx.x)];
-  const int x = (int)blockIdx.x - row.item0, h = x % a.hkv, j = x / a.hkv;
-  const int64_t t = (int64_t)row.tok0 + j;
-  int32_t* dst = a.pages + (t * a.hkv + h) * a.n_pages;
-  const int n = (row.start + j) / a.block + 1, P = a.n_pages, tid = threadIdx.x;
+  const Choice c = choice_of(rows, a, scores);
+  const int n = c.n, P = a.n_pages, tid = threadIdx.x;
   if (n <= P) {  // all of them
-    for (int i = tid; i < P; i += kThreads) dst[i] = i < n ? i : -1;
+    for (int i = tid; i < P; i += kThreads) c.dst[i] = i < n ? i : -1;
     return;
   }
-  const uint64_t* src = scores + row.score0 + ((int64_t)j * a.hkv + h) * row.stride;
-  const auto key = [&](int i) { return i < a.n_first || i >= n - a.n_last ? kForcedKey : src[i]; };
+  const auto key = [&](int i) {
+    return i < a.n_first || i >= n - a.n_last ? kForcedKey : c.src[i];
+  };
   uint64_t known = 0;  // the bits of the threshold found so far
   int left = P;        // of the keys that agree with them, how many are selected
   for (int shift = 56; shift >= 0; shift -= 8) {
@@ -206,7 +423,7 @@ __global__ __launch_bounds__(kThreads) void choose_kernel(const Rows rows, const
     const int rank = scan(equal ? 1 : 0, s_wave, &equals);
     const bool take = i < n && (k > known || (equal && rank < left));
     const int at = scan(take ? 1 : 0, s_wave, &chosen);
-    if (take) dst[out + at] = i;
+    if (take) c.dst[out + at] = i;
     out += chosen;
     left -= min(left, equals);
   }
@@ -235,9 +452,16 @@ hipError_t launch_score(int d, const SelectArgs& a, const SelectRows& rows, int 
 }
 
 hipError_t launch_choose(const SelectArgs& a, const SelectRows& rows, int n_rows, int items,
-                         hipStream_t s) {
+                         int most, hipStream_t s) {
   return by_size(rows, n_rows, [&](const auto& r) {
-    hipLaunchKernelGGL(choose_kernel, dim3(items), dim3(kThreads), 0, s, r, a, a.scores);
+    if (most <= 1024)
+      hipLaunchKernelGGL((choose_kernel<256, 4>), dim3(items), dim3(256), 0, s, r, a, a.scores);
+    else if (most <= 4096)
+      hipLaunchKernelGGL((choose_kernel<1024, 4>), dim3(items), dim3(1024), 0, s, r, a, a.scores);
+    else if (most <= 16384)
+      hipLaunchKernelGGL((choose_kernel<1024, 16>), dim3(items), dim3(1024), 0, s, r, a, a.scores);
+    else
+      hipLaunchKernelGGL(choose_long_kernel, dim3(items), dim3(kThreads), 0, s, r, a, a.scores);
   });
 }
 

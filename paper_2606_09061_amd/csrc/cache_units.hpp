@@ -218,15 +218,23 @@ __device__ __forceinline__ void join_waves(const State<D, NC>& st, Shared& s, in
   }
   __syncthreads();
   if (x < 16 * NC) {
-    float M = -INFINITY, L = 0.f;
-    for (int w = w0; w < w0 + waves; ++w) M = fmaxf(M, s.m[w][x]);
-    for (int w = w0; w < w0 + waves; ++w) {
-      const float f = s.m[w][x] == -INFINITY ? 0.f : exp2f(s.m[w][x] - M);
-      s.f[w][x] = f;
-      L += f * s.l[w][x];
+    float M = -INFINITY, L = 0.f, m[kWaves], f[kWaves];
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      m[w] = w < waves ? s.m[w0 + w][x] : -INFINITY;
+      f[w] = w < waves ? s.l[w0 + w][x] : 0.f;
+      M = fmaxf(M, m[w]);
+    }
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      const float l = f[w];
+      f[w] = m[w] == -INFINITY ? 0.f : exp2f(m[w] - M);
+      L += f[w] * l;
     }
     const float inv = L == 0.f ? 0.f : 1.f / L;  // L == 0: it saw no key
-    for (int w = w0; w < w0 + waves; ++w) s.f[w][x] *= inv;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w)
+      if (w < waves) s.f[w0 + w][x] = f[w] * inv;
     log_sum(x, L == 0.f ? -INFINITY : M + __log2f(L));
   }
 }
@@ -255,10 +263,12 @@ __device__ __forceinline__ void write_rows(const State<D, NC>& st, const Shared&
       const int p = x % (D / 4), r = x / (D / 4);
       if (16 * c + r >= m_rows) break;  // a thread's rows come in increasing order
       f32x4_t v = {0.f, 0.f, 0.f, 0.f};
-      for (int w = w0; w < w0 + waves; ++w)
-        v += s.f[w][16 * c + r] *
-             *reinterpret_cast<const f32x4_t*>(reinterpret_cast<const float*>(slice(w)) + r * D +
-                                               (p ^ r) * 4);
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w)
+        if (w < waves)
+          v += s.f[w0 + w][16 * c + r] *
+               *reinterpret_cast<const f32x4_t*>(
+                   reinterpret_cast<const float*>(slice(w0 + w)) + r * D + (p ^ r) * 4);
       put(16 * c + r, p, v);
     }
   }
@@ -335,7 +345,7 @@ __device__ __forceinline__ Own own_of(const Batch& b, const AttnArgs& a, int r) 
   return o;
 }
 
-// A workgroup of tokens: each of its units, taken by a.unit_waves waves, is a token's
+// A workgroup of tokens: each of its units, taken by 2^a.log2_waves waves, is a token's
 // G rows over a piece of its own keys, or (LIST) of its page list, whose blocks of
 // the piece come to s_blocks, their number to s_count.
 template <int D, int B, bool LIST, class Batch, class Slice>
@@ -350,8 +360,8 @@ __device__ __forceinline__ void token_units(const Batch& b, int block, const Att
   constexpr int NKS = D / 32;
   const int tid = threadIdx.x, lane = tid & 63, i = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int W = a.unit_waves, mine = wave / W, w0 = mine * W, x = tid - 64 * w0;
-  const int item = block * (kWaves / W) + mine;
+  const int W = 1 << a.log2_waves, mine = wave >> a.log2_waves, w0 = mine << a.log2_waves;
+  const int x = tid - 64 * w0, item = block * (kWaves >> a.log2_waves) + mine;
   const bool real = item < a.items;  // the last workgroup may have fewer units
   const Own row = own_of<B, LIST>(b, a, row_index(b.r, &AttnRow::item0, min(item, a.items - 1)));
   const int unit = min(item, a.items - 1) - row.item0;
