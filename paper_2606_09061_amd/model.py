@@ -4,17 +4,17 @@ The paper's predictor and target latency T* refer to a whole model iteration
 (Sec. 3.2.1; Sec. 4.4 uses Qwen3-8B with T* = 105 ms), so this module runs the
 scheduler's batch through every layer of such a model with synthetic weights:
 
-    embedding -> L x [RMSNorm -> QKV GEMM -> cpl_qkv_rope -> cp_kv_append ->
-    cp_attn_mixed -> O GEMM (+ residual) -> RMSNorm -> gate/up GEMM ->
-    cpl_swiglu -> down GEMM (+ residual)] -> RMSNorm -> LM head on each row's
-    last token -> argmax
+    embedding -> L x [RMSNorm -> QKV GEMM -> cp_qkv_append -> cp_attn_mixed ->
+    O GEMM (+ residual) -> RMSNorm -> gate/up GEMM -> cpl_swiglu -> down GEMM
+    (+ residual)] -> RMSNorm -> LM head on each row's last token -> argmax
 
-``Model.verify`` runs the same layers over trees of drafted tokens
+``Model.forward`` can attend to common prefixes once for the requests that share
+them, and to selected pages instead of all (libcpcache.so).  ``Model.verify`` runs the same layers over trees of drafted tokens
 (libcptree.so): every node's logits, the accepted path, its K/V moved up.
 
 Every step runs in this package's HIP kernels (libcplayer.so for the
-projections and the element-wise parts, libcpattn.so for append and
-attention); the largest of the feed-forward's projections, and those of shapes
+projections and the element-wise parts, libcpcache.so for rotation and append,
+libcpattn.so for attention); the largest of the feed-forward's projections, and those of shapes
 or tensors that the kernels do not take, run as library GEMMs (torch.mm /
 addmm, i.e. hipBLASLt).  Each layer has
 its own paged KV pool; all layers share one block table, whose row s maps
@@ -383,9 +383,15 @@ class Model:
     """Synthetic-weight decoder stack with per-layer paged KV pools."""
 
     def __init__(self, cfg: ModelConfig = QWEN3_8B, max_seqs=128, max_seq_len=4096,
-                 max_tokens=2048, seed=0, device=None, lm_head=True, fill_caches=False):
+                 max_tokens=2048, seed=0, device=None, lm_head=True, fill_caches=False,
+                 page_bounds=False):
+        """``page_bounds``: every iteration keeps the bounds of the pages that it
+        writes (an eighth of K's memory at 16 tokens a page), by which
+        forward(budget=...) selects pages."""
         import torch
         from workloads.tensors import _randn_bf16
+
+        from . import cache
 
         self.cfg = c = cfg
         self.dev = device or torch.device("cuda", 0)
@@ -428,6 +434,14 @@ class Model:
                                    device=self.dev) for _ in range(c.layers)]
         self.desc = cp.make_desc(c.hq, c.hkv, D, c.block_size, nb, mbr, max_seqs,
                                  1.0 / math.sqrt(D))
+        # (a page that is not written yet holds zeros: nothing reads its bounds)
+        self.bounds = [torch.zeros(nb, c.hkv, 2, D, dtype=torch.bfloat16, device=self.dev)
+                       for _ in range(c.layers)] if page_bounds else None
+        if page_bounds and fill_caches:
+            n = mbr * c.block_size
+            for kc, b in zip(self.kc, self.bounds):
+                for slot in range(max_seqs):
+                    cache.page_bounds(self.desc, kc, self.bt, [(slot, 0, n, n)], b)
         T = max_tokens
 
         def buf(*shape):
@@ -435,56 +449,80 @@ class Model:
 
         self.x, self.h = buf(T, H), buf(T, H)
         self.qkv = buf(T, nqkv)
-        self.q, self.k, self.v = buf(T, c.hq, D), buf(T, c.hkv, D), buf(T, c.hkv, D)
-        self.attn = buf(T, c.hq, D)
+        self.q, self.attn = buf(T, c.hq, D), buf(T, c.hq, D)
         self.gu, self.act = buf(T, 2 * c.inter), buf(T, c.inter)
-        self.pos_host = torch.zeros(T, dtype=torch.int32).pin_memory()
-        self.pos_copied = torch.cuda.Event()   # the last upload out of pos_host is done
         self.pos = torch.zeros(T, dtype=torch.int32, device=self.dev)
         self.tokens = torch.randint(0, c.vocab, (T,), generator=gen, device=self.dev)
         self.ws = torch.empty(64 << 20, dtype=torch.uint8, device=self.dev)      # attention plan
         # split-K partials of the projections (grown on demand)
         self.ws_gemm = torch.empty(256, dtype=torch.uint8, device=self.dev)
-        # an append item covers one row's tokens inside one block: at most
-        # max_tokens + max_seqs items of 16 bytes, so the append never needs more
-        self.ws_append = torch.empty(16 * (max_tokens + max_seqs) + 256, dtype=torch.uint8,
-                                     device=self.dev)
 
-    def forward(self, rows, stream=None):
+    def forward(self, rows, stream=None, groups=None, budget=None):
         """Runs one iteration for the batch ``rows`` [(slot, start, len, ctx)];
         returns the greedy next token of every row (device int64 [n_rows]), or
-        None when the model has no LM head."""
+        None when the model has no LM head.
+
+        ``groups`` [(first row, rows, tokens in common)]: the rows of a group share
+        the pages of their first tokens (tree.kv_fork), which are read once for
+        all of them; for iterations of decode rows and short chunks.  ``budget``:
+        every token attends to so many pages of each kv head instead of all, the
+        first, the last and those whose bounds promise most (``page_bounds`` has
+        to be kept); for iterations of decode rows."""
         import torch
+
+        from . import cache
         c = self.cfg
         rows = np.ascontiguousarray(np.asarray(rows, dtype=np.int32).reshape(-1, 4))
         T = int(rows[:, 2].sum())
+        if groups is not None and budget is not None:
+            raise ValueError("groups or a budget of pages, not both")
+        if budget is not None and (self.bounds is None or (rows[:, 2] > 1).any()):
+            raise ValueError("a budget of pages is for decode rows, with page_bounds kept")
+        if budget is not None and not 2 <= budget <= cache.MAX_PAGES:
+            raise ValueError(f"a budget is 2 to {cache.MAX_PAGES} pages")
         if T == 0:
             return None
         if T > self.max_tokens:
             raise ValueError(f"batch of {T} tokens exceeds the model's {self.max_tokens}")
+        # (both check what they are given, before anything runs)
+        need = 0
+        if groups is not None:
+            groups = cache._groups(groups)
+            need = cache.prefix_attn_workspace_bytes(self.desc, rows, groups)
+        elif budget is not None:
+            need = max(cache.page_attn_workspace_bytes(self.desc, rows, budget),
+                       cache.page_select_workspace_bytes(self.desc, rows, budget))
         s = stream or torch.cuda.current_stream(self.dev)
-        pos = positions_of(rows)
-        self.pos_copied.synchronize()   # the previous iteration's upload has left pos_host
-        self.pos_host[:T].numpy()[:] = pos
         with torch.cuda.stream(s):
-            self.pos[:T].copy_(self.pos_host[:T], non_blocking=True)
-            self.pos_copied.record(s)
+            if need > self.ws.numel():
+                self.ws = torch.empty(need, dtype=torch.uint8, device=self.dev)
             x = self.x[:T]
             torch.index_select(self.embed, 0, self.tokens[:T], out=x)
-            # every layer attends with the same rows: plan once, run per layer
-            # (the plan is built once per iteration; only a workspace that is
-            # too small costs a second planning, to learn the size)
-            try:
-                plan = cp.attn_prepare(self.desc, rows, self.ws, stream=s)
-            except cp.CpError as e:
-                if e.code != cp.CP_ERR_WORKSPACE:
-                    raise
-                self.ws = torch.empty(cp.workspace_bytes(self.desc, rows), dtype=torch.uint8,
-                                      device=self.dev)
-                plan = cp.attn_prepare(self.desc, rows, self.ws, stream=s)
-            self._layers(rows, T, int((rows[:, 2] > 0).sum()), s,
-                         lambda q, kc, vc, out: cp.attn_run(plan, q, kc, vc, self.bt, out, self.ws,
-                                                            stream=s))
+            if groups is not None:
+                def attend(q, kc, vc, bounds, out):
+                    cache.prefix_attn(self.desc, q, kc, vc, self.bt, rows, groups, out, self.ws, s)
+            elif budget is not None:
+                pages = torch.empty(T, c.hkv, budget, dtype=torch.int32, device=self.dev)
+
+                def attend(q, kc, vc, bounds, out):
+                    cache.page_select(self.desc, q, bounds, self.bt, rows, pages, 1, 1, self.ws, s)
+                    cache.page_attn(self.desc, q, kc, vc, self.bt, pages, rows, out, self.ws, s)
+            else:
+                # every layer attends with the same rows: plan once, run per layer
+                # (the plan is built once per iteration; only a workspace that is
+                # too small costs a second planning, to learn the size)
+                try:
+                    plan = cp.attn_prepare(self.desc, rows, self.ws, stream=s)
+                except cp.CpError as e:
+                    if e.code != cp.CP_ERR_WORKSPACE:
+                        raise
+                    self.ws = torch.empty(cp.workspace_bytes(self.desc, rows), dtype=torch.uint8,
+                                          device=self.dev)
+                    plan = cp.attn_prepare(self.desc, rows, self.ws, stream=s)
+
+                def attend(q, kc, vc, bounds, out):
+                    cp.attn_run(plan, q, kc, vc, self.bt, out, self.ws, stream=s)
+            self._layers(rows, T, int((rows[:, 2] > 0).sum()), s, attend)
             if self.lm_head is None:
                 return None
             last = torch.from_numpy(np.cumsum(rows[:, 2]).astype(np.int64) - 1)
@@ -495,14 +533,16 @@ class Model:
             project(hl, self.lm_head, logits, None, s, self.ws_gemm)
             return torch.argmax(logits, dim=-1)
 
-    def _layers(self, rows, T, n_head, s, attend):
-        """The decoder layers over the embeddings in x[:T], whose positions are in
-        pos[:T], on stream ``s``: K/V appended, ``attend(q, kc, vc, out)`` for the
-        attention.  The projections' workspace is grown for ``n_head`` rows of
-        the LM head too."""
+    def _layers(self, rows, T, n_head, s, attend, positions=None):
+        """The decoder layers over the embeddings in x[:T] on stream ``s``: K/V
+        appended, rotated to the tokens' own positions or to ``positions``, and
+        ``attend(q, kc, vc, bounds, out)`` for the attention.  The projections'
+        workspace is grown for ``n_head`` rows of the LM head too."""
         import torch
+
+        from . import cache
         c = self.cfg
-        x, h, qkv, q, k, v = (b[:T] for b in (self.x, self.h, self.qkv, self.q, self.k, self.v))
+        x, h, qkv, q = (b[:T] for b in (self.x, self.h, self.qkv, self.q))
         attn, gu, act = self.attn[:T], self.gu[:T], self.act[:T]
         need = max(gemm_workspace_bytes(T, qkv.shape[1], c.hidden),
                    gemm_workspace_bytes(T, c.hidden, c.hq * c.head_dim),
@@ -512,13 +552,15 @@ class Model:
                    if self.lm_head is not None else 0)
         if need > self.ws_gemm.numel():
             self.ws_gemm = torch.empty(need, dtype=torch.uint8, device=self.dev)
-        for L, kc, vc in zip(self.layers, self.kc, self.vc):
+        for L, kc, vc, bounds in zip(self.layers, self.kc, self.vc,
+                                     self.bounds or [None] * len(self.layers)):
             rmsnorm(x, L["in_norm"], h, c.eps, s)
             project_attn(h, L["qkv"], qkv, None, s, self.ws_gemm)
-            qkv_rope(qkv, L["q_norm"], L["k_norm"], self.pos, c.hq, c.hkv, c.head_dim,
-                     c.theta, c.eps, q, k, v, s)
-            cp.kv_append(self.desc, k, v, kc, vc, self.bt, rows, self.ws_append, stream=s)
-            attend(q, kc, vc, attn)
+            cache.qkv_append(self.desc, qkv, L["q_norm"], L["k_norm"], rows, q, kc, vc, self.bt,
+                             c.theta, c.eps, positions, s)
+            if bounds is not None:
+                cache.page_bounds(self.desc, kc, self.bt, rows, bounds, s)
+            attend(q, kc, vc, bounds, attn)
             project_attn(attn.view(T, c.hq * c.head_dim), L["o"], x, x, s, self.ws_gemm)
             rmsnorm(x, L["post_norm"], h, c.eps, s)
             project(h, L["gate_up"], gu, None, s, self.ws_gemm)
@@ -538,7 +580,7 @@ class Model:
         next_token as its root.  Returns device int32 tensors (target [T], path
         [rows, max_path], n_accepted [rows], next_token [rows])."""
         import torch
-        from . import tree
+        from . import cache, tree
         c = self.cfg
         if self.lm_head is None:
             raise ValueError("verify needs a model with an LM head")
@@ -571,13 +613,16 @@ class Model:
                 x, h = self.x[:T], self.h[:T]
                 torch.index_select(self.embed, 0, tokens, out=x)
                 self._layers(rows, T, T, s,
-                             lambda q, kc, vc, out: tree.attn(self.desc, q, kc, vc, self.bt, mask,
-                                                              rows, out, self.ws, s))
+                             lambda q, kc, vc, _, out: tree.attn(self.desc, q, kc, vc, self.bt,
+                                                                 mask, rows, out, self.ws, s),
+                             self.pos[:T])
                 rmsnorm(x, self.final_norm, h, c.eps, s)
                 project(h, self.lm_head, logits, None, s, self.ws_gemm)
             tree.verify(logits, tokens, parents, rows, target, path, n_accepted, after, stream=s)
             if T > 0:
                 tree.kv_compact(pools, self.bt, rows, path, n_accepted, s)
+                for kc, bounds in zip(self.kc, self.bounds or ()):   # of the pages moved into
+                    cache.page_bounds(self.desc, kc, self.bt, rows, bounds, s)
         return target, path, n_accepted, after
 
 
