@@ -237,7 +237,7 @@ int launch_plan(const cp_attn_desc* d, const AttnPlan& p, AttnArgs a, hipStream_
         b.g[n_groups].row0 = n;
         // (of a group that began in an earlier launch: no item, it is this one's first)
         b.g[n_groups++].item0 = (int32_t)group_items;
-        wide |= fresh && p.prefix[t.group].wide;
+        wide |= fresh && p.prefix[t.group].wide != kNarrow;
         group_items += shared;
         last = t.group;
         if (fresh) ++begun;

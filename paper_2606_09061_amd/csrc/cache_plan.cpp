@@ -34,9 +34,25 @@ cptree::Cost cost_of(int d, bool wide, double memory) {
   return {kTurn, 5.5 * x, 0.3 + 1.2 * x, 3.2, 5.5, 0.3 * x, memory};
 }
 
+// Common K and V beyond which groups of one wide tile read them past the caches.
+constexpr double kStreamBytes = 64e6;
+
 // us that keys take to come from memory
 double memory_us(const cp_attn_desc& d, double keys) {
   return keys * d.num_kv_heads * d.head_dim * 4.0 / 5.3e6;
+}
+
+// Turns of a piece: the tree plan's choice or a somewhat longer piece, whose fewer
+// partial rows may be worth more than CUs that stay idle.
+int piece_of(const cptree::Work& w, const cptree::Cost& c) {
+  double time = 0;
+  const int chosen = cptree::best_piece(w, c, &time);
+  int best = chosen;
+  for (const int piece : {chosen * 5 / 4, chosen * 3 / 2, chosen * 2}) {
+    const double t = cptree::time_of(cptree::load_of(w, piece), c);
+    if (t < time) time = t, best = piece;
+  }
+  return std::max(1, best);
 }
 
 // Adds a row, in pieces of kPieceTokens tokens.
@@ -67,9 +83,8 @@ bool cut_rows(AttnPlan& out, const cp_attn_desc& d, double keys, int per_turn, i
       work.per_split.push_back(r.n * d.num_kv_heads);
       work.partial.push_back(r.n * d.num_q_heads);
     }
-    double time = 0;
-    const int turns = cptree::best_piece(work, cost_of(d.head_dim, false, memory_us(d, keys)), &time);
-    out.piece = (int)std::min<int64_t>(most, (int64_t)std::max(1, turns) * per_turn);
+    const int turns = piece_of(work, cost_of(d.head_dim, false, memory_us(d, keys)));
+    out.piece = (int)std::min<int64_t>(most, (int64_t)turns * per_turn);
   }
   int64_t partial = 0, items = 0, longest = 0;
   for (TokenRow& r : out.rows) {
@@ -96,7 +111,7 @@ void cut_groups(AttnPlan& out, const cp_attn_desc& d, bool wide) {
   int64_t uncut = 0;
   double keys = 0;
   for (size_t i = 0; i < out.prefix.size(); ++i)
-    if (out.prefix[i].wide == wide) {
+    if ((out.prefix[i].wide != kNarrow) == wide) {
       uncut += prefix_items(out.prefix[i], G, d.num_kv_heads);
       keys += out.prefix[i].keys;
     }
@@ -105,17 +120,16 @@ void cut_groups(AttnPlan& out, const cp_attn_desc& d, bool wide) {
   if (uncut < kUncut) {
     for (size_t i = 0; i < out.prefix.size(); ++i) {
       const PrefixRow& p = out.prefix[i];
-      if (out.prefix[i].wide != wide) continue;
+      if ((out.prefix[i].wide != kNarrow) != wide) continue;
       work.turns.push_back((uint32_t)ceil_div(p.keys, turn));
       work.per_split.push_back((uint32_t)prefix_items(p, G, d.num_kv_heads));
       work.partial.push_back((uint32_t)((int64_t)p.n * d.num_q_heads));
     }
-    double time = 0;
-    piece = std::max(1, cptree::best_piece(work, cost_of(d.head_dim, wide, memory_us(d, keys)), &time));
+    piece = piece_of(work, cost_of(d.head_dim, wide, memory_us(d, keys)));
   }
   for (size_t i = 0; i < out.prefix.size(); ++i) {
     PrefixRow& p = out.prefix[i];
-    if (out.prefix[i].wide != wide) continue;
+    if ((out.prefix[i].wide != kNarrow) != wide) continue;
     const int64_t turns = ceil_div(p.keys, turn);
     const int64_t per = ceil_div(turns, std::min<int64_t>(kMaxGroupSplits, ceil_div(turns, piece)));
     p.n_split = (int32_t)ceil_div(turns, per);
@@ -162,7 +176,13 @@ bool plan_prefix(const cp_attn_desc& desc, const cp_row_meta* rows, int32_t n_ro
     add_row(out, tok, rows[i], ref);
     tok += rows[i].chunk_len;
   }
-  for (PrefixRow& p : out.prefix) p.wide = (int64_t)p.n * G > kNarrowTile;
+  double common = 0;
+  for (const PrefixRow& p : out.prefix) common += p.keys;
+  const bool large = common * desc.num_kv_heads * desc.head_dim * 4.0 > kStreamBytes;
+  for (PrefixRow& p : out.prefix) {
+    const int64_t m = (int64_t)p.n * G;
+    p.wide = m <= kNarrowTile ? kNarrow : m <= kWideTile && large ? kStreamed : kCached;
+  }
   cut_groups(out, desc, false);
   cut_groups(out, desc, true);
   for (PrefixRow& p : out.prefix) {

@@ -26,6 +26,8 @@ constexpr int kMaxGroupSplits = 128;
 // A group's (token, q head) rows per kv head that a workgroup takes: the narrow
 // kernel's waves share the keys, the wide one's the rows.
 constexpr int kNarrowTile = 32, kWideTile = 128;
+// PrefixRow::wide: a group's kernel, and how a wide one reads its keys.
+constexpr int32_t kNarrow = 0, kCached = 1, kStreamed = 2;
 
 struct TokenRow {    // a piece of a row's tokens
   int32_t tok0, n, start, req;
@@ -53,7 +55,7 @@ bool plan_prefix(const cp_attn_desc& desc, const cp_row_meta* rows, int32_t n_ro
 
 // Workgroups of a group's common keys.
 inline int64_t prefix_items(const PrefixRow& p, int group, int hkv) {
-  const int tile = p.wide ? kWideTile : kNarrowTile;
+  const int tile = p.wide != kNarrow ? kWideTile : kNarrowTile;
   return ((int64_t)p.n * group + tile - 1) / tile * hkv * p.n_split;
 }
 

@@ -43,6 +43,17 @@ using namespace cpattn;
 using namespace cpattn::prefill_impl;
 using cpcache::AttnArgs;  // not cpattn's
 
+// prefill_impl::copy16_to_lds past the caches, for keys that one workgroup reads
+__device__ __forceinline__ void copy16_to_lds_nt(const uint16_t* base, uint32_t byte_off,
+                                                 uint8_t* lds) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  const uint32_t dst = (uint32_t)(uintptr_t)(lds_ptr_t)lds;
+  asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, %1 nt" ::"v"(byte_off), "s"(base),
+               "{m0}"(dst)
+               : "memory");
+#endif
+}
+
 // The pointers come as arguments of their own, which may be restrict: the table's
 // entries are then scalar loads, and no wait for one drains the copies on their way.
 template <int D, int B, int G>
@@ -102,6 +113,12 @@ __global__ __launch_bounds__(2 * kWideTile, 2) void shared_wide_kernel(
   const Vis vis{it.kv_end};
   const int hq = a.hq, hkv = a.hkv, mbr = a.mbr;
   const float scale_log2 = a.scale_log2;
+  // what the tile copies K and V with
+  const bool streamed = row.wide == kStreamed;
+  const auto copy16_to_lds = [&](const uint16_t* base, uint32_t byte_off, uint8_t* lds) {
+    if (streamed) copy16_to_lds_nt(base, byte_off, lds);
+    else prefill_impl::copy16_to_lds(base, byte_off, lds);
+  };
 #include "prefill_tile.inc"
 }
 

@@ -65,7 +65,7 @@ void check(const cp_attn_desc& d, const std::vector<cp_row_meta>& rows,
     std::vector<Range> parts;
     for (size_t i = 0; i < p.prefix.size(); ++i) {
       const PrefixRow& g = p.prefix[i];
-      const int64_t turn = p.prefix[i].wide ? kWideTurn : kTurn;
+      const int64_t turn = p.prefix[i].wide != kNarrow ? kWideTurn : kTurn;
       CHECK(g.n >= 1 && g.keys >= B && g.keys % B == 0 && g.split_keys >= 1);
       CHECK(g.n_split >= 1 && g.n_split <= kMaxGroupSplits);
       CHECK((int64_t)g.n_split * g.split_keys >= g.keys && (int64_t)(g.n_split - 1) * g.split_keys < g.keys);
