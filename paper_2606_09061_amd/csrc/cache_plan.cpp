@@ -34,7 +34,16 @@ cptree::Cost cost_of(int d, bool wide, double memory) {
   return {kTurn, 5.5 * x, 0.3 + 1.2 * x, 3.2, 5.5, 0.3 * x, memory};
 }
 
-// Common K and V beyond which groups of one wide tile read them past the caches.
+// A narrow workgroup starts and ends sooner, a wide one takes four times the rows
+// and reads K and V for all of them: groups of up to kWideTile rows stay narrow while
+// there are few common keys in all.  us, narrow / wide, on 32/8 heads: one group of 36
+// rows and 256 keys 11.0 / 12.5, 1,000 keys 11.7 / 13.6, 4,000 keys 16.3 / 15.8, 16,000
+// keys 31 / 26; of 128 rows 13.5 / 14.8, 15.7 / 17.1, 23.6 / 19.6, 53 / 31; 8 groups of
+// 36 rows and 256 keys 19.9 / 15.9.
+constexpr double kNarrowKeys = 1536;
+// Common K and V beyond which groups of one wide tile read them past the caches: 8
+// groups of 128 rows and 4,096 keys on 64/8 heads, 134 MB, 49 -> 43 us; one of 8,192
+// on 32/8, 34 MB, 25.1 -> 25.8.
 constexpr double kStreamBytes = 64e6;
 
 // us that keys take to come from memory
@@ -179,9 +188,10 @@ bool plan_prefix(const cp_attn_desc& desc, const cp_row_meta* rows, int32_t n_ro
   double common = 0;
   for (const PrefixRow& p : out.prefix) common += p.keys;
   const bool large = common * desc.num_kv_heads * desc.head_dim * 4.0 > kStreamBytes;
+  const int64_t narrow = common <= kNarrowKeys ? kWideTile : kNarrowTile;
   for (PrefixRow& p : out.prefix) {
     const int64_t m = (int64_t)p.n * G;
-    p.wide = m <= kNarrowTile ? kNarrow : m <= kWideTile && large ? kStreamed : kCached;
+    p.wide = m <= narrow ? kNarrow : m <= kWideTile && large ? kStreamed : kCached;
   }
   cut_groups(out, desc, false);
   cut_groups(out, desc, true);
