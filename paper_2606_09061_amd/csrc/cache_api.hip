@@ -146,7 +146,7 @@ int by_rows(const std::vector<R>& rows, int32_t R::*item0, int64_t most, Items&&
 // Pages that a workgroup scores: a turn of its waves (64 pages of head_dim 128), and
 // as many more as leave kScoreItems workgroups.
 constexpr int kLeastChunk = 64, kMostChunk = 512;
-constexpr int64_t kScoreItems = 2048;
+constexpr int64_t kScoreItems = 1024;
 
 // The scores that cp_page_select keeps: rows whose tokens may have to choose.
 int64_t plan_select(const cp_attn_desc& d, const cp_row_meta* rows, int32_t n_rows, int32_t n_pages,

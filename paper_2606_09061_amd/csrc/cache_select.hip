@@ -89,12 +89,20 @@ __global__ __launch_bounds__(kThreads, G <= 4 ? 4 : 2) void score_kernel(
   uint64_t* dst = scores + row.score0 + ((int64_t)j * a.hkv + h) * row.stride;
   const int group = lane / L;
   constexpr int STEP = kWaves * PPW * U;
-  int32_t blk[U];
-  const auto load_entries = [&](int b) {  // past the last page that one again
-#pragma unroll
-    for (int u = 0; u < U; ++u) blk[u] = bt_row[min(b + u * PPW + group, p1 - 1)];
+  const int begin = p0 + wave * PPW * U;
+  if (begin >= p1) return;  // whole wave
+  // past the last page that one again
+  const auto entry = [&](int b, int u) { return bt_row[min(b + u * PPW + group, p1 - 1)]; };
+  const auto there = [&](int blk) { return blk >= 0 && blk < a.num_blocks; };
+  int32_t blk[U], blk_next[U];
+  uint4 lo[U], hi[U];
+  const auto load = [&](int u, int at) {
+    const uint4* src = bounds + ((int64_t)(there(at) ? at : 0) * a.hkv + h) * 2 * L + sub;
+    lo[u] = cpattn::ld_global16_nt(src);
+    hi[u] = cpattn::ld_global16_nt(src + L);
   };
-  load_entries(p0 + wave * PPW * U);
+#pragma unroll
+  for (int u = 0; u < U; ++u) blk[u] = entry(begin, u);
   double qd[G][8];
 #pragma unroll
   for (int e = 0; e < G; ++e) {
@@ -103,22 +111,22 @@ __global__ __launch_bounds__(kThreads, G <= 4 ? 4 : 2) void score_kernel(
 #pragma unroll
     for (int i = 0; i < 8; ++i) qd[e][i] = (double)(i & 1 ? bf16hi(w[i / 2]) : bf16lo(w[i / 2]));
   }
-  for (int b = p0 + wave * PPW * U; b < p1; b += STEP) {
-    uint4 lo[U], hi[U];
-    bool there[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      there[u] = blk[u] >= 0 && blk[u] < a.num_blocks;
-      const uint4* src = bounds + ((int64_t)(there[u] ? blk[u] : 0) * a.hkv + h) * 2 * L + sub;
-      lo[u] = cpattn::ld_global16_nt(src);
-      hi[u] = cpattn::ld_global16_nt(src + L);
-    }
-    load_entries(min(b + STEP, p1 - 1));
+  for (int u = 0; u < U; ++u) load(u, blk[u]);
+#pragma unroll
+  for (int u = 0; u < U; ++u) blk_next[u] = entry(begin + STEP, u);
+  for (int b = begin; b < p1; b += STEP) {
     double sum[U * H];
+    uint32_t found = 0;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const uint32_t lw[4] = {lo[u].x, lo[u].y, lo[u].z, lo[u].w};
       const uint32_t hw[4] = {hi[u].x, hi[u].y, hi[u].z, hi[u].w};
+      // the next pages' bounds are on their way while these are in use
+      found |= there(blk[u]) ? 1u << u : 0u;
+      blk[u] = blk_next[u];
+      load(u, blk[u]);
+      blk_next[u] = entry(b + 2 * STEP, u);
       double s[G];
 #pragma unroll
       for (int e = 0; e < G; ++e) s[e] = 0.0;
@@ -146,8 +154,7 @@ __global__ __launch_bounds__(kThreads, G <= 4 ? 4 : 2) void score_kernel(
     if constexpr (G > 1) k = max(k, partner64<4>(k));
     if constexpr (L == 16 && H4 > 1) k = max(k, partner64<8>(k));
     const int u = lane & 3, page = b + u * PPW + group;
-    const bool found = u == 0 ? there[0] : u == 1 ? there[1] : u == 2 ? there[2] : there[3];
-    if (sub < U && page < p1) dst[page] = found ? k : 0;
+    if (sub < U && page < p1) dst[page] = found >> u & 1 ? k : 0;
   }
 }
 
