@@ -147,6 +147,16 @@ int by_rows(const std::vector<R>& rows, int32_t R::*item0, int64_t most, Items&&
 // as many more as leave kScoreItems workgroups.
 constexpr int kLeastChunk = 64, kMostChunk = 512;
 constexpr int64_t kScoreItems = 1024;
+// Whether one launch does both, a workgroup of 8 or 16 waves each (token, kv head):
+// where their number is about the CUs', or there are few pages to score and no more
+// than that.  us, one launch / two, on 32/8 heads: 63 pages, 8 to 256 (token, kv
+// head)s 6.9 to 8.6 / 10.4 to 11.8, 512 15.7 / 14.3; 251 pages, 8 10.4 / 9.1, 128 11.8
+// / 12.4, 256 13.1 / 16.4, 512 24.9 / 26.2, 1,024 57 / 50; 938 pages, 8 23 / 10, 256 28
+// / 36, 512 56 / 60.  64/8 heads agree.
+bool in_one(int64_t units, int most) {
+  if (most > kOnePages) return false;
+  return most <= 128 ? units <= 256 : units >= 128 && units <= 512;
+}
 
 // The scores that cp_page_select keeps: rows whose tokens may have to choose.
 int64_t plan_select(const cp_attn_desc& d, const cp_row_meta* rows, int32_t n_rows, int32_t n_pages,
@@ -428,6 +438,13 @@ int cp_page_select(const cp_attn_desc* desc, const void* q, const void* bounds,
                        n_first,
                        n_last,
                        chunk};
+    const auto choices = [&](const SelectRow& r) { return (int64_t)r.n * hkv; };
+    if (in_one(tokens * hkv, most))
+      return by_rows<SelectRow, kSelectRows>(
+          plan, &SelectRow::item0, kMaxItems, choices,
+          [&](SelectRows& batch, int n, int items, size_t) {
+            return finish(launch_select(desc->head_dim, a, batch, n, items, s), s);
+          });
     scored.clear();
     for (const SelectRow& r : plan)
       if (r.stride > 0) scored.push_back(r);
@@ -441,7 +458,7 @@ int cp_page_select(const cp_attn_desc* desc, const void* q, const void* bounds,
         });
     if (rc != CP_OK) return rc;
     return by_rows<SelectRow, kSelectRows>(
-        plan, &SelectRow::item0, kMaxItems, [&](const SelectRow& r) { return (int64_t)r.n * hkv; },
+        plan, &SelectRow::item0, kMaxItems, choices,
         [&](SelectRows& batch, int n, int items, size_t) {
           return finish(launch_choose(a, batch, n, items, most, s), s);
         });

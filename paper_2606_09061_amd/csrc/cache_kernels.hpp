@@ -63,6 +63,10 @@ hipError_t launch_bounds(int d, int block, const BoundsArgs& a, const BoundsRows
                          int pages, hipStream_t s);
 hipError_t launch_score(int d, const SelectArgs& a, const SelectRows& rows, int n_rows, int items,
                         hipStream_t s);
+// scores and choice of tokens that have up to kOnePages pages
+constexpr int kOnePages = 1024;
+hipError_t launch_select(int d, const SelectArgs& a, const SelectRows& rows, int n_rows, int items,
+                         hipStream_t s);
 // most: the largest number of pages of a token
 hipError_t launch_choose(const SelectArgs& a, const SelectRows& rows, int n_rows, int items,
                          int most, hipStream_t s);

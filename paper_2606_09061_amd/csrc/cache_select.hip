@@ -4,6 +4,8 @@
 // have with one of a group's q heads.  Which pages are selected hangs on the
 // order of the scores, so they are fp64: products of bf16 are exact in it and
 // their sums are, for all but extreme values, too, whatever their order.
+#include <type_traits>
+
 #include "cache_device.hpp"
 
 namespace cpcache {
@@ -61,34 +63,27 @@ __device__ __forceinline__ void sum_step(double* u, int lane) {
   }
 }
 
-// Scores.  A workgroup takes a.chunk pages of one (token, kv head), its waves
-// 64 / L of them at a time, L = D / 8 lanes a page with 8 features each.  With
-// lo + hi and hi - lo of a feature, 2 max(q lo, q hi) = q (lo + hi) + |q| (hi - lo):
+// Scores of pages [p0, p1) of kv head h of token t, by the NW waves of a workgroup:
+// store(page, key).  A wave takes 64 / L pages at a time, L = D / 8 lanes a page with
+// 8 features each.  With lo + hi and hi - lo of a feature,
+//     2 max(q lo, q hi) = q (lo + hi) + |q| (hi - lo):
 // two fp64 multiply-adds per head and feature.  Sums over a page's lanes are split
 // by head first, then by the U pages that the lanes have in hand.  At 4 heads a
-// group that is some 170 vector operations per 2 KB of bounds.
-template <int D, int G, class Rows>
-__global__ __launch_bounds__(kThreads, G <= 4 ? 4 : 2) void score_kernel(
-    const Rows rows, const SelectArgs a, const uint16_t* __restrict__ q,
-    const uint4* __restrict__ bounds, const int32_t* __restrict__ bt,
-    uint64_t* __restrict__ scores) {
+// group that is some 170 vector operations per 2 KB of bounds.  (On the fp64 matrix
+// instructions, 4x4x4 in four blocks, the scores of 32 requests of ~34,000 keys took
+// 78 us on 32/8 heads and 189 on 64/8, here 55 and 76.)
+template <int D, int G, int NW, class Store>
+__device__ __forceinline__ void score_pages(const SelectArgs& a, int64_t t, int h,
+                                            const int32_t* __restrict__ bt_row, int p0, int p1,
+                                            const uint16_t* __restrict__ q,
+                                            const uint4* __restrict__ bounds, Store&& store) {
   constexpr int L = D / 8, PPW = 64 / L, U = 4;  // pages per load, loads in flight
   // heads per lane behind the steps over lane bits 4 and 8
   constexpr int H4 = G > 1 ? G / 2 : 1, H = L == 16 && H4 > 1 ? H4 / 2 : H4;
   const int lane = threadIdx.x & 63, sub = lane % L;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const SelectRow row = rows.r[row_index(rows.r, &SelectRow::item0, (int)blockIdx.x)];
-  const int chunks = (row.stride + a.chunk - 1) / a.chunk;
-  const int x = (int)blockIdx.x - row.item0;
-  const int chunk = x % chunks, h = x / chunks % a.hkv, j = x / chunks / a.hkv;
-  const int n_pages = (row.start + j) / a.block + 1;  // of this token
-  const int p0 = chunk * a.chunk, p1 = min(n_pages, p0 + a.chunk);
-  if (p0 >= p1) return;
-  const int64_t t = (int64_t)row.tok0 + j;
-  const int32_t* bt_row = bt + (int64_t)row.req * a.mbr;
-  uint64_t* dst = scores + row.score0 + ((int64_t)j * a.hkv + h) * row.stride;
   const int group = lane / L;
-  constexpr int STEP = kWaves * PPW * U;
+  constexpr int STEP = NW * PPW * U;
   const int begin = p0 + wave * PPW * U;
   if (begin >= p1) return;  // whole wave
   // past the last page that one again
@@ -154,8 +149,25 @@ __global__ __launch_bounds__(kThreads, G <= 4 ? 4 : 2) void score_kernel(
     if constexpr (G > 1) k = max(k, partner64<4>(k));
     if constexpr (L == 16 && H4 > 1) k = max(k, partner64<8>(k));
     const int u = lane & 3, page = b + u * PPW + group;
-    if (sub < U && page < p1) dst[page] = found >> u & 1 ? k : 0;
+    if (sub < U && page < p1) store(page, found >> u & 1 ? k : 0);
   }
+}
+
+// A workgroup of the scores takes a.chunk pages of one (token, kv head).
+template <int D, int G, class Rows>
+__global__ __launch_bounds__(kThreads, G <= 4 ? 4 : 2) void score_kernel(
+    const Rows rows, const SelectArgs a, const uint16_t* __restrict__ q,
+    const uint4* __restrict__ bounds, const int32_t* __restrict__ bt,
+    uint64_t* __restrict__ scores) {
+  const SelectRow row = rows.r[row_index(rows.r, &SelectRow::item0, (int)blockIdx.x)];
+  const int chunks = (row.stride + a.chunk - 1) / a.chunk;
+  const int x = (int)blockIdx.x - row.item0;
+  const int chunk = x % chunks, h = x / chunks % a.hkv, j = x / chunks / a.hkv;
+  const int p0 = chunk * a.chunk, p1 = min((row.start + j) / a.block + 1, p0 + a.chunk);
+  if (p0 >= p1) return;
+  uint64_t* dst = scores + row.score0 + ((int64_t)j * a.hkv + h) * row.stride;
+  score_pages<D, G, kWaves>(a, (int64_t)row.tok0 + j, h, bt + (int64_t)row.req * a.mbr, p0, p1, q,
+                            bounds, [&](int page, uint64_t key) { dst[page] = key; });
 }
 
 // Inclusive sum of x over the lanes of a wave.
@@ -182,34 +194,30 @@ __device__ __forceinline__ uint64_t max64(uint64_t x) {
   return max(x, (uint64_t)__shfl_xor((unsigned long long)x, 32, 64));
 }
 
-// Where the selected pages of a (token, kv head) go, and how many it has to choose
-// from.
+// A (token, kv head) that selects: item blockIdx.x of the launch.
 struct Choice {
-  int n;
-  const uint64_t* src;
-  int32_t* dst;
+  int n;  // pages to choose from
+  int64_t t;
+  int h, req;
+  int64_t score0;  // the first of its scores
 };
 
 template <class Rows>
-__device__ __forceinline__ Choice choice_of(const Rows& rows, const SelectArgs& a,
-                                            const uint64_t* scores) {
+__device__ __forceinline__ Choice choice_of(const Rows& rows, const SelectArgs& a) {
   const SelectRow row = rows.r[row_index(rows.r, &SelectRow::item0, (int)blockIdx.x)];
   const int x = (int)blockIdx.x - row.item0, h = x % a.hkv, j = x / a.hkv;
-  const int64_t t = (int64_t)row.tok0 + j;
-  return Choice{(row.start + j) / a.block + 1,
-                scores + row.score0 + ((int64_t)j * a.hkv + h) * row.stride,
-                a.pages + (t * a.hkv + h) * a.n_pages};
+  return Choice{(row.start + j) / a.block + 1, (int64_t)row.tok0 + j, h, row.req,
+                row.score0 + ((int64_t)j * a.hkv + h) * row.stride};
 }
 
-// The choice: one workgroup of NT threads per (token, kv head), which holds up to
-// NT NU keys in registers.  The fixed pages aside, the place of the threshold
-// is found eight bits at a time from the highest one in which the keys differ,
-// by a histogram of the keys that agree with the bits known so far.  Once few keys
-// are left, or all of them are selected, each counts those before it.  The
-// selected pages are written in order, by the ballots of the waves.
-template <int NT, int NU, class Rows>
-__global__ __launch_bounds__(NT) void choose_kernel(const Rows rows, const SelectArgs a,
-                                                    const uint64_t* __restrict__ scores) {
+// The choice of a.n_pages of n > a.n_pages pages, by a workgroup of NT threads that
+// holds up to NT NU keys, src(page), in registers.  The fixed pages aside, the
+// place of the threshold is found eight bits at a time from the highest one in
+// which the keys differ, by a histogram of the keys that agree with the bits known
+// so far.  Once few keys are left, or all of them are selected, each counts those
+// before it.  The selected pages are written in order, by the ballots of the waves.
+template <int NT, int NU, class Src>
+__device__ __forceinline__ void choose_pages(const SelectArgs& a, int n, Src&& src, int32_t* dst) {
   constexpr int NW = NT / 64, kFew = 128, NC = NU * NW, CPL = NC > 64 ? NC / 64 : 1;
   static_assert(NW <= 16 && NT % kFew == 0 && (NC <= 64 || NC == 64 * CPL), "geometry");
   __shared__ __align__(16) int s_hist[2][256];
@@ -217,20 +225,15 @@ __global__ __launch_bounds__(NT) void choose_kernel(const Rows rows, const Selec
   __shared__ uint64_t s_max[16], s_not_min[16], s_key[kFew];
   __shared__ int s_page[kFew], s_digit, s_left, s_in, s_few;
   __shared__ unsigned long long s_take[NC];
-  const Choice c = choice_of(rows, a, scores);
-  const int n = c.n, P = a.n_pages, tid = threadIdx.x, lane = tid & 63;
+  const int P = a.n_pages, tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  if (n <= P) {  // all of them
-    for (int i = tid; i < P; i += NT) c.dst[i] = i < n ? i : -1;
-    return;
-  }
   // n > P >= fixed pages: those are apart
   const int first = a.n_first, last = n - a.n_last;  // chosen from: [first, last)
   uint64_t key[NU];
 #pragma unroll
   for (int u = 0; u < NU; ++u) {
     const int i = u * NT + tid;
-    key[u] = i >= first && i < last ? c.src[i] : 0;
+    key[u] = i >= first && i < last ? src(i) : 0;
   }
   for (int x = tid; x < 512; x += NT) s_hist[x >> 8][x & 255] = 0;
   if (tid < 2 * CPL * 64) s_count[0][tid] = 0;  // (NT >= 2 CPL 64)
@@ -359,8 +362,41 @@ __global__ __launch_bounds__(NT) void choose_kernel(const Rows rows, const Selec
 #pragma unroll
   for (int u = 0; u < NU; ++u) {
     const int at = position(chosen, u, before);
-    if (chosen >> u & 1) c.dst[at] = u * NT + tid;
+    if (chosen >> u & 1) dst[at] = u * NT + tid;
   }
+}
+
+// All of n <= a.n_pages pages.
+__device__ __forceinline__ void take_all(const SelectArgs& a, int n, int32_t* dst) {
+  for (int i = threadIdx.x; i < a.n_pages; i += blockDim.x) dst[i] = i < n ? i : -1;
+}
+
+template <int NT, int NU, class Rows>
+__global__ __launch_bounds__(NT) void choose_kernel(const Rows rows, const SelectArgs a,
+                                                    const uint64_t* __restrict__ scores) {
+  const Choice c = choice_of(rows, a);
+  int32_t* dst = a.pages + (c.t * a.hkv + c.h) * a.n_pages;
+  if (c.n <= a.n_pages) return take_all(a, c.n, dst);
+  const uint64_t* src = scores + c.score0;
+  choose_pages<NT, NU>(a, c.n, [&](int i) { return src[i]; }, dst);
+}
+
+// Scores and choice in one, for up to kOnePages pages a token.
+template <int G>
+constexpr int kOneThreads = G <= 4 ? 1024 : 512;  // (128 and 256 registers a lane)
+template <int D, int G, class Rows>
+__global__ __launch_bounds__(kOneThreads<G>) void select_kernel(
+    const Rows rows, const SelectArgs a, const uint16_t* __restrict__ q,
+    const uint4* __restrict__ bounds, const int32_t* __restrict__ bt) {
+  constexpr int NT = kOneThreads<G>;
+  __shared__ uint64_t s_score[kOnePages];
+  const Choice c = choice_of(rows, a);
+  int32_t* dst = a.pages + (c.t * a.hkv + c.h) * a.n_pages;
+  if (c.n <= a.n_pages) return take_all(a, c.n, dst);
+  score_pages<D, G, NT / 64>(a, c.t, c.h, bt + (int64_t)c.req * a.mbr, 0, c.n, q, bounds,
+                             [&](int page, uint64_t key) { s_score[page] = key; });
+  __syncthreads();
+  choose_pages<NT, kOnePages / NT>(a, c.n, [&](int i) { return s_score[i]; }, dst);
 }
 
 // Exclusive sum of x over the workgroup's threads; `total` gets the whole.
@@ -391,14 +427,13 @@ __global__ __launch_bounds__(kThreads) void choose_long_kernel(const Rows rows, 
   __shared__ int s_hist[256];
   __shared__ int s_wave[kWaves];
   __shared__ int s_digit, s_left;
-  const Choice c = choice_of(rows, a, scores);
+  const Choice c = choice_of(rows, a);
+  int32_t* dst = a.pages + (c.t * a.hkv + c.h) * a.n_pages;
+  if (c.n <= a.n_pages) return take_all(a, c.n, dst);
+  const uint64_t* src = scores + c.score0;
   const int n = c.n, P = a.n_pages, tid = threadIdx.x;
-  if (n <= P) {  // all of them
-    for (int i = tid; i < P; i += kThreads) c.dst[i] = i < n ? i : -1;
-    return;
-  }
   const auto key = [&](int i) {
-    return i < a.n_first || i >= n - a.n_last ? kForcedKey : c.src[i];
+    return i < a.n_first || i >= n - a.n_last ? kForcedKey : src[i];
   };
   uint64_t known = 0;  // the bits of the threshold found so far
   int left = P;        // of the keys that agree with them, how many are selected
@@ -430,7 +465,7 @@ __global__ __launch_bounds__(kThreads) void choose_long_kernel(const Rows rows, 
     const int rank = scan(equal ? 1 : 0, s_wave, &equals);
     const bool take = i < n && (k > known || (equal && rank < left));
     const int at = scan(take ? 1 : 0, s_wave, &chosen);
-    if (take) c.dst[out + at] = i;
+    if (take) dst[out + at] = i;
     out += chosen;
     left -= min(left, equals);
   }
@@ -438,24 +473,43 @@ __global__ __launch_bounds__(kThreads) void choose_long_kernel(const Rows rows, 
 
 template <int D, int G>
 hipError_t launch_score_t(const SelectArgs& a, const SelectRows& rows, int n_rows, int items,
-                          hipStream_t s) {
+                          bool one, hipStream_t s) {
   return by_size(rows, n_rows, [&](const auto& r) {
-    hipLaunchKernelGGL((score_kernel<D, G>), dim3(items), dim3(kThreads), 0, s, r, a, a.q,
-                       (const uint4*)a.bounds, a.bt, a.scores);
+    if (one)
+      hipLaunchKernelGGL((select_kernel<D, G>), dim3(items), dim3(kOneThreads<G>), 0, s, r, a, a.q,
+                         (const uint4*)a.bounds, a.bt);
+    else
+      hipLaunchKernelGGL((score_kernel<D, G>), dim3(items), dim3(kThreads), 0, s, r, a, a.q,
+                         (const uint4*)a.bounds, a.bt, a.scores);
   });
+}
+
+hipError_t launch_score_g(int d, const SelectArgs& a, const SelectRows& rows, int n_rows, int items,
+                          bool one, hipStream_t s) {
+  const auto f = [&](auto g) {
+    constexpr int G = decltype(g)::value;
+    return d == 128 ? launch_score_t<128, G>(a, rows, n_rows, items, one, s)
+                    : launch_score_t<64, G>(a, rows, n_rows, items, one, s);
+  };
+  switch (a.hq / a.hkv) {
+    case 1: return f(std::integral_constant<int, 1>());
+    case 2: return f(std::integral_constant<int, 2>());
+    case 4: return f(std::integral_constant<int, 4>());
+    case 8: return f(std::integral_constant<int, 8>());
+  }
+  return hipErrorInvalidValue;
 }
 
 }  // namespace
 
 hipError_t launch_score(int d, const SelectArgs& a, const SelectRows& rows, int n_rows, int items,
                         hipStream_t s) {
-  switch (a.hq / a.hkv) {
-    case 1: return (d == 128 ? launch_score_t<128, 1> : launch_score_t<64, 1>)(a, rows, n_rows, items, s);
-    case 2: return (d == 128 ? launch_score_t<128, 2> : launch_score_t<64, 2>)(a, rows, n_rows, items, s);
-    case 4: return (d == 128 ? launch_score_t<128, 4> : launch_score_t<64, 4>)(a, rows, n_rows, items, s);
-    case 8: return (d == 128 ? launch_score_t<128, 8> : launch_score_t<64, 8>)(a, rows, n_rows, items, s);
-  }
-  return hipErrorInvalidValue;
+  return launch_score_g(d, a, rows, n_rows, items, false, s);
+}
+
+hipError_t launch_select(int d, const SelectArgs& a, const SelectRows& rows, int n_rows, int items,
+                         hipStream_t s) {
+  return launch_score_g(d, a, rows, n_rows, items, true, s);
 }
 
 hipError_t launch_choose(const SelectArgs& a, const SelectRows& rows, int n_rows, int items,

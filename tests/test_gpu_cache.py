@@ -369,6 +369,15 @@ def test_select_of_long_contexts_with_equal_scores(ctx, n_pages):
     s.check(n_pages, 0, 0)
 
 
+@pytest.mark.parametrize("reqs,pages", [(1, 127), (1, 128), (1, 129), (64, 100), (65, 100), (128, 60),
+                                        (32, 300), (31, 130), (129, 140), (40, 1023), (40, 1025)])
+@pytest.mark.parametrize("hq,hkv", [(8, 4), (32, 4)])
+def test_select_in_one_launch_and_in_two(reqs, pages, hq, hkv):
+    """Around the numbers of rows and pages at which the launches change."""
+    rows = [(16 * pages - 1 - 16 * (r % 3) * (pages > 3), 1) for r in range(reqs)]
+    Select(hq, hkv, 64, 16, rows, reqs + pages, pool=700).check(21, 2, 3)
+
+
 def test_select_scores_a_hair_apart():
     """Scores that 32 bits cannot tell apart: 2^24 and the sums of it and 1, 2, ..."""
     s = Select(1, 1, 64, 16, [(16 * 50 - 1, 1)], 3)
