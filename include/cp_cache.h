@@ -54,7 +54,8 @@ extern "C" {
  * The q heads go to q[T][Hq][D], the k and v heads to slot p of the request's
  * pages, whatever `positions` holds.  The same bits as the two calls; every
  * other slot is left untouched, and a slot whose table entry lies outside
- * [0, num_blocks) is not written.  theta > 1, eps > 0; sm_scale is not used. */
+ * [0, num_blocks) is not written.  q overlaps none of the inputs.  theta > 1,
+ * eps > 0; sm_scale is not used. */
 int cp_qkv_append(const cp_attn_desc *desc, const void *qkv, const void *q_norm_w,
                   const void *k_norm_w, const int32_t *positions, double theta, float eps,
                   void *q, void *k_cache, void *v_cache, const int32_t *block_tables,
@@ -83,9 +84,10 @@ size_t cp_page_select_workspace_bytes(const cp_attn_desc *desc, const cp_row_met
  *     s(i) = max over the q heads e of kv head h of
  *            sum_d max(q[t][e][d] lo[i][d], q[t][e][d] hi[i][d]),
  * lo and hi the page's bounds: no key of the page has a larger product with q.
- * Scores are summed in fp64; equal ones go to the lower page, and a score that
- * is NaN counts as larger than any number.  pages[T][Hkv][n_pages] (int32) gets
- * them in rising order, and -1 behind them where there are fewer.
+ * Scores are summed in fp64; equal ones go to the lower page.  (Where q or bounds
+ * hold infinities or NaN, the list is one of that many pages all the same, the
+ * fixed ones among them.)  pages[T][Hkv][n_pages] (int32) gets them in rising
+ * order, and -1 behind them where there are fewer.
  * 1 <= n_pages <= CP_CACHE_MAX_PAGES, n_first, n_last >= 0, n_first + n_last <=
  * n_pages.  Bounds of a page whose table entry lies outside [0, num_blocks) are
  * taken as the lowest score.  bounds 16-byte, pages 4-byte, ws 256-byte

@@ -422,8 +422,11 @@ int cp_page_select(const cp_attn_desc* desc, const void* q, const void* bounds,
     (void)hipGetLastError();
     const int hkv = desc->num_kv_heads;
     int chunk = kLeastChunk, most = 0;
-    while (chunk < kMostChunk && scores > 2 * chunk * kScoreItems) chunk *= 2;
     for (const SelectRow& r : plan) most = std::max(most, (r.start + r.n - 1) / desc->block_size + 1);
+    // (a token's scores fit a launch, whatever its pages and heads)
+    while ((chunk < kMostChunk && scores > 2 * chunk * kScoreItems) ||
+           (int64_t)hkv * (most / chunk + 1) > kMaxItems / 2)
+      chunk *= 2;
     const SelectArgs a{static_cast<const uint16_t*>(q),
                        static_cast<const uint16_t*>(bounds),
                        block_tables,

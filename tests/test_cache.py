@@ -263,6 +263,24 @@ def test_short_workspaces_are_refused():
     assert need > 256 and _attn(d, rows, 600, need - 1) == binding.CP_ERR_WORKSPACE
 
 
+def test_the_largest_batches_are_planned():
+    """The longest rows and the most heads: queries answer, calls get as far as their
+    workspace."""
+    d = _desc(num_q_heads=8192, num_kv_heads=1024, max_blocks_per_req=(1 << 27) - 1)
+    far = 1 << 30
+    for rows in (_rows([0, far - 1, 1, far]), _rows([0, far - 16384, 16384, far])):
+        need = cache.page_select_workspace_bytes(d, rows, 4)
+        assert need >= 1024 * (1 << 26) * 8
+        assert _select(d, rows, ws_bytes=need - 1) == binding.CP_ERR_WORKSPACE
+        assert cache.page_attn_workspace_bytes(d, rows, 4) >= 256
+        need = cache.prefix_attn_workspace_bytes(d, rows, [(0, 1, far - 16384)])
+        assert _prefix(d, rows, [(0, 1, far - 16384)], ws_bytes=need - 1) == binding.CP_ERR_WORKSPACE
+    rows = _rows([0, far - 16384, 16384, far])
+    with pytest.raises(cp.CpError) as e:                 # partial rows past their index type
+        cache.page_attn_workspace_bytes(d, rows, 4096)
+    assert e.value.code == UNSUPPORTED and _attn(d, rows, 4096) == UNSUPPORTED
+
+
 def test_a_select_workspace_serves_smaller_batches():
     d = _desc(max_blocks_per_req=4000)
     sizes = [cache.page_select_workspace_bytes(d, _rows([0, c, 2, c + 2], [1, 50, 1, 51]), 20)

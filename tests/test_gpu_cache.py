@@ -669,6 +669,89 @@ def test_debug_mode_finds_bad_entries(monkeypatch):
         assert e.value.code == cp.binding.CP_ERR_BAD_META
 
 
+def test_calls_refuse_tensors_of_other_kinds():
+    """Type, shape, strides, device; nothing is written."""
+    c = Case(4, 2, 64, 16, [(40, 1), (9, 2)], 17, groups=[(0, 1, 32)])
+    g = c.gpu()
+    q, k, v, bt, t = g["q"], g["k"], g["v"], g["bt"], c.t
+    w = torch.ones(64, dtype=torch.bfloat16, device=DEV)
+    qkv = torch.zeros(t, 8 * 64, dtype=torch.bfloat16, device=DEV)
+    bounds = torch.zeros(k.shape[0], 2, 2, 64, dtype=torch.bfloat16, device=DEV)
+    pages = torch.zeros(t, 2, 3, dtype=torch.int32, device=DEV)
+    out = torch.full_like(q, 7)
+    d = c.desc()
+    calls = {
+        "append": (lambda qkv, qw, kw, q, k, v, bt: cache.qkv_append(
+            d, qkv, qw, kw, c.rows, q, k, v, bt, THETA, EPS),
+            dict(qkv=qkv, qw=w, kw=w, q=out, k=k, v=v, bt=bt)),
+        "bounds": (lambda k, bt, bounds: cache.page_bounds(d, k, bt, c.rows, bounds),
+                   dict(k=k, bt=bt, bounds=bounds)),
+        "select": (lambda q, bounds, bt, pages: cache.page_select(d, q, bounds, bt, c.rows, pages),
+                   dict(q=q, bounds=bounds, bt=bt, pages=pages)),
+        "attn": (lambda q, k, v, bt, pages, out: cache.page_attn(d, q, k, v, bt, pages, c.rows, out),
+                 dict(q=q, k=k, v=v, bt=bt, pages=pages, out=out)),
+        "prefix": (lambda q, k, v, bt, out: cache.prefix_attn(d, q, k, v, bt, c.rows, c.groups, out),
+                   dict(q=q, k=k, v=v, bt=bt, out=out)),
+    }
+    for name, (call, good) in calls.items():
+        for arg, x in good.items():
+            wide = torch.zeros(*x.shape[:-1], 2 * x.shape[-1], dtype=x.dtype, device=DEV)
+            other = torch.int64 if x.dtype == torch.int32 else torch.float16
+            for bad in (x.to(other), x[:-1].contiguous(), wide[..., ::2], x.cpu(), x[None]):
+                with pytest.raises(cp.CpError) as e:
+                    call(**{**good, arg: bad})
+                assert e.value.code == cp.binding.CP_ERR_INVALID_ARG, (name, arg)
+    small = torch.empty(64, dtype=torch.uint8, device=DEV)
+    for call in (lambda: cache.page_select(d, q, bounds, bt, c.rows, pages, ws=small),
+                 lambda: cache.page_attn(d, q, k, v, bt, pages, c.rows, out, small),
+                 lambda: cache.prefix_attn(d, q, k, v, bt, c.rows, c.groups, out, small)):
+        with pytest.raises(cp.CpError) as e:
+            call()
+        assert e.value.code == cp.binding.CP_ERR_WORKSPACE
+    for positions in (torch.zeros(t, dtype=torch.int64, device=DEV),
+                      torch.zeros(t + 1, dtype=torch.int32, device=DEV)):
+        with pytest.raises(cp.CpError):
+            cache.qkv_append(d, qkv, w, w, c.rows, out, k, v, bt, THETA, EPS, positions)
+    torch.cuda.synchronize()
+    assert (out == 7).all() and (bounds == 0).all() and (pages == 0).all()
+    assert same_bits((k, v), (c.k.to(DEV), c.v.to(DEV)))
+
+
+def test_offsets_beyond_32_bits():
+    """Pools of more than 2^31 values and 2^32 bytes, the pages in use at their end:
+    the same bits as in small pools."""
+    hq, hkv, d, block, far = 16, 8, 128, 16, 140000
+    a = Append(hq, hkv, d, block, [(700, 3), (720, 1), (40, 2)], 16)
+    c, (small_k, small_v) = a.c, a.pools
+    c.groups = np.array([(0, 2, 0)], np.int32)
+    nb = c.k.shape[0]
+    small_k.copy_(torch.nan_to_num(c.k, nan=1.0))
+    small_v.copy_(torch.nan_to_num(c.v, nan=1.0))
+    k = torch.empty(far + nb, hkv, block, d, dtype=torch.bfloat16, device=DEV)
+    v = torch.empty(far + nb, hkv, d, block, dtype=torch.bfloat16, device=DEV)
+    b = torch.empty(far + nb, hkv, 2, d, dtype=torch.bfloat16, device=DEV)
+    assert k[:far].numel() > 1 << 31
+    k[far:], v[far:] = small_k, small_v
+    table, results = c.table.copy(), []
+    whole = [(int(s), 0, int(n), int(n)) for s, _, _, n in c.rows]
+    for kk, vv, bb, shift in ((small_k, small_v, torch.empty_like(b[far:]), 0), (k, v, b, far)):
+        bt = torch.from_numpy(table + shift).to(DEV)
+        desc = cp.make_desc(hq, hkv, d, block, kk.shape[0], table.shape[1], len(table), c.scale)
+        q, out, out2 = (torch.empty(c.t, hq, d, dtype=torch.bfloat16, device=DEV) for _ in range(3))
+        pages = torch.empty(c.t, hkv, 7, dtype=torch.int32, device=DEV)
+        cache.qkv_append(desc, a.qkv, a.qw, a.kw, c.rows, q, kk, vv, bt, THETA, EPS)
+        cache.page_bounds(desc, kk, bt, whole, bb)
+        cache.page_select(desc, q, bb, bt, c.rows, pages)
+        cache.page_attn(desc, q, kk, vv, bt, pages, c.rows, out)
+        cache.prefix_attn(desc, q, kk, vv, bt, c.rows, c.groups, out2)
+        used = torch.from_numpy(np.unique(np.concatenate(
+            [c.table[s, :-(-n // block)] for s, _, _, n in c.rows.tolist()]))).to(DEV).long() + shift
+        results.append((q, kk[used], vv[used], bb[used], out, out2, pages.view(torch.int16)))
+    assert same_bits(*results) and torch.isfinite(results[0][4].float()).all()
+    del k, v, b, results
+    torch.cuda.empty_cache()
+
+
 # ---------------------------------------------------------------- a round of them together
 
 def test_a_sparse_decode_round():
