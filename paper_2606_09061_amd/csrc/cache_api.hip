@@ -264,7 +264,7 @@ int launch_plan(const cp_attn_desc* d, const AttnPlan& p, AttnArgs a, hipStream_
     for (int i = n; i <= kAttnRows; ++i) b.r[i] = AttnRow{INT_MAX, end, 0, 0};
     a.part0 = (int)part0, a.n_groups = n_groups, a.group_items = (int)group_items;
     a.items = (int)items;
-    const int per = 4 / p.unit_waves, all = (int)(group_items + (items + per - 1) / per);
+    const int per = std::max(1, 4 / p.unit_waves), all = (int)(group_items + (items + per - 1) / per);
     const hipError_t e = a.pages    ? launch_pages(D, B, a, b, n, all, s)
                          : !wide    ? launch_shared(D, B, a, b, n, all, s)
                          : D == 128 ? launch_shared_wide128(B, a, b, all, s)

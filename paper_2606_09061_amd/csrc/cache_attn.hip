@@ -6,16 +6,29 @@ namespace cpcache {
 
 namespace {
 
-template <int D, int B, class Batch>
-__global__ __launch_bounds__(kThreads, 2) void pages_kernel(
+template <int D, int B, int NW, class Batch>
+__global__ __launch_bounds__(64 * NW, 2) void pages_kernel(
     const Batch b, const AttnArgs a, const uint16_t* __restrict__ q,
     const uint16_t* __restrict__ k_cache, const uint16_t* __restrict__ v_cache,
     const int32_t* __restrict__ bt, const int32_t* __restrict__ pages) {
-  __shared__ __align__(16) uint8_t slices[kWaves][kSlice<D>];
-  __shared__ Shared s;
-  __shared__ int s_blocks[kWaves][kListPages], s_count[kWaves];
-  token_units<D, B, true>(b, (int)blockIdx.x, a, q, k_cache, v_cache, bt, pages, s, s_blocks,
+  constexpr int UNITS = NW == kWaves ? NW : 1;  // at most
+  __shared__ __align__(16) uint8_t slices[NW][kSlice<D>];
+  __shared__ Shared<NW> s;
+  __shared__ int s_blocks[UNITS][kListPages], s_count[UNITS];
+  token_units<D, B, true, NW>(b, (int)blockIdx.x, a, q, k_cache, v_cache, bt, pages, s, s_blocks,
                           s_count, [&](int w) { return slices[w]; });
+}
+
+// Tokens over all of their keys.
+template <int D, int B, class Batch>
+__global__ __launch_bounds__(64 * kAllWaves, 2) void tokens_kernel(
+    const Batch b, const AttnArgs a, const uint16_t* __restrict__ q,
+    const uint16_t* __restrict__ k_cache, const uint16_t* __restrict__ v_cache,
+    const int32_t* __restrict__ bt) {
+  __shared__ __align__(16) uint8_t slices[kAllWaves][kSlice<D>];
+  __shared__ Shared<kAllWaves> s;
+  token_units<D, B, false, kAllWaves>(b, (int)blockIdx.x, a, q, k_cache, v_cache, bt, nullptr, s,
+                                      nullptr, nullptr, [&](int w) { return slices[w]; });
 }
 
 // The groups' workgroups come first, the tokens' behind them.
@@ -25,7 +38,7 @@ __global__ __launch_bounds__(kThreads, 2) void shared_kernel(
     const uint16_t* __restrict__ k_cache, const uint16_t* __restrict__ v_cache,
     const int32_t* __restrict__ bt) {
   __shared__ __align__(16) uint8_t slices[kWaves][kSlice<D>];
-  __shared__ Shared s;
+  __shared__ Shared<kWaves> s;
   const auto slice = [&](int w) { return slices[w]; };
   const int x = (int)blockIdx.x - a.group_items;
   if (x < 0) {
@@ -33,7 +46,7 @@ __global__ __launch_bounds__(kThreads, 2) void shared_kernel(
     group_unit<D, B>(row, (int)blockIdx.x - row.item0, a, q, k_cache, v_cache, bt, s, slice);
     return;
   }
-  token_units<D, B, false>(b, x, a, q, k_cache, v_cache, bt, nullptr, s, nullptr, nullptr, slice);
+  token_units<D, B, false, kWaves>(b, x, a, q, k_cache, v_cache, bt, nullptr, s, nullptr, nullptr, slice);
 }
 
 // Merge of several pieces: with O_s and L_s, a piece's normalised output and the
@@ -124,8 +137,12 @@ template <int D, int B>
 hipError_t launch_pages_t(const AttnArgs& a, const AttnBatch& b, int n_rows, int items,
                           hipStream_t s) {
   return by_size(b, 0, n_rows, [&](const auto& x) {
-    hipLaunchKernelGGL((pages_kernel<D, B>), dim3(items), dim3(kThreads), 0, s, x, a, a.q,
-                       a.k_cache, a.v_cache, a.bt, a.pages);
+    if (1 << a.log2_waves == kAllWaves)
+      hipLaunchKernelGGL((pages_kernel<D, B, kAllWaves>), dim3(items), dim3(64 * kAllWaves), 0, s,
+                         x, a, a.q, a.k_cache, a.v_cache, a.bt, a.pages);
+    else
+      hipLaunchKernelGGL((pages_kernel<D, B, kWaves>), dim3(items), dim3(kThreads), 0, s, x, a,
+                         a.q, a.k_cache, a.v_cache, a.bt, a.pages);
   });
 }
 
@@ -133,8 +150,12 @@ template <int D, int B>
 hipError_t launch_shared_t(const AttnArgs& a, const AttnBatch& b, int n_rows, int items,
                            hipStream_t s) {
   return by_size(b, a.n_groups, n_rows, [&](const auto& x) {
-    hipLaunchKernelGGL((shared_kernel<D, B>), dim3(items), dim3(kThreads), 0, s, x, a, a.q,
-                       a.k_cache, a.v_cache, a.bt);
+    if (1 << a.log2_waves == kAllWaves)
+      hipLaunchKernelGGL((tokens_kernel<D, B>), dim3(items), dim3(64 * kAllWaves), 0, s, x, a, a.q,
+                         a.k_cache, a.v_cache, a.bt);
+    else
+      hipLaunchKernelGGL((shared_kernel<D, B>), dim3(items), dim3(kThreads), 0, s, x, a, a.q,
+                         a.k_cache, a.v_cache, a.bt);
   });
 }
 

@@ -20,18 +20,38 @@ constexpr int64_t kUncut = 8 * cptree::kSlots;
 // where they do, unless long items would end far apart.  us, 1 / 2 / 4 waves, lists
 // of 64 pages on 32/8 heads: 256 items 48 / 31 / 29, 384 48 / 41 / 44, 512 52 / 54 /
 // 56, 768 65 / 85 / 81, 1,024 95 / 104 / 106, 2,048 198 / 223 / 219; of 256 pages: 384
-// 173 / 123 / 130, 512 186 / 165 / 165, 768 262 / 257 / 261, 2,048 739 / 681 / 667.
+// 173 / 123 / 130, 512 186 / 165 / 165, 768 262 / 257 / 261, 2,048 739 / 681 / 667; 352
+// items of 3 turns 25.7 / 19.4 / 20.6.
 int unit_waves(int64_t items, int64_t turns) {
   if (items <= 320) return 4;
-  if (items <= 512) return turns > 8 ? 2 : 1;
+  if (items <= 512) return 2;
   return items <= 1536 || turns <= 16 ? 1 : 4;
 }
 
-// Times of the attention kernels (pieces.hpp), in us.
-cptree::Cost cost_of(int d, bool wide, double memory) {
-  const double x = d / 128.0;
-  if (wide) return {kWideTurn, 0.4 + 2.2 * x, 1.0 + 0.2 * x, 7.0, 3.0, 0.2 * x, memory};
-  return {kTurn, 5.5 * x, 0.3 + 1.2 * x, 3.2, 5.5, 0.3 * x, memory};
+// Whether items of so many turns, uncut, are done in one launch, by eight waves each:
+// where cutting and merging them takes as long.  us in a graph, so / cut or with fewer
+// waves, lists on 32/8 heads of 64: 32 pages (4 turns), 8 items 6.0 / 6.3, 64 items 6.8 /
+// 7.7; 64 pages, 8 items 7.3 / 8.3, 64 items 9.7 / 11.8, 256 items 15.6 / 17.4; 128 pages,
+// 8 items 11.4 / 8.6, 64 items 15.1 / 13, 128 items 18.8 / 20.6; 256 pages, 128 items 31.6 /
+// 33.  Heads of 128: 64 pages, 8 items 9.4 / 9.0 (a launch less is worth 1.6 to the
+// host), 16 items 11.4 / 10.0, 64 items 16.6 / 14.0.
+bool whole(int d, int64_t items, int64_t turns) {
+  if (d == 64) return items <= 256 && (turns <= 8 || (items >= 128 && turns <= 32));
+  return items <= 8 && turns <= 8;
+}
+// Whether tokens of groups read all of their keys so, common ones too, which the
+// caches hold then.  us, so / the groups' keys once, 32/8 heads of 128, 4 requests: 128
+// keys in common 5.3 / 8.6, 500 8.0 / 10.1, 1,000 10.7 / 10.3 (eager 10.2 / 11.0), 2,000 17.7 /
+// 10.7; 32 requests: 500 8.5 / 12.8, 1,000 10.8 / 14.2, 2,000 17.9 / 17.4; 64 requests: 128
+// 10.4 / 12.8, 500 16.6 / 17.3.  4/2 heads of 64, 4 requests: 500 5.9 / 8.0, 1,000 8.3 /
+// 8.2 (8.4 / 11.1); 64 requests: 500 7.4 / 8.9.
+bool ungrouped(int64_t items, int64_t turns) { return items <= 256 && turns <= 8; }
+
+// Times of the attention kernels (pieces.hpp), in us; `merged`: with a merge in any case.
+cptree::Cost cost_of(int d, bool wide, bool merged, double memory) {
+  const double x = d / 128.0, merge = merged ? 0.0 : 4.5;
+  if (wide) return {kWideTurn, 0.4 + 2.2 * x, 1.0 + 0.2 * x, 7.0, merge, 0.2 * x, memory};
+  return {kTurn, 5.5 * x, 0.3 + 1.2 * x, 3.2, merge, 0.3 * x, memory};
 }
 
 // A narrow workgroup starts and ends sooner, a wide one takes four times the rows
@@ -78,21 +98,27 @@ void reset(AttnPlan& out) {
 }
 
 // Cuts the rows' ranges, own(row) units of which `per_turn` make a turn and
-// `most` may make a piece, and lays out the workspace.
+// `most` may make a piece (`one`: in no case), and lays out the workspace.
 template <class Own>
-bool cut_rows(AttnPlan& out, const cp_attn_desc& d, double keys, int per_turn, int most, Own&& own) {
+bool cut_rows(AttnPlan& out, const cp_attn_desc& d, double keys, int per_turn, int most, bool one,
+              Own&& own) {
   thread_local cptree::Work work;
   work.turns.clear(), work.per_split.clear(), work.partial.clear();
-  int64_t uncut = 0;
-  for (const TokenRow& r : out.rows) uncut += (int64_t)r.n * d.num_kv_heads;
+  int64_t uncut = 0, all = 0;
+  for (const TokenRow& r : out.rows)
+    uncut += (int64_t)r.n * d.num_kv_heads, all = std::max<int64_t>(all, own(r));
   out.piece = most;
+  if (one || (out.prefix.empty() && whole(d.head_dim, uncut, ceil_div(all, per_turn)))) {
+    out.unit_waves = kAllWaves;
+    return true;
+  }
   if (uncut < kUncut && !out.rows.empty()) {
     for (const TokenRow& r : out.rows) {
       work.turns.push_back((uint32_t)ceil_div(own(r), per_turn));
       work.per_split.push_back(r.n * d.num_kv_heads);
       work.partial.push_back(r.n * d.num_q_heads);
     }
-    const int turns = piece_of(work, cost_of(d.head_dim, false, memory_us(d, keys)));
+    const int turns = piece_of(work, cost_of(d.head_dim, false, !out.prefix.empty(), memory_us(d, keys)));
     out.piece = (int)std::min<int64_t>(most, (int64_t)turns * per_turn);
   }
   int64_t partial = 0, items = 0, longest = 0;
@@ -134,7 +160,7 @@ void cut_groups(AttnPlan& out, const cp_attn_desc& d, bool wide) {
       work.per_split.push_back((uint32_t)prefix_items(p, G, d.num_kv_heads));
       work.partial.push_back((uint32_t)((int64_t)p.n * d.num_q_heads));
     }
-    piece = piece_of(work, cost_of(d.head_dim, wide, memory_us(d, keys)));
+    piece = piece_of(work, cost_of(d.head_dim, wide, true, memory_us(d, keys)));
   }
   for (size_t i = 0; i < out.prefix.size(); ++i) {
     PrefixRow& p = out.prefix[i];
@@ -162,13 +188,21 @@ bool plan_pages(const cp_attn_desc& desc, const cp_row_meta* rows, int32_t n_row
     tok += rows[i].chunk_len;
   }
   for (const TokenRow& r : out.rows) keys += (double)r.n * listed(r) * B;
-  return cut_rows(out, desc, keys, kTurn / desc.block_size, kListPages, listed);
+  return cut_rows(out, desc, keys, kTurn / desc.block_size, kListPages, false, listed);
 }
 
 bool plan_prefix(const cp_attn_desc& desc, const cp_row_meta* rows, int32_t n_rows,
                  const cp_prefix_group* groups, int32_t n_groups, AttnPlan& out) {
   reset(out);
   const int hq = desc.num_q_heads, G = hq / desc.num_kv_heads, B = desc.block_size;
+  int64_t items = 0, most = 0;
+  for (int32_t i = 0; i < n_rows; ++i)
+    if (rows[i].chunk_len > 0) {
+      items += (int64_t)rows[i].chunk_len * desc.num_kv_heads;
+      most = std::max<int64_t>(most, rows[i].ctx_len);
+    }
+  const bool one = n_groups > 0 && ungrouped(items, ceil_div(most, kTurn));
+  if (one) n_groups = 0;
   int32_t tok = 0, g = 0, last = -1;
   for (int32_t i = 0; i < n_rows; ++i) {
     while (g < n_groups && i >= groups[g].first_row + groups[g].n_rows) ++g;
@@ -204,7 +238,7 @@ bool plan_prefix(const cp_attn_desc& desc, const cp_row_meta* rows, int32_t n_ro
   };
   double keys = 0;
   for (const TokenRow& r : out.rows) keys += (double)own(r);
-  return cut_rows(out, desc, keys, kTurn, INT32_MAX / kTurn * kTurn, own);
+  return cut_rows(out, desc, keys, kTurn, INT32_MAX / kTurn * kTurn, one, own);
 }
 
 }  // namespace cpcache

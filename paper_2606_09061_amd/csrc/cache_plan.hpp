@@ -18,6 +18,8 @@ constexpr int kPieceTokens = 512, kPiecePages = 2048;
 // Keys that the four waves of a narrow attention workgroup take in turn, and those
 // of a wide one's step.
 constexpr int kTurn = 128, kWideTurn = 64;
+// Waves of a workgroup where all take the same item (others have four).
+constexpr int kAllWaves = 8;
 // Most pages of a piece of a page list (its workgroup holds them in LDS).
 constexpr int kListPages = 256;
 // Most pieces of a group's keys (the factors of their merge are in LDS).
@@ -38,7 +40,7 @@ struct TokenRow {    // a piece of a row's tokens
 struct AttnPlan {
   std::vector<TokenRow> rows;       // in the order of their tokens
   std::vector<PrefixRow> prefix;    // of the groups that share something
-  int unit_waves = 4;               // waves of a (token, kv head, piece) item: 1, 2 or 4
+  int unit_waves = 4;               // waves of a (token, kv head, piece) item: 1, 2, 4 or 8
   int piece = 0;                    // keys, or entries of a list, of a piece of the rows' ranges
   bool parts = false;               // some row has several, and all have partial rows
   int32_t row_part0 = 0;            // the first of them; the groups' come before

@@ -27,8 +27,7 @@ using cpattn::shfl_xor_f;
 
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kWaves = kThreads / 64;
+constexpr int kThreads = 256, kWaves = kThreads / 64;
 
 __device__ __forceinline__ f32x4_t mfma16x16x32(uint4 a, uint4 b, f32x4_t c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a),
@@ -202,15 +201,16 @@ __device__ __forceinline__ void attend(State<D, NC>& st, const uint4 (&qv)[NC][D
 
 // The waves' states of up to kNarrowTile rows in LDS: row r of wave w counts with
 // factor f[w][r] = 2^(m_w - max m) / (sum of all weights so scaled).
+template <int NW>
 struct Shared {
-  float m[kWaves][kNarrowTile], l[kWaves][kNarrowTile], f[kWaves][kNarrowTile];
+  float m[NW][kNarrowTile], l[NW][kNarrowTile], f[NW][kNarrowTile];
 };
 
 // The maxima and sums of `waves` waves from wave w0 on, which share 16 NC rows, and
 // from them the rows' factors; x counts the threads of those waves.
 // log_sum(row, y) gets the log2 of the sum of each row's weights.
-template <int D, int NC, class LogSum>
-__device__ __forceinline__ void join_waves(const State<D, NC>& st, Shared& s, int wave, int w0,
+template <int D, int NC, int NW, class LogSum>
+__device__ __forceinline__ void join_waves(const State<D, NC>& st, Shared<NW>& s, int wave, int w0,
                                            int waves, int x, LogSum&& log_sum) {
   const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
 #pragma unroll
@@ -222,22 +222,22 @@ __device__ __forceinline__ void join_waves(const State<D, NC>& st, Shared& s, in
   }
   __syncthreads();
   if (x < 16 * NC) {
-    float M = -INFINITY, L = 0.f, m[kWaves], f[kWaves];
+    float M = -INFINITY, L = 0.f, m[NW], f[NW];
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
+    for (int w = 0; w < NW; ++w) {
       m[w] = w < waves ? s.m[w0 + w][x] : -INFINITY;
       f[w] = w < waves ? s.l[w0 + w][x] : 0.f;
       M = fmaxf(M, m[w]);
     }
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
+    for (int w = 0; w < NW; ++w) {
       const float l = f[w];
       f[w] = m[w] == -INFINITY ? 0.f : exp2f(m[w] - M);
       L += f[w] * l;
     }
     const float inv = L == 0.f ? 0.f : 1.f / L;  // L == 0: it saw no key
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w)
+    for (int w = 0; w < NW; ++w)
       if (w < waves) s.f[w0 + w][x] = f[w] * inv;
     log_sum(x, L == 0.f ? -INFINITY : M + __log2f(L));
   }
@@ -245,8 +245,8 @@ __device__ __forceinline__ void join_waves(const State<D, NC>& st, Shared& s, in
 
 // Writes the sums of those waves' outputs, 16 rows at a time: put(row, p, v) gets
 // features 4 p .. 4 p + 3 of each row below m_rows.  slice(w) is wave w's LDS.
-template <int D, int NC, class Slice, class Put>
-__device__ __forceinline__ void write_rows(const State<D, NC>& st, const Shared& s, int wave,
+template <int D, int NC, int NW, class Slice, class Put>
+__device__ __forceinline__ void write_rows(const State<D, NC>& st, const Shared<NW>& s, int wave,
                                            int w0, int waves, int x0, int m_rows, Slice&& slice,
                                            Put&& put) {
   constexpr int NDT = D / 16;
@@ -268,7 +268,7 @@ __device__ __forceinline__ void write_rows(const State<D, NC>& st, const Shared&
       if (16 * c + r >= m_rows) break;  // a thread's rows come in increasing order
       f32x4_t v = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int w = 0; w < kWaves; ++w)
+      for (int w = 0; w < NW; ++w)
         if (w < waves)
           v += s.f[w0 + w][16 * c + r] *
                *reinterpret_cast<const f32x4_t*>(
@@ -285,7 +285,7 @@ __device__ __forceinline__ void group_unit(const PrefixRow& row, int unit, const
                                            const uint16_t* __restrict__ q,
                                            const uint16_t* __restrict__ k_cache,
                                            const uint16_t* __restrict__ v_cache,
-                                           const int32_t* __restrict__ bt, Shared& s,
+                                           const int32_t* __restrict__ bt, Shared<kWaves>& s,
                                            Slice&& slice) {
   constexpr int NC = kNarrowTile / 16, NKS = D / 32;
   const int G = 1 << a.log2_group, all = row.n << a.log2_group;
@@ -349,23 +349,25 @@ __device__ __forceinline__ Own own_of(const Batch& b, const AttnArgs& a, int r) 
   return o;
 }
 
-// A workgroup of tokens: each of its units, taken by 2^a.log2_waves waves, is a token's
+// A workgroup of tokens: each of its units, taken by 2^a.log2_waves waves or by
+// all kAllWaves, is a token's
 // G rows over a piece of its own keys, or (LIST) of its page list, whose blocks of
 // the piece come to s_blocks, their number to s_count.
-template <int D, int B, bool LIST, class Batch, class Slice>
+template <int D, int B, bool LIST, int NW, class Batch, class Slice>
 __device__ __forceinline__ void token_units(const Batch& b, int block, const AttnArgs& a,
                                             const uint16_t* __restrict__ q,
                                             const uint16_t* __restrict__ k_cache,
                                             const uint16_t* __restrict__ v_cache,
                                             const int32_t* __restrict__ bt,
-                                            const int32_t* __restrict__ pages, Shared& s,
+                                            const int32_t* __restrict__ pages, Shared<NW>& s,
                                             int (*s_blocks)[kListPages], int* s_count,
                                             Slice&& slice) {
   constexpr int NKS = D / 32;
   const int tid = threadIdx.x, lane = tid & 63, i = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int W = 1 << a.log2_waves, mine = wave >> a.log2_waves, w0 = mine << a.log2_waves;
-  const int x = tid - 64 * w0, item = block * (kWaves >> a.log2_waves) + mine;
+  const int log2_waves = NW == kWaves ? a.log2_waves : __builtin_ctz(NW);
+  const int W = 1 << log2_waves, mine = wave >> log2_waves, w0 = mine << log2_waves;
+  const int x = tid - 64 * w0, item = block * (NW >> log2_waves) + mine;
   const bool real = item < a.items;  // the last workgroup may have fewer units
   const Own row = own_of<B, LIST>(b, a, row_index(b.r, &AttnRow::item0, min(item, a.items - 1)));
   const int unit = min(item, a.items - 1) - row.item0;

@@ -79,7 +79,7 @@ __global__ __launch_bounds__(2 * kWideTile, 2) void shared_wide_kernel(
   __shared__ __attribute__((aligned(1024))) uint8_t vb0[C::TILE_BYTES];
   __shared__ __attribute__((aligned(1024))) uint8_t vb1[C::TILE_BYTES];
 
-  __shared__ Shared s;
+  __shared__ Shared<kWaves> s;
   // a wave's slice, half a tile
   const auto slice = [&](int w) {
     static_assert(2 * kSlice<D> == C::TILE_BYTES, "slices");
@@ -87,7 +87,7 @@ __global__ __launch_bounds__(2 * kWideTile, 2) void shared_wide_kernel(
   };
   const int token_item = (int)blockIdx.x - a.group_items;
   if (token_item >= 0) {
-    token_units<D, B, false>(b, token_item, a, q, k_cache, v_cache, bt, nullptr, s, nullptr,
+    token_units<D, B, false, kWaves>(b, token_item, a, q, k_cache, v_cache, bt, nullptr, s, nullptr,
                              nullptr, slice);
     return;
   }

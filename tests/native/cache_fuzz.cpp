@@ -108,6 +108,8 @@ void check(const cp_attn_desc& d, const std::vector<cp_row_meta>& rows,
       tok += m.chunk_len;
     }
     CHECK(at == p.rows.size() && split == p.parts);
+    CHECK(p.unit_waves == 1 || p.unit_waves == 2 || p.unit_waves == 4 ||
+          (p.unit_waves == kAllWaves && p.prefix.empty() && !p.parts));
     if (split) parts.push_back({p.row_part0, own_parts});
     no_overlap(parts, p.partial_rows);
   }

@@ -253,11 +253,11 @@ def test_short_workspaces_are_refused():
     need = cache.page_select_workspace_bytes(_desc(), GOOD, 4)
     assert need == (19 * 8) * 8                          # the second row has 19 pages
     assert _select(ws_bytes=need - 1) == binding.CP_ERR_WORKSPACE
-    rows = _rows([0, 300, 1, 301], [1, 200, 1, 201])
-    need = cache.prefix_attn_workspace_bytes(_desc(), rows, [(0, 2, 192)])
-    assert need > 256 and _prefix(rows=rows, groups=[(0, 2, 192)],
-                                  ws_bytes=need - 1) == binding.CP_ERR_WORKSPACE
     d = _desc(max_blocks_per_req=4000)
+    rows = _rows([0, 1300, 1, 1301], [1, 1200, 1, 1201])
+    need = cache.prefix_attn_workspace_bytes(d, rows, [(0, 2, 1200)])
+    assert need > 256 and _prefix(d, rows=rows, groups=[(0, 2, 1200)],
+                                  ws_bytes=need - 1) == binding.CP_ERR_WORKSPACE
     rows = _rows([0, 40000, 1, 40001])
     need = cache.page_attn_workspace_bytes(d, rows, 600)
     assert need > 256 and _attn(d, rows, 600, need - 1) == binding.CP_ERR_WORKSPACE

@@ -474,6 +474,15 @@ def test_page_attn_reads_listed_pages_only():
     assert torch.isnan(out[0, 2:, 5]).all() and not torch.isnan(out[0, :2]).any()
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("reqs,heads", [(1, 2), (4, 1), (5, 2), (63, 2), (64, 2), (65, 2), (128, 2)])
+@pytest.mark.parametrize("n_pages", [64, 65, 200])
+def test_page_attn_in_one_launch_and_in_pieces(d, reqs, heads, n_pages):
+    c = Case(2 * heads, heads, d, 16, [(1029 + 16 * i, 1) for i in range(reqs)], reqs)
+    pages = c.lists(n_pages)
+    c.check(c.listed(pages), f"{reqs} x {heads}, {n_pages} pages", pages)
+
+
 @pytest.mark.parametrize("lens", [[1] * 8, [1] * 9, [1] * 92, [2, 0] * 50, [1] * 200])
 def test_page_attn_numbers_of_rows(lens):
     c = Case(4, 2, 64, 16, [(11 * i, n) for i, n in enumerate(lens)], len(lens))
@@ -490,11 +499,18 @@ def test_page_attn_of_a_long_chunk():
 
 # ---------------------------------------------------------------- common prefixes
 
+# Few tokens of few keys are attended one by one, whether they share keys or not;
+# beside a longer row the groups' common keys are read once.
+FAR = [(1100, 1)]
+beside = pytest.mark.parametrize("far", [[], FAR], ids=["", "far"])
+
+
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("block", [16, 32])
 @pytest.mark.parametrize("hq,hkv", HEADS)
-def test_prefix_attn_matches_the_oracle(hq, hkv, d, block):
-    rows = [(100, 1), (130, 2), (96, 1), (70, 3), (5, 0), (300, 1), (200, 1), (0, 1), (900, 4)]
+@beside
+def test_prefix_attn_matches_the_oracle(hq, hkv, d, block, far):
+    rows = [(100, 1), (130, 2), (96, 1), (70, 3), (5, 0), (300, 1), (200, 1), (0, 1), (900, 4)] + far
     c = Case(hq, hkv, d, block, rows, 100 * hq + hkv + d + block,
              groups=[(0, 3, 96), (4, 3, 165)])
     c.check(c.prefix(), f"{hq}/{hkv} d {d} block {block}")
@@ -502,16 +518,18 @@ def test_prefix_attn_matches_the_oracle(hq, hkv, d, block):
 
 @pytest.mark.parametrize("common", [0, 1, 15, 16, 17, 31, 32, 33, 64, 127, 128, 129, 1000, 5000])
 @pytest.mark.parametrize("n", [1, 2, 9])
-def test_prefix_attn_lengths(common, n):
-    rows = [(common + 3 * i, 1 + i % 2) for i in range(n)]
+@beside
+def test_prefix_attn_lengths(common, n, far):
+    rows = [(common + 3 * i, 1 + i % 2) for i in range(n)] + far
     c = Case(8, 2, 128, 16, rows, common + n, groups=[(0, n, common)])
     c.check(c.prefix(), f"{common} tokens in common, {n} rows")
 
 
 @pytest.mark.parametrize("n", [3, 4, 5, 7, 8, 9, 31, 33, 64, 65, 100])
 @pytest.mark.parametrize("hq,hkv,d,block", [(4, 1, 128, 16), (8, 1, 64, 32), (2, 2, 128, 32)])
-def test_prefix_attn_sizes_of_groups(n, hq, hkv, d, block):
-    rows = [(200 + 5 * (i % 7), 1) for i in range(n)] + [(50, 1)]
+@beside
+def test_prefix_attn_sizes_of_groups(n, hq, hkv, d, block, far):
+    rows = [(200 + 5 * (i % 7), 1) for i in range(n)] + [(50, 1)] + far
     c = Case(hq, hkv, d, block, rows, n, groups=[(0, n, 200)])
     c.check(c.prefix(), f"{n} rows of a group")
 
@@ -535,10 +553,12 @@ def test_prefix_attn_of_many_rows_and_groups():
 
 
 @pytest.mark.parametrize("n", [8, 9, 92, 93, 112, 113, 200])
-def test_prefix_attn_numbers_of_rows(n):
-    c = Case(2, 1, 64, 16, [(20 + i, 1) for i in range(n)], n, groups=[(n // 3, n // 2, 20)])
+@beside
+def test_prefix_attn_numbers_of_rows(n, far):
+    rows = [(20 + i, 1) for i in range(n)] + far
+    c = Case(2, 1, 64, 16, rows, n, groups=[(n // 3, n // 2, 20)])
     c.check(c.prefix(), f"{n} rows")
-    c = Case(2, 1, 64, 16, [(20 + i, 1) for i in range(n)], n, groups=[(i, 1, 20) for i in range(n)])
+    c = Case(2, 1, 64, 16, rows, n, groups=[(i, 1, 20) for i in range(n)])
     c.check(c.prefix(), f"{n} groups")
 
 
@@ -561,9 +581,10 @@ def test_prefix_attn_without_groups():
     c.check(c.prefix(), "no groups")
 
 
-def test_prefix_attn_what_a_token_does_not_see_does_not_touch_it():
+@beside
+def test_prefix_attn_what_a_token_does_not_see_does_not_touch_it(far):
     """NaN in a later token's key and value, and in another row's own pages."""
-    c = Case(8, 2, 128, 16, [(100, 5), (110, 1)], 8, groups=[(0, 2, 100)])
+    c = Case(8, 2, 128, 16, [(100, 5), (110, 1)] + far, 8, groups=[(0, 2, 100)])
     b = c.table[c.rows[0, 0], 103 // 16]
     c.k[b, 0, 103 % 16, 3], c.v[b, 1, 4, 103 % 16] = NAN, NAN
     c.check(c.prefix(), "poisoned token")
@@ -571,9 +592,10 @@ def test_prefix_attn_what_a_token_does_not_see_does_not_touch_it():
 
 
 @pytest.mark.parametrize("scale", [30.0, 1e-3, 1000.0])
-def test_attn_large_scores(scale):
+@beside
+def test_attn_large_scores(scale, far):
     """Scores far apart: the running maximum moves, most weights vanish."""
-    c = Case(8, 2, 64, 16, [(500, 2), (530, 1)], 9, groups=[(0, 2, 500)])
+    c = Case(8, 2, 64, 16, [(500, 2), (530, 1)] + far, 9, groups=[(0, 2, 500)])
     c.scale = scale / 8
     c.check(c.prefix(), f"scale {scale}")
     pages = c.lists(20)
@@ -597,11 +619,12 @@ def test_attn_repeats_bit_for_bit_and_reads_no_stale_workspace():
             assert torch.equal(out, first[i])
 
 
-def test_calls_in_graphs_streams_and_threads():
+@beside
+def test_calls_in_graphs_streams_and_threads(far):
     """Captured once and replayed on new contents, beside the same calls of other
     threads on streams of their own."""
     from concurrent.futures import ThreadPoolExecutor
-    c = Case(8, 2, 128, 16, [(300, 1), (310, 1), (40, 2)], 11, groups=[(0, 2, 300)])
+    c = Case(8, 2, 128, 16, [(300, 1), (310, 1), (40, 2)] + far, 11, groups=[(0, 2, 300)])
     s = Select(8, 2, 128, 16, [(2000, 1), (300, 2)], 12)
     g, sg, pages = c.gpu(), s.gpu(), torch.from_numpy(c.lists(7)).to(DEV)
     out = [c.new_out(), c.new_out(), torch.zeros(3, 2, 9, dtype=torch.int32, device=DEV)]
