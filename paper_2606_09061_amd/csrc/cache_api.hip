@@ -148,14 +148,14 @@ int by_rows(const std::vector<R>& rows, int32_t R::*item0, int64_t most, Items&&
 constexpr int kLeastChunk = 64, kMostChunk = 512;
 constexpr int64_t kScoreItems = 1024;
 // Whether one launch does both, a workgroup of 8 or 16 waves each (token, kv head):
-// where their number is about the CUs', or there are few pages to score and no more
-// than that.  us, one launch / two, on 32/8 heads: 63 pages, 8 to 256 (token, kv
-// head)s 6.9 to 8.6 / 10.4 to 11.8, 512 15.7 / 14.3; 251 pages, 8 10.4 / 9.1, 128 11.8
-// / 12.4, 256 13.1 / 16.4, 512 24.9 / 26.2, 1,024 57 / 50; 938 pages, 8 23 / 10, 256 28
-// / 36, 512 56 / 60.  64/8 heads agree.
-bool in_one(int64_t units, int most) {
-  if (most > kOnePages) return false;
-  return most <= 128 ? units <= 256 : units >= 128 && units <= 512;
+// where there are few pages to score, or about as many workgroups as CUs.  us, one launch
+// / two, 32/8 heads of 128, 8 (token, kv head)s: 63 pages 6.9 / 8.4, 125 8.8 / 8.6 (eager
+// 8.6 / 9.7), 188 9.2 / 8.8, 256 11.2 / 8.7; 128 of them: 63 8.3 / 9.6, 156 10.2 / 11.1, 256
+// 12.5 / 13.1; 256: 251 13.1 / 16.4, 938 28 / 36; 512: 125 20.0 / 16.2, 219 24.2 / 24.9, 938
+// 56 / 60; 1,024: 251 57 / 50.  Heads of 64, 8 of them: 219 8.0 / 8.5, 256 9.2 / 8.6.
+bool in_one(int d, int64_t units, int most) {
+  if (most > kOnePages || units > 512) return false;
+  return units > 256 ? most > 192 : units >= 128 || most <= (d == 64 ? 224 : 128);
 }
 
 // The scores that cp_page_select keeps: rows whose tokens may have to choose.
@@ -442,7 +442,7 @@ int cp_page_select(const cp_attn_desc* desc, const void* q, const void* bounds,
                        n_last,
                        chunk};
     const auto choices = [&](const SelectRow& r) { return (int64_t)r.n * hkv; };
-    if (in_one(tokens * hkv, most))
+    if (in_one(desc->head_dim, tokens * hkv, most))
       return by_rows<SelectRow, kSelectRows>(
           plan, &SelectRow::item0, kMaxItems, choices,
           [&](SelectRows& batch, int n, int items, size_t) {

@@ -221,8 +221,8 @@ __device__ __forceinline__ Choice choice_of(const Rows& rows, const SelectArgs& 
 // head)s; 5.2 for 32 of 256 pages, 8 of them.
 template <int NT, int NU, class Src>
 __device__ __forceinline__ void choose_pages(const SelectArgs& a, int n, Src&& src, int32_t* dst) {
-  constexpr int NW = NT / 64, kFew = 128, NC = NU * NW, CPL = NC > 64 ? NC / 64 : 1;
-  static_assert(NW <= 16 && NT % kFew == 0 && (NC <= 64 || NC == 64 * CPL), "geometry");
+  constexpr int NW = NT / 64, SH = 8, kFew = NT / SH, NC = NU * NW, CPL = NC > 64 ? NC / 64 : 1;
+  static_assert(NW <= 16 && NT % SH == 0 && (NC <= 64 || NC == 64 * CPL), "geometry");
   __shared__ __align__(16) int s_hist[2][256];
   __shared__ int s_count[2][CPL * 64];
   __shared__ uint64_t s_max[16], s_not_min[16], s_key[kFew];
@@ -333,21 +333,19 @@ __device__ __forceinline__ void choose_pages(const SelectArgs& a, int n, Src&& s
         s_key[at] = key[u], s_page[at] = u * NT + tid;
       }
     __syncthreads();
-    // SH threads count the keys before one (whatever their order here)
-    constexpr int SH = NT / kFew >= 8 ? 8 : 2;
-    if (tid < kFew * SH) {
-      const int e0 = tid % SH, x = min(tid / SH, in - 1);
-      const uint64_t k = s_key[x];
-      const int page = s_page[x];
-      int before = 0;
+    // SH threads count the keys before one (whatever their order here); two of them,
+    // and up to 128 keys, took 5 us of a workgroup of four waves
+    const int e0 = tid % SH, x = min(tid / SH, in - 1);
+    const uint64_t k = s_key[x];
+    const int page = s_page[x];
+    int before = 0;
 #pragma unroll 4
-      for (int e = e0; e < in; e += SH)
-        before += s_key[e] > k || (s_key[e] == k && s_page[e] < page);
+    for (int e = e0; e < in; e += SH)
+      before += s_key[e] > k || (s_key[e] == k && s_page[e] < page);
 #pragma unroll
-      for (int m = 1; m < SH; m <<= 1) before += __shfl_xor(before, m, 64);
-      if (e0 == 0 && tid / SH < in && before < left)
-        atomicOr(&s_take[page >> 6], 1ull << (page & 63));
-    }
+    for (int m = 1; m < SH; m <<= 1) before += __shfl_xor(before, m, 64);
+    if (e0 == 0 && tid / SH < in && before < left)
+      atomicOr(&s_take[page >> 6], 1ull << (page & 63));
     __syncthreads();
 #pragma unroll
     for (int u = 0; u < NU; ++u) chosen |= (uint32_t)(s_take[u * NW + wave] >> lane & 1) << u;

@@ -370,12 +370,13 @@ def test_select_of_long_contexts_with_equal_scores(ctx, n_pages):
 
 
 @pytest.mark.parametrize("reqs,pages", [(1, 127), (1, 128), (1, 129), (64, 100), (65, 100), (128, 60),
-                                        (32, 300), (31, 130), (129, 140), (40, 1023), (40, 1025)])
-@pytest.mark.parametrize("hq,hkv", [(8, 4), (32, 4)])
-def test_select_in_one_launch_and_in_two(reqs, pages, hq, hkv):
+                                        (32, 300), (31, 130), (129, 140), (40, 1023), (40, 1025),
+                                        (1, 224), (1, 225), (128, 192), (128, 193), (5, 33)])
+@pytest.mark.parametrize("hq,hkv,d", [(8, 4, 64), (32, 4, 64), (16, 4, 128)])
+def test_select_in_one_launch_and_in_two(reqs, pages, hq, hkv, d):
     """Around the numbers of rows and pages at which the launches change."""
     rows = [(16 * pages - 1 - 16 * (r % 3) * (pages > 3), 1) for r in range(reqs)]
-    Select(hq, hkv, 64, 16, rows, reqs + pages, pool=700).check(21, 2, 3)
+    Select(hq, hkv, d, 16, rows, reqs + pages, pool=700).check(21, 2, 3)
 
 
 def test_select_scores_a_hair_apart():
