@@ -151,11 +151,12 @@ constexpr int64_t kScoreItems = 1024;
 // where there are few pages to score, or about as many workgroups as CUs.  us, one launch
 // / two, 32/8 heads of 128, 8 (token, kv head)s: 63 pages 6.9 / 8.4, 125 8.8 / 8.6 (eager
 // 8.6 / 9.7), 188 9.2 / 8.8, 256 11.2 / 8.7; 128 of them: 63 8.3 / 9.6, 156 10.2 / 11.1, 256
-// 12.5 / 13.1; 256: 251 13.1 / 16.4, 938 28 / 36; 512: 125 20.0 / 16.2, 219 24.2 / 24.9, 938
-// 56 / 60; 1,024: 251 57 / 50.  Heads of 64, 8 of them: 219 8.0 / 8.5, 256 9.2 / 8.6.
+// 12.5 / 13.1; 256: 251 13.1 / 16.4, 938 28 / 36; 384: 475 34.6 / 31.1; 512: 125 20.0 / 16.2,
+// 219 24.2 / 24.9, 938 56 / 60; 1,024: 251 57 / 50.  Heads of 64, 8 of them: 219 8.0 / 8.5, 256
+// 9.2 / 8.6.
 bool in_one(int d, int64_t units, int most) {
   if (most > kOnePages || units > 512) return false;
-  return units > 256 ? most > 192 : units >= 128 || most <= (d == 64 ? 224 : 128);
+  return units > 256 ? units > 448 && most > 192 : units >= 128 || most <= (d == 64 ? 224 : 128);
 }
 
 // The scores that cp_page_select keeps: rows whose tokens may have to choose.

@@ -54,7 +54,7 @@ __global__ __launch_bounds__(kThreads, 2) void shared_kernel(
 //     sum_s 2^(L_s - max L) O_s / sum_s 2^(L_s - max L),
 // over its own pieces and its group's.  A row (token, q head) takes `share` times
 // D / 4 threads of 4 features, each of which takes every share-th piece; they meet
-// in LDS.  A workgroup's rows are one token's.  3.1 us for a token of 8 pieces on 32
+// in LDS.  A workgroup's rows are one token's.  3.1 us for a token of 4 pieces on 32
 // heads; 6.4 for 128 tokens on 64 heads, 18 MB of partial rows: latency.
 template <int D, int B, bool LIST, class Batch>
 __global__ __launch_bounds__(kThreads) void cache_merge_kernel(const Batch b, const AttnArgs a,

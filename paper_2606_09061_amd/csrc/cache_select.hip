@@ -217,8 +217,8 @@ __device__ __forceinline__ Choice choice_of(const Rows& rows, const SelectArgs& 
 // which the keys differ, by a histogram of the keys that agree with the bits known
 // so far.  Once few keys are left, or all of them are selected, each counts those
 // before it.  The selected pages are written in order, by the ballots of the waves.
-// Bound by its barriers, some three a digit: 8.5 us for 128 of ~2,100 pages, 256 (token, kv
-// head)s; 5.2 for 32 of 256 pages, 8 of them.
+// Bound by its barriers, some three a digit: 8.7 us for 128 of ~2,100 pages, 256 (token, kv
+// head)s; 5.1 for 32 of 256 pages, 8 of them.
 template <int NT, int NU, class Src>
 __device__ __forceinline__ void choose_pages(const SelectArgs& a, int n, Src&& src, int32_t* dst) {
   constexpr int NW = NT / 64, SH = 8, kFew = NT / SH, NC = NU * NW, CPL = NC > 64 ? NC / 64 : 1;

@@ -59,8 +59,9 @@ struct State {
 // end of a tile to the product with it in the next.
 //
 // Bound by HBM where there is work for all CUs: 48 tokens on 64/8 heads of 128, 256
-// pages of 16 each, 121 us for 807 MB, 6.6 TB/s.  One token's 64 pages, on 32/8 heads:
-// 6.8 us, a launch's latency and that of table, K, V and the joining of the waves.
+// pages of 16 each, 122 us for 807 MB, 6.6 TB/s.  One token's 64 pages, on 32/8 heads:
+// 9.8 us by eight waves a kv head, a launch's latency and those of table, K, V, four
+// tiles and the joining of the waves.
 template <int D, int B, int NC, class BlockOf>
 __device__ __forceinline__ void attend(State<D, NC>& st, const uint4 (&qv)[NC][D / 32], int n_keys,
                                        int first, int stride, int kvh, int hkv, float scale_log2,
