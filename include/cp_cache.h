@@ -131,12 +131,13 @@ size_t cp_prefix_attn_workspace_bytes(const cp_attn_desc *desc, const cp_row_met
 /* Causal attention as in cp_attn_mixed, for decode rows and short chunks of
  * requests with a common prefix.  The first common / B entries of the table
  * rows of a group's requests are the same (as cp_kv_fork leaves them): those
- * pages are read once for the whole group, through its first row's table, and
- * every row's other keys one by one.  Groups come in rising order and do not
+ * pages are read once for the whole group, through its first row's table (where
+ * few tokens have few keys, by each of them), and every row's other keys one by
+ * one.  Groups come in rising order and do not
  * overlap; 0 <= common <= chunk_start of each of the group's rows that has
- * tokens; else CP_ERR_BAD_META.  A row in no group shares nothing.  Each token
- * of a row is attended on its own behind the prefix, so long chunks belong to
- * cp_attn_mixed.  Precision, ws and out as in cp_page_attn.  With CP_DEBUG=1
+ * tokens; else CP_ERR_BAD_META.  A row in no group shares nothing.  Behind the
+ * prefix a row's tokens are taken some at a time, 16 (token, q head) pairs of a
+ * kv head at most, so long chunks belong to cp_attn_mixed.  Precision, ws and out as in cp_page_attn.  With CP_DEBUG=1
  * table rows of a group that differ where they should not are
  * CP_ERR_BAD_META. */
 int cp_prefix_attn(const cp_attn_desc *desc, const void *q, const void *k_cache,

@@ -49,8 +49,8 @@ using SelectRows = RowsOf<SelectRow, kSelectRows>;
 // other: the next one's first token ends a row, and the place behind the last row
 // holds the launch's end.  With `own` keys (or entries of a list) of its last
 // token, a row has ceil(own / piece) pieces, and the partial rows of its item x,
-// (piece, token, kv head), are (item0 + x) G and on, behind those of the launches
-// before.
+// (piece, up to T tokens, kv head), are (item0 + x) T G and on, behind those of the
+// launches before.
 struct AttnRow {     // 16 bytes
   int32_t item0;     // the launch's items of rows before it
   int32_t tok0, start, req;

@@ -219,6 +219,7 @@ AttnArgs attn_args(const cp_attn_desc* d, const AttnPlan& p, const void* q, cons
                   0,
                   0,
                   __builtin_ctz(p.unit_waves),
+                  p.log2_tokens,
                   0,
                   0,
                   d->sm_scale * cpattn::kLog2e};
@@ -238,7 +239,7 @@ int launch_plan(const cp_attn_desc* d, const AttnPlan& p, AttnArgs a, hipStream_
     const size_t first = r;
     for (; r < p.rows.size() && n < kAttnRows; ++r) {
       const TokenRow& t = p.rows[r];
-      const int64_t more = (int64_t)t.n_split * t.n * hkv;
+      const int64_t more = (int64_t)t.n_split * p.items_of(t.n) * hkv;
       const bool other = t.group >= 0 && t.group != last, fresh = other && t.group == begun;
       const int64_t shared = fresh ? prefix_items(p.prefix[t.group], G, hkv) : 0;
       if (n > 0 && items + group_items + more + shared > kMaxItems) break;
@@ -274,7 +275,7 @@ int launch_plan(const cp_attn_desc* d, const AttnPlan& p, AttnArgs a, hipStream_
     if (rc == CP_OK && merge)
       rc = finish(launch_cache_merge(D, B, a, b, n, end - p.rows[first].tok0, most, s), s);
     if (rc != CP_OK) return rc;
-    if (p.parts) part0 += items * G;
+    if (p.parts) part0 += (items * G) << p.log2_tokens;
   }
   return CP_OK;
 }

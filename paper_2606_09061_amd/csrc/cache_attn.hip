@@ -72,10 +72,12 @@ __global__ __launch_bounds__(kThreads) void cache_merge_kernel(const Batch b, co
   float M = -INFINITY, W = 0.f;
   f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
   if (h < a.hq) {
-    // workgroup (split, j, kvh) of the row's launch wrote its G rows; pieces
+    // unit (split, tokens, kvh) of the row's launch wrote their rows; pieces
     // [0, own) are the row's, those behind them the group's
-    const int64_t first = a.part0 + ((int64_t)row.item0 + (int64_t)j * a.hkv + kvh) * G + e;
-    const int64_t stride = (int64_t)row.n * a.hq;
+    const int log2_rows = a.log2_tokens + a.log2_group, jb = j >> a.log2_tokens;
+    const int64_t first = a.part0 + ((row.item0 + (int64_t)jb * a.hkv + kvh) << log2_rows) +
+                          ((j - (jb << a.log2_tokens)) << a.log2_group) + e;
+    const int64_t stride = (int64_t)(((row.n - 1) >> a.log2_tokens) + 1) * a.hkv << log2_rows;
     int own = row.n_split, n = own;
     int64_t gfirst = 0, gstride = 0;
     if (row.group >= 0) {

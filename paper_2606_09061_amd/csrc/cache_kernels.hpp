@@ -49,7 +49,8 @@ struct AttnArgs {
   float* part_lse;       // [partial rows], log2 of the weights' sum
   int hq, hkv, mbr, log2_group, n_pages, piece;
   int part0;             // the partial rows of the launch's first item of rows
-  int items, log2_waves; // the launch's (token, kv head, piece) items, and waves of each
+  int items, log2_waves; // the launch's (tokens, kv head, piece) items, and waves of each
+  int log2_tokens;       // most tokens of an item
   int n_groups;          // of the launch
   int group_items;       // its first workgroups, which are the groups'
   float scale_log2;      // sm_scale * log2(e)

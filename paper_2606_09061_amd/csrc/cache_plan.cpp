@@ -93,7 +93,7 @@ void add_row(AttnPlan& out, int32_t tok0, const cp_row_meta& m, int32_t group) {
 
 void reset(AttnPlan& out) {
   out.rows.clear(), out.prefix.clear();
-  out.piece = 1, out.parts = false, out.row_part0 = 0;
+  out.log2_tokens = 0, out.piece = 1, out.parts = false, out.row_part0 = 0;
   out.partial_rows = 0, out.off_lse = 0, out.ws_bytes = 256;
 }
 
@@ -106,7 +106,7 @@ bool cut_rows(AttnPlan& out, const cp_attn_desc& d, double keys, int per_turn, i
   work.turns.clear(), work.per_split.clear(), work.partial.clear();
   int64_t uncut = 0, all = 0;
   for (const TokenRow& r : out.rows)
-    uncut += (int64_t)r.n * d.num_kv_heads, all = std::max<int64_t>(all, own(r));
+    uncut += (int64_t)out.items_of(r.n) * d.num_kv_heads, all = std::max<int64_t>(all, own(r));
   out.piece = most;
   if (one || (out.prefix.empty() && whole(d.head_dim, uncut, ceil_div(all, per_turn)))) {
     out.unit_waves = kAllWaves;
@@ -115,7 +115,7 @@ bool cut_rows(AttnPlan& out, const cp_attn_desc& d, double keys, int per_turn, i
   if (uncut < kUncut && !out.rows.empty()) {
     for (const TokenRow& r : out.rows) {
       work.turns.push_back((uint32_t)ceil_div(own(r), per_turn));
-      work.per_split.push_back(r.n * d.num_kv_heads);
+      work.per_split.push_back(out.items_of(r.n) * d.num_kv_heads);
       work.partial.push_back(r.n * d.num_q_heads);
     }
     const int turns = piece_of(work, cost_of(d.head_dim, false, !out.prefix.empty(), memory_us(d, keys)));
@@ -125,8 +125,9 @@ bool cut_rows(AttnPlan& out, const cp_attn_desc& d, double keys, int per_turn, i
   for (TokenRow& r : out.rows) {
     r.n_split = (int)ceil_div(own(r), out.piece);
     out.parts |= r.n_split > 1 || r.group >= 0;
-    partial += (int64_t)r.n_split * r.n * d.num_q_heads;
-    items += (int64_t)r.n_split * r.n * d.num_kv_heads;
+    const int64_t mine = (int64_t)r.n_split * out.items_of(r.n) * d.num_kv_heads;
+    partial += (mine * (d.num_q_heads / d.num_kv_heads)) << out.log2_tokens;
+    items += mine;
     longest = std::max<int64_t>(longest, ceil_div(std::min<int64_t>(own(r), out.piece), per_turn));
   }
   out.unit_waves = unit_waves(items, longest);
@@ -233,6 +234,8 @@ bool plan_prefix(const cp_attn_desc& desc, const cp_row_meta* rows, int32_t n_ro
     p.part0 = (int32_t)std::min<int64_t>(out.partial_rows, INT32_MAX);
     out.partial_rows += (int64_t)p.n_split * p.n * hq;
   }
+  for (const TokenRow& r : out.rows)  // 16 columns at most
+    while (r.n > (1 << out.log2_tokens) && ((2 * G) << out.log2_tokens) <= 16) ++out.log2_tokens;
   const auto own = [&](const TokenRow& r) {
     return (int64_t)r.start + r.n - (r.group < 0 ? 0 : out.prefix[r.group].keys);
   };

@@ -40,12 +40,16 @@ struct TokenRow {    // a piece of a row's tokens
 struct AttnPlan {
   std::vector<TokenRow> rows;       // in the order of their tokens
   std::vector<PrefixRow> prefix;    // of the groups that share something
-  int unit_waves = 4;               // waves of a (token, kv head, piece) item: 1, 2, 4 or 8
+  int unit_waves = 4;               // waves of a (tokens, kv head, piece) item: 1, 2, 4 or 8
+  int log2_tokens = 0;              // most tokens of an item: neighbours share their keys
   int piece = 0;                    // keys, or entries of a list, of a piece of the rows' ranges
   bool parts = false;               // some row has several, and all have partial rows
   int32_t row_part0 = 0;            // the first of them; the groups' come before
   int64_t partial_rows = 0;
   size_t off_lse = 0, ws_bytes = 256;  // partial rows of D fp32, then their log sums
+
+  // items of n tokens, per kv head and piece
+  int items_of(int n) const { return ((n - 1) >> log2_tokens) + 1; }
 };
 
 // rows: valid for desc, within the limits of cp_cache.h.  Both return whether the

@@ -53,7 +53,10 @@ struct State {
 
 // Attends the wave's rows qv to keys [0, n_keys) of consecutive blocks, of which it
 // takes tiles of 32 keys first, first + stride, ...; block_of(i) is the i-th block's
-// place in the pool, for i below the blocks that n_keys fill.  K and V are
+// place in the pool, for i below the blocks that n_keys fill.  The lane's column sees
+// `mine` of the keys, and all columns see `least` (of an NC of 1; else all see all).
+// Values that some do not see are taken out of the product where they are infinities
+// or NaN, and added by those that do.  K and V are
 // loaded as they lie in memory, K's rows passing through `slice`, LDS that only
 // this wave uses.  K of the next tile is on its way from there on, V from the
 // end of a tile to the product with it in the next.
@@ -64,7 +67,7 @@ struct State {
 // tiles and the joining of the waves.
 template <int D, int B, int NC, class BlockOf>
 __device__ __forceinline__ void attend(State<D, NC>& st, const uint4 (&qv)[NC][D / 32], int n_keys,
-                                       int first, int stride, int kvh, int hkv, float scale_log2,
+                                       int mine, int least, int first, int stride, int kvh, int hkv, float scale_log2,
                                        const uint16_t* __restrict__ k_cache,
                                        const uint16_t* __restrict__ v_cache, uint8_t* slice,
                                        BlockOf&& block_of) {
@@ -139,20 +142,39 @@ __device__ __forceinline__ void attend(State<D, NC>& st, const uint4 (&qv)[NC][D
         for (int c = 0; c < NC; ++c) s[c][b] = mfma16x16x32(k, qv[c][ks], s[c][b]);
       }
     __builtin_amdgcn_wave_barrier();
-    const int left = n_keys - t * TK;  // keys of the tile (wave-uniform)
-    if (left < TK) {  // those past the range may be anything, V included
-      const int mine = left - 8 * g;
-#pragma unroll
-      for (int c = 0; c < NC; ++c)
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if (e >= mine) s[c][e >> 2][e & 3] = -INFINITY;
+    // the lane's values of keys from `end` on are zeroed
+    const auto cut_v = [&](int end) {
 #pragma unroll
       for (int dt = 0; dt < NDT; ++dt) {
         uint32_t* w = reinterpret_cast<uint32_t*>(&vr[dt]);
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-          w[e] &= (2 * e < mine ? 0x0000ffffu : 0u) | (2 * e + 1 < mine ? 0xffff0000u : 0u);
+          w[e] &= (2 * e < end ? 0x0000ffffu : 0u) | (2 * e + 1 < end ? 0xffff0000u : 0u);
+      }
+    };
+    const int left = n_keys - t * TK, all = least - t * TK;  // of the tile (wave-uniform)
+    bool apart = false;  // values of keys from `all` on are added below
+    if (all < TK) {  // those past the range may be anything, V included
+      const int end = mine - t * TK - 8 * g;
+#pragma unroll
+      for (int c = 0; c < NC; ++c)
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (e >= end) s[c][e >> 2][e & 3] = -INFINITY;
+      cut_v(left - 8 * g);
+      if constexpr (NC == 1) {
+        if (all < left) {
+          bool odd = false;
+#pragma unroll
+          for (int dt = 0; dt < NDT; ++dt) {
+            const uint32_t w[4] = {vr[dt].x, vr[dt].y, vr[dt].z, vr[dt].w};
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+              odd |= 8 * g + e >= all && (w[e / 2] >> (16 * (e & 1)) & 0x7f80u) == 0x7f80u;
+          }
+          apart = __builtin_amdgcn_ballot_w64(odd) != 0;
+          if (apart) cut_v(all - 8 * g);
+        }
       }
     }
     uint4 pv[NC];
@@ -189,6 +211,23 @@ __device__ __forceinline__ void attend(State<D, NC>& st, const uint4 (&qv)[NC][D
     for (int dt = 0; dt < NDT; ++dt)
 #pragma unroll
       for (int c = 0; c < NC; ++c) st.o[c][dt] = mfma16x16x32(vr[dt], pv[c], st.o[c][dt]);
+    if constexpr (NC == 1) {
+      if (apart)
+        for (int k = max(all, 0); k < min(left, TK); ++k) {
+          const uint32_t w[4] = {pv[0].x, pv[0].y, pv[0].z, pv[0].w};
+          const uint32_t pair = k & 4 ? (k & 2 ? w[3] : w[2]) : (k & 2 ? w[1] : w[0]);
+          const uint32_t theirs = __shfl(pair, 16 * (k >> 3) + i, 64);
+          const float p = __uint_as_float(k & 1 ? theirs & 0xffff0000u : theirs << 16);
+          const uint16_t* vp = v_cache + block_at(t, k / B) + k % B;
+          if (t * TK + k < mine)
+#pragma unroll
+            for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+              for (int r = 0; r < 4; ++r)
+                st.o[0][dt][r] +=
+                    p * __uint_as_float((uint32_t)vp[(16 * dt + 4 * g + r) * B] << 16);
+        }
+    }
     load_v(next);
   };
 
@@ -307,7 +346,7 @@ __device__ __forceinline__ void group_unit(const PrefixRow& row, int unit, const
   }
   const int32_t* blocks = bt + (int64_t)row.req * a.mbr + begin / B;
   State<D, NC> st;
-  attend<D, B, NC>(st, qv, n_keys, wave, kWaves, kvh, a.hkv, a.scale_log2, k_cache, v_cache,
+  attend<D, B, NC>(st, qv, n_keys, n_keys, n_keys, wave, kWaves, kvh, a.hkv, a.scale_log2, k_cache, v_cache,
                    slice(wave), [&](int b) { return blocks[b]; });
   const int64_t part = (int64_t)row.part0 + ((int64_t)kvh * row.n_split + split) * all + m0;
   join_waves(st, s, wave, 0, kWaves, threadIdx.x, [&](int r, float x) {
@@ -350,10 +389,12 @@ __device__ __forceinline__ Own own_of(const Batch& b, const AttnArgs& a, int r) 
   return o;
 }
 
-// A workgroup of tokens: each of its units, taken by 2^a.log2_waves waves or by
-// all kAllWaves, is a token's
-// G rows over a piece of its own keys, or (LIST) of its page list, whose blocks of
-// the piece come to s_blocks, their number to s_count.
+// A workgroup of tokens: each of its units, taken by 2^a.log2_waves waves or by all
+// kAllWaves, are the G rows of up to 2^a.log2_tokens tokens of a row (the columns, 16 at
+// most) over a piece of their own keys, or (LIST) of one token over a piece of its page
+// list, whose blocks come to s_blocks, their number to s_count.  Tokens taken together
+// read K and V once: 128 rows of up to 4 tokens behind ~500 keys of their own, 64/8 heads
+// of 128, 148 -> 112 us; 266 rows of a dozen keys, 16/16 heads of 64, 48 -> 35.
 template <int D, int B, bool LIST, int NW, class Batch, class Slice>
 __device__ __forceinline__ void token_units(const Batch& b, int block, const AttnArgs& a,
                                             const uint16_t* __restrict__ q,
@@ -372,14 +413,19 @@ __device__ __forceinline__ void token_units(const Batch& b, int block, const Att
   const bool real = item < a.items;  // the last workgroup may have fewer units
   const Own row = own_of<B, LIST>(b, a, row_index(b.r, &AttnRow::item0, min(item, a.items - 1)));
   const int unit = min(item, a.items - 1) - row.item0;
-  const int kvh = unit % a.hkv, j = unit / a.hkv % row.n, split = unit / a.hkv / row.n;
-  const int G = 1 << a.log2_group;
+  const int G = 1 << a.log2_group, log2_tokens = LIST ? 0 : a.log2_tokens;
+  const int blocks_of = LIST ? row.n : ((row.n - 1) >> log2_tokens) + 1;
+  const int kvh = unit % a.hkv, split = unit / a.hkv / blocks_of;
+  const int j = (unit / a.hkv % blocks_of) << log2_tokens;  // the first token
+  const int rows = min(1 << log2_tokens, row.n - j) << a.log2_group;
   const int64_t t = (int64_t)row.tok0 + j;
   const int pos = row.start + j;
   const int32_t* bt_row = bt + (int64_t)row.req * a.mbr;
   uint4 qv[1][NKS];
-  {  // past the last row that again (not stored)
-    const uint16_t* qb = q + (t * a.hq + kvh * G + min(i, G - 1)) * D + g * 8;
+  const int col = min(i, rows - 1);  // past the last row that again (not stored)
+  {
+    const uint16_t* qb =
+        q + ((t + (col >> a.log2_group)) * a.hq + kvh * G + (col & (G - 1))) * D + g * 8;
 #pragma unroll
     for (int ks = 0; ks < NKS; ++ks) qv[0][ks] = ld_global16(qb + ks * 32);
   }
@@ -403,24 +449,33 @@ __device__ __forceinline__ void token_units(const Batch& b, int block, const Att
       if (list[end - 1] == top) n_keys -= B - 1 - pos % B;
     }
     const int* blocks = s_blocks[mine];
-    attend<D, B, 1>(st, qv, real ? n_keys : 0, wave - w0, W, kvh, a.hkv, a.scale_log2, k_cache,
-                    v_cache, slice(wave),
+    if (!real) n_keys = 0;
+    attend<D, B, 1>(st, qv, n_keys, n_keys, n_keys, wave - w0, W, kvh, a.hkv, a.scale_log2,
+                    k_cache, v_cache, slice(wave),
                     [&](int b) { return __builtin_amdgcn_readfirstlane(blocks[b]); });
   } else {
     const int64_t begin = row.keys + (int64_t)split * a.piece;
-    n_keys = (int)min((int64_t)a.piece, pos + 1 - begin);  // maybe none
+    const auto seen = [&](int ahead) {  // by the token so far behind the first one; maybe none
+      return (int)min((int64_t)a.piece, pos + ahead + 1 - begin);
+    };
+    n_keys = real ? seen((rows - 1) >> a.log2_group) : 0;
     const int32_t* blocks = bt_row + begin / B;
-    attend<D, B, 1>(st, qv, real ? n_keys : 0, wave - w0, W, kvh, a.hkv, a.scale_log2, k_cache,
-                    v_cache, slice(wave), [&](int b) { return blocks[b]; });
+    attend<D, B, 1>(st, qv, n_keys, seen(col >> a.log2_group), seen(0), wave - w0, W, kvh, a.hkv,
+                    a.scale_log2, k_cache, v_cache, slice(wave),
+                    [&](int b) { return blocks[b]; });
   }
-  const int64_t part = (int64_t)a.part0 + ((int64_t)row.item0 + unit) * G;
+  const int64_t part =
+      (int64_t)a.part0 + (((int64_t)row.item0 + unit) << (log2_tokens + a.log2_group));
   join_waves(st, s, wave, w0, W, x, [&](int r, float y) {
-    if (real && !row.alone && r < G) a.part_lse[part + r] = y;
+    if (real && !row.alone && r < rows) a.part_lse[part + r] = y;
   });
-  write_rows(st, s, wave, w0, W, x, G, slice, [&](int r, int p, const f32x4_t& v) {
-    if (!real) return;
+  // (all units of the workgroup write as many rows as a unit can have: the same barriers)
+  write_rows(st, s, wave, w0, W, x, G << log2_tokens, slice, [&](int r, int p, const f32x4_t& v) {
+    if (!real || r >= rows) return;
     if (row.alone)
-      *reinterpret_cast<uint2*>(a.out + (t * a.hq + kvh * G + r) * D + 4 * p) =
+      *reinterpret_cast<uint2*>(a.out +
+                                ((t + (r >> a.log2_group)) * a.hq + kvh * G + (r & (G - 1))) * D +
+                                4 * p) =
           make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
     else
       *reinterpret_cast<f32x4_t*>(a.part_o + (part + r) * D + 4 * p) = v;

@@ -99,9 +99,10 @@ void check(const cp_attn_desc& d, const std::vector<cp_row_meta>& rows,
           CHECK(r.group == -1);
         }
         CHECK(own >= 1 && r.n_split == (own - 1) / p.piece + 1);  // as the kernels have it
-        CHECK((int64_t)r.n_split * r.n * hkv <= kMaxItems);
+        const int64_t items = (int64_t)r.n_split * p.items_of(r.n) * hkv;
+        CHECK(items <= kMaxItems && (int64_t)p.items_of(r.n) << p.log2_tokens >= r.n);
         CHECK(r.n_split == 1 || !which || p.piece % B == 0);
-        own_parts += (int64_t)r.n_split * r.n * hq;
+        own_parts += items * (hq / hkv) << p.log2_tokens;
         split |= r.n_split > 1 || r.group >= 0;
         j += r.n;
       }
@@ -110,6 +111,7 @@ void check(const cp_attn_desc& d, const std::vector<cp_row_meta>& rows,
     CHECK(at == p.rows.size() && split == p.parts);
     CHECK(p.unit_waves == 1 || p.unit_waves == 2 || p.unit_waves == 4 ||
           (p.unit_waves == kAllWaves && p.prefix.empty() && !p.parts));
+    CHECK(p.log2_tokens == 0 || (which && hq / hkv << p.log2_tokens <= 16));
     if (split) parts.push_back({p.row_part0, own_parts});
     no_overlap(parts, p.partial_rows);
   }

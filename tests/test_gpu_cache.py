@@ -593,6 +593,39 @@ def test_prefix_attn_what_a_token_does_not_see_does_not_touch_it(far):
     assert not torch.isnan(c.prefix()[:3]).any()
 
 
+CHUNKS = [1, 2, 3, 4, 5, 15, 16, 17, 33, 600]
+
+
+@pytest.mark.parametrize("hq,hkv,d,block", [(1, 1, 64, 16), (4, 2, 128, 32), (8, 1, 128, 16),
+                                            (4, 1, 64, 32)])
+@pytest.mark.parametrize("start", [0, 27, 31, 1100, 2047])
+def test_prefix_attn_of_chunks(hq, hkv, d, block, start):
+    """Neighbouring tokens share the products over their own keys."""
+    rows = [(start + i % 3, n) for i, n in enumerate(CHUNKS)]
+    c = Case(hq, hkv, d, block, rows, start + hq, groups=[(0, 4, start), (5, 4, start)])
+    c.check(c.prefix(), f"chunks behind {start} keys")
+    c = Case(hq, hkv, d, block, rows[:6], start + hq, groups=[(1, 4, start)])
+    c.check(c.prefix(), f"fewer of them behind {start} keys")
+
+
+@pytest.mark.parametrize("hq,hkv,d,block", [(1, 1, 64, 16), (4, 2, 128, 32), (8, 1, 128, 16)])
+@pytest.mark.parametrize("start", [30, 1100])
+def test_prefix_attn_of_chunks_with_infinities_and_nan(hq, hkv, d, block, start):
+    """They reach the tokens that see them and no others."""
+    rows = [(start + i % 3, n) for i, n in enumerate(CHUNKS[:9])]
+    c = Case(hq, hkv, d, block, rows, start + hq, groups=[(0, 4, start), (5, 4, start)])
+    for i, (a, n) in enumerate(rows):
+        for at, value, pool in ((n - 1, math.inf, c.v), (n // 2, NAN, c.v), (2 * n // 3, -math.inf, c.v),
+                                (3 * n // 4, NAN, c.k)):
+            p = a + at
+            b, h, f = c.table[c.rows[i, 0], p // block], i % hkv, (7 * i + at) % d
+            if pool is c.v:
+                pool[b, h, f, p % block] = value
+            elif at > 1:
+                pool[b, h, p % block, f] = value
+    c.check(c.prefix(), f"chunks behind {start} keys")
+
+
 @pytest.mark.parametrize("scale", [30.0, 1e-3, 1000.0])
 @beside
 def test_attn_large_scores(scale, far):
