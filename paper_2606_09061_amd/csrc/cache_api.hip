@@ -147,16 +147,24 @@ int by_rows(const std::vector<R>& rows, int32_t R::*item0, int64_t most, Items&&
 // as many more as leave kScoreItems workgroups.
 constexpr int kLeastChunk = 64, kMostChunk = 512;
 constexpr int64_t kScoreItems = 1024;
-// Whether one launch does both, a workgroup of 8 or 16 waves each (token, kv head):
-// where there are few pages to score, or about as many workgroups as CUs.  us, one launch
-// / two, 32/8 heads of 128, 8 (token, kv head)s: 63 pages 6.9 / 8.4, 125 8.8 / 8.6 (eager
-// 8.6 / 9.7), 188 9.2 / 8.8, 256 11.2 / 8.7; 128 of them: 63 8.3 / 9.6, 156 10.2 / 11.1, 256
-// 12.5 / 13.1; 256: 251 13.1 / 16.4, 938 28 / 36; 384: 475 34.6 / 31.1; 512: 125 20.0 / 16.2,
-// 219 24.2 / 24.9, 938 56 / 60; 1,024: 251 57 / 50.  Heads of 64, 8 of them: 219 8.0 / 8.5, 256
-// 9.2 / 8.6.
-bool in_one(int d, int64_t units, int most) {
-  if (most > kOnePages || units > 512) return false;
-  return units > 256 ? units > 448 && most > 192 : units >= 128 || most <= (d == 64 ? 224 : 128);
+// How one launch does both, a workgroup each (token, kv head), if it does: of four waves
+// for few pages or many (token, kv head)s, of 8 or 16 where there are about as many of
+// these as CUs.  us, 32/8 heads of 128, in two launches / by 4 waves / by 16, n (token, kv
+// head)s: n 8, 63 pages 8.4 / 5.9 / 6.9, 125 8.5 / 7.2 / 8.7, 188 8.8 / 8.6 / 9.1, 250 8.8 /
+// 10.0 / 10.4; n 128, 125 9.7 / 8.2 / 9.6, 250 12.1 / 12.0 / 11.9, 475 15.7 / 19.5 / 17.1;
+// n 256, 250 15.8 / 13.4 / 13.1, 475 24.5 / 21.7 / 18.9, 1,000 38.1 / 38.2 / 31.1; n 384, 250
+// 21.2 / 18.3 / 23.3, 1,000 47.5 / 52.0 / 56.0; n 512, 475 37.5 / 29.9 / 37.2; n 2,048, 125
+// 61.8 / 48.3 / 85.8.  Of uneven numbers of pages the largest sets the time: up to 500, n
+// 256 20.1 / 20.6 / 17.9, n 512 30.2 / 29.6 / 34.0; up to 1,000, n 512 47.9 / 51.0 / 54.3.
+// (By 16 waves up to 4,096: 256 x 2,000 60.6 / 56.9, uneven 62 / 73.)  64/8 heads, n 8:
+// 125 9.3 / 8.8, 188 9.6 / 10.8.  16/16 heads of 64: n 16, 250 8.3 / 6.7; n 1,024, up to
+// 1,000 50.3 / 44.0.
+One in_one(const cp_attn_desc& d, int64_t n, int most) {
+  const bool half = d.head_dim == 64, heavy = d.num_q_heads >= 8 * d.num_kv_heads;
+  if (most <= 256)
+    return n >= 112 || half || most <= (heavy ? 128 : 176) ? One::kFour256 : One::kNo;
+  if (n > 256) return most <= (half ? 1024 : 512) ? One::kFour1024 : One::kNo;
+  return n > 128 && most <= 1024 ? One::kAll1024 : One::kNo;
 }
 
 // The scores that cp_page_select keeps: rows whose tokens may have to choose.
@@ -444,11 +452,12 @@ int cp_page_select(const cp_attn_desc* desc, const void* q, const void* bounds,
                        n_last,
                        chunk};
     const auto choices = [&](const SelectRow& r) { return (int64_t)r.n * hkv; };
-    if (in_one(desc->head_dim, tokens * hkv, most))
+    const One one = in_one(*desc, tokens * hkv, most);
+    if (one != One::kNo)
       return by_rows<SelectRow, kSelectRows>(
           plan, &SelectRow::item0, kMaxItems, choices,
           [&](SelectRows& batch, int n, int items, size_t) {
-            return finish(launch_select(desc->head_dim, a, batch, n, items, s), s);
+            return finish(launch_select(desc->head_dim, a, batch, n, items, one, s), s);
           });
     scored.clear();
     for (const SelectRow& r : plan)

@@ -64,10 +64,11 @@ hipError_t launch_bounds(int d, int block, const BoundsArgs& a, const BoundsRows
                          int pages, hipStream_t s);
 hipError_t launch_score(int d, const SelectArgs& a, const SelectRows& rows, int n_rows, int items,
                         hipStream_t s);
-// scores and choice of tokens that have up to kOnePages pages
-constexpr int kOnePages = 1024;
+// scores and choice of tokens that have up to so many pages, by four waves each or by
+// as many as their registers allow
+enum class One { kNo, kFour256, kFour1024, kAll1024 };
 hipError_t launch_select(int d, const SelectArgs& a, const SelectRows& rows, int n_rows, int items,
-                         hipStream_t s);
+                         One one, hipStream_t s);
 // most: the largest number of pages of a token
 hipError_t launch_choose(const SelectArgs& a, const SelectRows& rows, int n_rows, int items,
                          int most, hipStream_t s);

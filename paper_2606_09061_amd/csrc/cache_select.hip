@@ -382,22 +382,21 @@ __global__ __launch_bounds__(NT) void choose_kernel(const Rows rows, const Selec
   choose_pages<NT, NU>(a, c.n, [&](int i) { return src[i]; }, dst);
 }
 
-// Scores and choice in one, for up to kOnePages pages a token.
+// Scores and choice in one, for up to NP pages a token.
 template <int G>
 constexpr int kOneThreads = G <= 4 ? 1024 : 512;  // (128 and 256 registers a lane)
-template <int D, int G, class Rows>
-__global__ __launch_bounds__(kOneThreads<G>) void select_kernel(
+template <int D, int G, int NT, int NP, class Rows>
+__global__ __launch_bounds__(NT, G <= 4 ? 4 : 2) void select_kernel(
     const Rows rows, const SelectArgs a, const uint16_t* __restrict__ q,
     const uint4* __restrict__ bounds, const int32_t* __restrict__ bt) {
-  constexpr int NT = kOneThreads<G>;
-  __shared__ uint64_t s_score[kOnePages];
+  __shared__ uint64_t s_score[NP];
   const Choice c = choice_of(rows, a);
   int32_t* dst = a.pages + (c.t * a.hkv + c.h) * a.n_pages;
   if (c.n <= a.n_pages) return take_all(a, c.n, dst);
   score_pages<D, G, NT / 64>(a, c.t, c.h, bt + (int64_t)c.req * a.mbr, 0, c.n, q, bounds,
                              [&](int page, uint64_t key) { s_score[page] = key; });
   __syncthreads();
-  choose_pages<NT, kOnePages / NT>(a, c.n, [&](int i) { return s_score[i]; }, dst);
+  choose_pages<NT, NP / NT>(a, c.n, [&](int i) { return s_score[i]; }, dst);
 }
 
 // Exclusive sum of x over the workgroup's threads; `total` gets the whole.
@@ -472,31 +471,41 @@ __global__ __launch_bounds__(kThreads) void choose_long_kernel(const Rows rows, 
   }
 }
 
+template <int X>
+using N = std::integral_constant<int, X>;
+
 template <int D, int G>
 hipError_t launch_score_t(const SelectArgs& a, const SelectRows& rows, int n_rows, int items,
-                          bool one, hipStream_t s) {
+                          One one, hipStream_t s) {
   return by_size(rows, n_rows, [&](const auto& r) {
-    if (one)
-      hipLaunchKernelGGL((select_kernel<D, G>), dim3(items), dim3(kOneThreads<G>), 0, s, r, a, a.q,
+    const auto both = [&](auto threads, auto pages) {
+      constexpr int NT = decltype(threads)::value, NP = decltype(pages)::value;
+      hipLaunchKernelGGL((select_kernel<D, G, NT, NP>), dim3(items), dim3(NT), 0, s, r, a, a.q,
                          (const uint4*)a.bounds, a.bt);
-    else
-      hipLaunchKernelGGL((score_kernel<D, G>), dim3(items), dim3(kThreads), 0, s, r, a, a.q,
-                         (const uint4*)a.bounds, a.bt, a.scores);
+    };
+    switch (one) {
+      case One::kFour256: return both(N<kThreads>(), N<256>());
+      case One::kFour1024: return both(N<kThreads>(), N<1024>());
+      case One::kAll1024: return both(N<kOneThreads<G>>(), N<1024>());
+      case One::kNo: break;
+    }
+    hipLaunchKernelGGL((score_kernel<D, G>), dim3(items), dim3(kThreads), 0, s, r, a, a.q,
+                       (const uint4*)a.bounds, a.bt, a.scores);
   });
 }
 
 hipError_t launch_score_g(int d, const SelectArgs& a, const SelectRows& rows, int n_rows, int items,
-                          bool one, hipStream_t s) {
+                          One one, hipStream_t s) {
   const auto f = [&](auto g) {
     constexpr int G = decltype(g)::value;
     return d == 128 ? launch_score_t<128, G>(a, rows, n_rows, items, one, s)
                     : launch_score_t<64, G>(a, rows, n_rows, items, one, s);
   };
   switch (a.hq / a.hkv) {
-    case 1: return f(std::integral_constant<int, 1>());
-    case 2: return f(std::integral_constant<int, 2>());
-    case 4: return f(std::integral_constant<int, 4>());
-    case 8: return f(std::integral_constant<int, 8>());
+    case 1: return f(N<1>());
+    case 2: return f(N<2>());
+    case 4: return f(N<4>());
+    case 8: return f(N<8>());
   }
   return hipErrorInvalidValue;
 }
@@ -505,12 +514,12 @@ hipError_t launch_score_g(int d, const SelectArgs& a, const SelectRows& rows, in
 
 hipError_t launch_score(int d, const SelectArgs& a, const SelectRows& rows, int n_rows, int items,
                         hipStream_t s) {
-  return launch_score_g(d, a, rows, n_rows, items, false, s);
+  return launch_score_g(d, a, rows, n_rows, items, One::kNo, s);
 }
 
 hipError_t launch_select(int d, const SelectArgs& a, const SelectRows& rows, int n_rows, int items,
-                         hipStream_t s) {
-  return launch_score_g(d, a, rows, n_rows, items, true, s);
+                         One one, hipStream_t s) {
+  return launch_score_g(d, a, rows, n_rows, items, one, s);
 }
 
 hipError_t launch_choose(const SelectArgs& a, const SelectRows& rows, int n_rows, int items,

@@ -369,11 +369,11 @@ def test_select_of_long_contexts_with_equal_scores(ctx, n_pages):
     s.check(n_pages, 0, 0)
 
 
-@pytest.mark.parametrize("reqs,pages", [(1, 127), (1, 128), (1, 129), (64, 100), (65, 100), (128, 60),
-                                        (32, 300), (31, 130), (129, 140), (40, 1023), (40, 1025),
-                                        (1, 224), (1, 225), (128, 192), (128, 193), (5, 33),
-                                        (112, 200), (113, 200)])
-@pytest.mark.parametrize("hq,hkv,d", [(8, 4, 64), (32, 4, 64), (16, 4, 128)])
+@pytest.mark.parametrize("reqs,pages", [
+    (1, 33), (1, 128), (1, 129), (1, 176), (1, 177), (1, 256), (1, 257), (27, 200), (28, 200), (32, 257),
+    (33, 300), (64, 256), (64, 1024), (64, 1025), (65, 257), (65, 512), (65, 513), (65, 1024), (65, 1025),
+    (300, 20)])
+@pytest.mark.parametrize("hq,hkv,d", [(8, 4, 64), (32, 4, 64), (16, 4, 128), (32, 4, 128)])
 def test_select_in_one_launch_and_in_two(reqs, pages, hq, hkv, d):
     """Around the numbers of rows and pages at which the launches change."""
     rows = [(16 * pages - 1 - 16 * (r % 3) * (pages > 3), 1) for r in range(reqs)]
