@@ -230,10 +230,13 @@ template <int D, int B>
 hipError_t launch_append_t(const AppendArgs& a, const AppendRows& rows, int n_rows, int tokens,
                            int v_items, hipStream_t s) {
   constexpr int HPW = 64 / (D / 8);
-  // Few tokens: a wave for each group of heads; many: a wave per token, whose
-  // rotation serves all of them.
+  // A wave's rotation serves about five loads of heads, or fewer where tokens are few.
+  // us, 1 / 2 / 4 / 8 waves a token: 4,096 tokens on 32/8 heads of 128, ten loads, 29.7 /
+  // 26.4 / 28.0 / -, on 64/8, eighteen, 50.5 / 40.7 / 40.4 / -, on 16/16 heads of 64, four,
+  // 13.4 / 15.5 / 17.4; 1,024 tokens on 32/8 12.4 / 9.5 / 9.4 / 11.8, on 64/8 18.6 / 12.9 /
+  // 11.8 / 13.9; 128 tokens on 64/8, 4 / 8 / 16: 7.0 / 5.8 / 6.3.
   const int groups = (a.hq + a.hkv + HPW - 1) / HPW;
-  const int parts = (int)std::min<int64_t>(groups, (4096 + tokens - 1) / tokens);
+  const int parts = std::max((groups + 4) / 5, (int)std::min<int64_t>(groups, (1024 + tokens - 1) / tokens));
   const int rope_blocks = (int)(((int64_t)tokens * parts + kWaves - 1) / kWaves);
   const int blocks = rope_blocks + (v_items + kWaves - 1) / kWaves;
   return by_size(rows, n_rows, [&](const auto& r) {
