@@ -70,11 +70,14 @@ def exported_symbols():
             "cp_prefix_attn"]
 
 
-def _pools(desc, dev, what, k_cache=None, v_cache=None):
-    """The addresses of the pools that are given."""
-    nb, hkv, d, b = desc.num_blocks, desc.num_kv_heads, desc.head_dim, desc.block_size
-    return [_ptr(t, _BF16, (nb, hkv, *page), dev, what)
-            for t, page in ((k_cache, (b, d)), (v_cache, (d, b))) if t is not None]
+def _k_pool(desc, k_cache, dev, what):
+    return _ptr(k_cache, _BF16,
+                (desc.num_blocks, desc.num_kv_heads, desc.block_size, desc.head_dim), dev, what)
+
+
+def _v_pool(desc, v_cache, dev, what):
+    return _ptr(v_cache, _BF16,
+                (desc.num_blocks, desc.num_kv_heads, desc.head_dim, desc.block_size), dev, what)
 
 
 def _table(desc, block_tables, dev, what):
@@ -98,12 +101,12 @@ def qkv_append(desc, qkv, q_norm_w, k_norm_w, rows, q, k_cache, v_cache, block_t
     rows = cp._rows(rows)
     dev, T = _device(qkv, what), _nodes(rows)
     hq, hkv, d = desc.num_q_heads, desc.num_kv_heads, desc.head_dim
-    k, v = _pools(desc, dev, what, k_cache, v_cache)
     _check(_call(dev, stream, load().cp_qkv_append, ctypes.byref(desc),
                  _ptr(qkv, _BF16, (T, (hq + 2 * hkv) * d), dev, what),
                  _ptr(q_norm_w, _BF16, (d,), dev, what), _ptr(k_norm_w, _BF16, (d,), dev, what),
                  None if positions is None else _ptr(positions, _I32, (T,), dev, what),
-                 float(theta), float(eps), _ptr(q, _BF16, (T, hq, d), dev, what), k, v,
+                 float(theta), float(eps), _ptr(q, _BF16, (T, hq, d), dev, what),
+                 _k_pool(desc, k_cache, dev, what), _v_pool(desc, v_cache, dev, what),
                  _table(desc, block_tables, dev, what), rows.tobytes(), rows.shape[0]), what)
 
 
@@ -115,7 +118,7 @@ def page_bounds(desc, k_cache, block_tables, rows, bounds, stream=None):
     dev = _device(k_cache, what)
     shape = (desc.num_blocks, desc.num_kv_heads, 2, desc.head_dim)
     _check(_call(dev, stream, load().cp_page_bounds, ctypes.byref(desc),
-                 *_pools(desc, dev, what, k_cache), _table(desc, block_tables, dev, what),
+                 _k_pool(desc, k_cache, dev, what), _table(desc, block_tables, dev, what),
                  rows.tobytes(), rows.shape[0], _ptr(bounds, _BF16, shape, dev, what)), what)
 
 
@@ -169,9 +172,9 @@ def page_attn(desc, q, k_cache, v_cache, block_tables, pages, rows, out, ws=None
     P = pages.shape[2]
     ws, ws_ptr, ws_bytes = _workspace(ws, lambda: page_attn_workspace_bytes(desc, rows, P), dev,
                                       stream, what)
-    k, v = _pools(desc, dev, what, k_cache, v_cache)
     _check(_call(dev, stream, load().cp_page_attn, ctypes.byref(desc),
-                 _ptr(q, _BF16, (T, hq, d), dev, what), k, v,
+                 _ptr(q, _BF16, (T, hq, d), dev, what), _k_pool(desc, k_cache, dev, what),
+                 _v_pool(desc, v_cache, dev, what),
                  _table(desc, block_tables, dev, what), _ptr(pages, _I32, (T, hkv, P), dev, what),
                  P, rows.tobytes(), rows.shape[0], _ptr(out, _BF16, (T, hq, d), dev, what), ws_ptr,
                  ws_bytes), what)
@@ -206,9 +209,9 @@ def prefix_attn(desc, q, k_cache, v_cache, block_tables, rows, groups, out, ws=N
     hq, d = desc.num_q_heads, desc.head_dim
     ws, ws_ptr, ws_bytes = _workspace(ws, lambda: prefix_attn_workspace_bytes(desc, rows, groups),
                                       dev, stream, what)
-    k, v = _pools(desc, dev, what, k_cache, v_cache)
     _check(_call(dev, stream, load().cp_prefix_attn, ctypes.byref(desc),
-                 _ptr(q, _BF16, (T, hq, d), dev, what), k, v,
+                 _ptr(q, _BF16, (T, hq, d), dev, what), _k_pool(desc, k_cache, dev, what),
+                 _v_pool(desc, v_cache, dev, what),
                  _table(desc, block_tables, dev, what), rows.tobytes(), rows.shape[0],
                  groups.tobytes(), groups.shape[0], _ptr(out, _BF16, (T, hq, d), dev, what), ws_ptr,
                  ws_bytes), what)
