@@ -810,6 +810,35 @@ def test_offsets_beyond_32_bits():
     torch.cuda.empty_cache()
 
 
+@pytest.mark.parametrize("seed", range(40))
+def test_random_batches(seed):
+    """Heads, rows, lengths, groups and lists of all sizes."""
+    r = np.random.default_rng(seed)
+    hq, hkv = (HEADS + [(32, 8), (16, 16), (64, 8)])[r.integers(10)]
+    d, block = int(r.choice([64, 128])), int(r.choice([16, 32]))
+    n, longest = int(2 ** r.uniform(0, 6.5)), int(2 ** r.uniform(2, 11.5))
+    longest = max(4, min(longest, 30_000_000 // (n * hkv * d)))
+    most, rows, groups = int(r.choice([1, 1, 2, 4, 9, 40])), [], []
+    while len(rows) < n:
+        count = int(min(n - len(rows), 1 + r.integers(12)))
+        common = int(r.integers(longest)) if r.random() < 0.8 else 0
+        if r.random() < 0.7:
+            groups.append((len(rows), count, common))
+        rows += [(common + int(r.integers(max(1, longest // int(r.integers(2, 13))))),
+                  int(r.integers(most + 1))) for _ in range(count)]
+    rows.append((0, 1))
+    n_pages = int(2 ** r.uniform(0, 7.5))
+    c = Case(hq, hkv, d, block, rows, seed, groups=groups)
+    c.check(c.prefix(), f"{hq}/{hkv} d {d} block {block}, {len(rows)} rows, {len(groups)} groups")
+    pages = c.lists(n_pages)
+    c.check(c.listed(pages), f"{n_pages} pages", pages)
+    first = int(r.integers(min(3, n_pages) + 1))
+    last = int(r.integers(min(3, n_pages - first) + 1))
+    Select(hq, hkv, d, block, rows, seed, pool=400).check(n_pages, first, last)
+    a = Append(hq, hkv, d, block, rows, seed)
+    assert same_bits(a.run(), a.two_calls())
+
+
 # ---------------------------------------------------------------- a round of them together
 
 def test_a_sparse_decode_round():
