@@ -6,8 +6,8 @@
 #include <cstdlib>
 #include <vector>
 
+#include "cache_batches.hpp"
 #include "cache_kernels.hpp"
-#include "cache_plan.hpp"
 #include "device.hpp"
 #include "plan.hpp"
 
@@ -119,78 +119,6 @@ int check_shared(const cp_attn_desc* d, const int32_t* bt, const cp_row_meta* ro
 
 bool pages_in_range(int32_t n_pages) { return n_pages >= 1 && n_pages <= CP_CACHE_MAX_PAGES; }
 
-// f(rows of one launch, their number, its items) for rows in batches; the places
-// behind them are no item's.  items_of(row) is the number of a row's items,
-// place(row, items before) enters that; `most` items a launch.
-template <class R, int N, class Items, class F>
-int by_rows(const std::vector<R>& rows, int32_t R::*item0, int64_t most, Items&& items_of, F&& f) {
-  for (size_t r = 0; r < rows.size();) {
-    RowsOf<R, N> batch;
-    int64_t items = 0;
-    int n = 0;
-    const size_t first = r;
-    for (; r < rows.size() && n < N; ++r) {
-      const int64_t more = items_of(rows[r]);
-      if (n > 0 && items + more > most) break;
-      batch.r[n] = rows[r];
-      batch.r[n++].*item0 = (int32_t)items;
-      items += more;
-    }
-    for (int i = n; i < N; ++i) batch.r[i] = R{}, batch.r[i].*item0 = INT_MAX;
-    const int rc = f(batch, n, (int)items, first);
-    if (rc != CP_OK) return rc;
-  }
-  return CP_OK;
-}
-
-// Pages that a workgroup scores: a turn of its waves (64 pages of head_dim 128), and
-// as many more as leave kScoreItems workgroups.
-constexpr int kLeastChunk = 64, kMostChunk = 512;
-constexpr int64_t kScoreItems = 1024;
-// How one launch does both, a workgroup each (token, kv head), if it does: of four waves
-// for few pages or many (token, kv head)s, of 8 or 16 where there are about as many of
-// these as CUs.  us, 32/8 heads of 128, in two launches / by 4 waves / by 16, n (token, kv
-// head)s: n 8, 63 pages 8.4 / 5.9 / 6.9, 125 8.5 / 7.2 / 8.7, 188 8.8 / 8.6 / 9.1, 250 8.8 /
-// 10.0 / 10.4; n 128, 125 9.7 / 8.2 / 9.6, 250 12.1 / 12.0 / 11.9, 475 15.7 / 19.5 / 17.1;
-// n 256, 250 15.8 / 13.4 / 13.1, 475 24.5 / 21.7 / 18.9, 1,000 38.1 / 38.2 / 31.1; n 384, 250
-// 21.2 / 18.3 / 23.3, 1,000 47.5 / 52.0 / 56.0; n 512, 475 37.5 / 29.9 / 37.2; n 2,048, 125
-// 61.8 / 48.3 / 85.8.  Of uneven numbers of pages the largest sets the time: up to 500, n
-// 256 20.1 / 20.6 / 17.9, n 512 30.2 / 29.6 / 34.0; up to 1,000, n 512 47.9 / 51.0 / 54.3.
-// (By 16 waves up to 4,096: 256 x 2,000 60.6 / 56.9, uneven 62 / 73.)  64/8 heads, n 8:
-// 125 9.3 / 8.8, 188 9.6 / 10.8.  16/16 heads of 64: n 16, 250 8.3 / 6.7; n 1,024, up to
-// 1,000 50.3 / 44.0.
-One in_one(const cp_attn_desc& d, int64_t n, int most) {
-  const bool half = d.head_dim == 64, heavy = d.num_q_heads >= 8 * d.num_kv_heads;
-  if (most <= 256)
-    return n >= 112 || half || most <= (heavy ? 128 : 176) ? One::kFour256 : One::kNo;
-  if (n > 256) return most <= (half ? 1024 : 512) ? One::kFour1024 : One::kNo;
-  return n > 128 && most <= 1024 ? One::kAll1024 : One::kNo;
-}
-
-// The scores that cp_page_select keeps: rows whose tokens may have to choose.
-int64_t plan_select(const cp_attn_desc& d, const cp_row_meta* rows, int32_t n_rows, int32_t n_pages,
-                    std::vector<SelectRow>& out) {
-  out.clear();
-  int64_t scores = 0;
-  int32_t tok = 0;
-  for (int32_t r = 0; r < n_rows; ++r) {
-    const cp_row_meta& m = rows[r];
-    const int32_t held = m.chunk_len == 0 ? 0 : (m.ctx_len - 1) / d.block_size + 1;
-    const int32_t stride = held > n_pages ? held : 0;
-    // a piece's workgroups of the scores fit a launch
-    const int64_t chunks = std::max(1, (stride + kLeastChunk - 1) / kLeastChunk);
-    const int32_t step =
-        (int32_t)std::max<int64_t>(1, std::min<int64_t>(kPieceTokens, kMaxItems / 2 / (chunks * d.num_kv_heads)));
-    for (int32_t j = 0; j < m.chunk_len; j += step) {
-      const int32_t n = std::min(step, m.chunk_len - j);
-      out.push_back(SelectRow{0, tok + j, n, m.chunk_start + j, m.req_id, stride, scores});
-      scores += (int64_t)n * d.num_kv_heads * stride;
-    }
-    tok += m.chunk_len;
-  }
-  return scores;
-}
-
 // One plan per thread, whose vectors keep their capacity.
 AttnPlan& thread_plan() {
   thread_local AttnPlan p;
@@ -233,59 +161,22 @@ AttnArgs attn_args(const cp_attn_desc* d, const AttnPlan& p, const void* q, cons
                   d->sm_scale * cpattn::kLog2e};
 }
 
-// The launches of a plan, each with some of the rows, the groups that begin among
-// them, and the merge of what has several pieces.
+// The launches of a plan, and the merges of what has several pieces.
 int launch_plan(const cp_attn_desc* d, const AttnPlan& p, AttnArgs a, hipStream_t s) {
-  const int hkv = d->num_kv_heads, G = d->num_q_heads / hkv, D = d->head_dim, B = d->block_size;
-  int64_t part0 = p.row_part0;
-  int begun = 0;  // groups whose workgroups have been launched
-  for (size_t r = 0; r < p.rows.size();) {
-    AttnBatch b;
-    int64_t items = 0, group_items = 0;
-    int n = 0, n_groups = 0, last = -1, most = 1;
-    bool merge = false, wide = false;
-    const size_t first = r;
-    for (; r < p.rows.size() && n < kAttnRows; ++r) {
-      const TokenRow& t = p.rows[r];
-      const int64_t more = (int64_t)t.n_split * p.items_of(t.n) * hkv;
-      const bool other = t.group >= 0 && t.group != last, fresh = other && t.group == begun;
-      const int64_t shared = fresh ? prefix_items(p.prefix[t.group], G, hkv) : 0;
-      if (n > 0 && items + group_items + more + shared > kMaxItems) break;
-      if (other) {
-        if (n_groups == kGroups) break;
-        b.g[n_groups] = p.prefix[t.group];
-        b.g[n_groups].row0 = n;
-        // (of a group that began in an earlier launch: no item, it is this one's first)
-        b.g[n_groups++].item0 = (int32_t)group_items;
-        wide |= fresh && p.prefix[t.group].wide != kNarrow;
-        group_items += shared;
-        last = t.group;
-        if (fresh) ++begun;
-      }
-      if (t.group >= 0) b.g[n_groups - 1].row1 = n + 1;
-      b.r[n++] = AttnRow{(int32_t)items, t.tok0, t.start, t.req};
-      items += more;
-      const int pieces = t.n_split + (t.group >= 0 ? p.prefix[t.group].n_split : 0);
-      merge |= t.n_split > 1 || t.group >= 0;
-      most = std::max(most, pieces);
-    }
-    const int32_t end = p.rows[r - 1].tok0 + p.rows[r - 1].n;
-    for (int i = n_groups; i < kGroups; ++i) b.g[i] = PrefixRow{}, b.g[i].item0 = INT_MAX;
-    for (int i = n; i <= kAttnRows; ++i) b.r[i] = AttnRow{INT_MAX, end, 0, 0};
-    a.part0 = (int)part0, a.n_groups = n_groups, a.group_items = (int)group_items;
-    a.items = (int)items;
-    const int per = std::max(1, 4 / p.unit_waves), all = (int)(group_items + (items + per - 1) / per);
-    const hipError_t e = a.pages    ? launch_pages(D, B, a, b, n, all, s)
-                         : !wide    ? launch_shared(D, B, a, b, n, all, s)
-                         : D == 128 ? launch_shared_wide128(B, a, b, all, s)
-                                    : launch_shared_wide64(B, a, b, all, s);
+  const int D = d->head_dim, B = d->block_size;
+  return attn_launches(*d, p, [&](const AttnLaunch& x) {
+    a.part0 = (int)x.part0, a.n_groups = x.n_groups, a.group_items = x.group_items;
+    a.items = x.items;
+    const int per = std::max(1, 4 / p.unit_waves), all = x.group_items + (x.items + per - 1) / per;
+    const hipError_t e = a.pages    ? launch_pages(D, B, a, x.b, x.n, all, s)
+                         : !x.wide  ? launch_shared(D, B, a, x.b, x.n, all, s)
+                         : D == 128 ? launch_shared_wide128(B, a, x.b, all, s)
+                                    : launch_shared_wide64(B, a, x.b, all, s);
     int rc = finish(e, s);
-    if (rc == CP_OK && merge)
-      rc = finish(launch_cache_merge(D, B, a, b, n, end - p.rows[first].tok0, most, s), s);
-    if (rc != CP_OK) return rc;
-    if (p.parts) part0 += (items * G) << p.log2_tokens;
-  }
-  return CP_OK;
+    if (rc == CP_OK && x.merge)
+      rc = finish(launch_cache_merge(*d, a, x.b, x.n, x.n_tokens, x.most, s), s);
+    return rc;
+  });
 }
 
 }  // namespace
@@ -345,7 +236,7 @@ int cp_qkv_append(const cp_attn_desc* desc, const void* qkv, const void* q_norm_
     };
     return by_rows<AppendRow, kAppendRows>(
         pieces, &AppendRow::item0, kMaxItems, items_of,
-        [&](AppendRows& batch, int n, int items, size_t) {
+        [&](AppendRows& batch, int n, int items) {
           int32_t before = 0;
           for (int i = 0; i < n; ++i) {
             batch.r[i].first = before;
@@ -385,7 +276,7 @@ int cp_page_bounds(const cp_attn_desc* desc, const void* k_cache, const int32_t*
     }
     return by_rows<Piece, kBoundsRows>(
         pieces, &Piece::item0, kMaxItems / desc->num_kv_heads, [](const Piece& p) { return p.pages; },
-        [&](RowsOf<Piece, kBoundsRows>& batch, int n, int pages, size_t) {
+        [&](RowsOf<Piece, kBoundsRows>& batch, int n, int pages) {
           BoundsRows r;
           for (int i = 0; i < kBoundsRows; ++i)
             r.r[i] = BoundsRow{batch.r[i].item0, batch.r[i].req, batch.r[i].page0, batch.r[i].ctx};
@@ -402,8 +293,9 @@ size_t cp_page_select_workspace_bytes(const cp_attn_desc* desc, const cp_row_met
     const int e = check_batch(desc, rows, n_rows, &tokens);
     if (e != CP_OK) return e;
     if (!pages_in_range(n_pages)) return CP_ERR_INVALID_ARG;
-    thread_local std::vector<SelectRow> plan;
-    bytes = std::max<size_t>(256, (size_t)plan_select(*desc, rows, n_rows, n_pages, plan) * 8);
+    thread_local SelectPlan plan;
+    plan_select(*desc, rows, n_rows, n_pages, plan);
+    bytes = std::max<size_t>(256, (size_t)plan.scores * 8);
     return CP_OK;
   });
   return rc == CP_OK ? bytes : 0;
@@ -423,20 +315,13 @@ int cp_page_select(const cp_attn_desc* desc, const void* q, const void* bounds,
     if (tokens == 0) return CP_OK;
     if (!usable(16, {q, bounds}) || !usable(4, {block_tables, pages}) || !usable(256, {ws}))
       return CP_ERR_INVALID_ARG;
-    thread_local std::vector<SelectRow> plan, scored;
-    const int64_t scores = plan_select(*desc, rows, n_rows, n_pages, plan);
-    if (ws_bytes < std::max<size_t>(256, (size_t)scores * 8)) return CP_ERR_WORKSPACE;
+    thread_local SelectPlan plan;
+    plan_select(*desc, rows, n_rows, n_pages, plan);
+    if (ws_bytes < std::max<size_t>(256, (size_t)plan.scores * 8)) return CP_ERR_WORKSPACE;
     hipStream_t s = (hipStream_t)stream;
     rc = check_tables(desc, block_tables, rows, n_rows, false, s);
     if (rc != CP_OK) return rc;
     (void)hipGetLastError();
-    const int hkv = desc->num_kv_heads;
-    int chunk = kLeastChunk, most = 0;
-    for (const SelectRow& r : plan) most = std::max(most, (r.start + r.n - 1) / desc->block_size + 1);
-    // (a token's scores fit a launch, whatever its pages and heads)
-    while ((chunk < kMostChunk && scores > 2 * chunk * kScoreItems) ||
-           (int64_t)hkv * (most / chunk + 1) > kMaxItems / 2)
-      chunk *= 2;
     const SelectArgs a{static_cast<const uint16_t*>(q),
                        static_cast<const uint16_t*>(bounds),
                        block_tables,
@@ -450,31 +335,17 @@ int cp_page_select(const cp_attn_desc* desc, const void* q, const void* bounds,
                        n_pages,
                        n_first,
                        n_last,
-                       chunk};
-    const auto choices = [&](const SelectRow& r) { return (int64_t)r.n * hkv; };
-    const One one = in_one(*desc, tokens * hkv, most);
-    if (one != One::kNo)
-      return by_rows<SelectRow, kSelectRows>(
-          plan, &SelectRow::item0, kMaxItems, choices,
-          [&](SelectRows& batch, int n, int items, size_t) {
-            return finish(launch_select(desc->head_dim, a, batch, n, items, one, s), s);
-          });
-    scored.clear();
-    for (const SelectRow& r : plan)
-      if (r.stride > 0) scored.push_back(r);
-    rc = by_rows<SelectRow, kSelectRows>(
-        scored, &SelectRow::item0, kMaxItems,
-        [&](const SelectRow& r) {
-          return (int64_t)r.n * hkv * ((r.stride + chunk - 1) / chunk);
-        },
-        [&](SelectRows& batch, int n, int items, size_t) {
+                       plan.chunk};
+    return select_launches(
+        *desc, plan,
+        [&](SelectRows& batch, int n, int items) {
           return finish(launch_score(desc->head_dim, a, batch, n, items, s), s);
-        });
-    if (rc != CP_OK) return rc;
-    return by_rows<SelectRow, kSelectRows>(
-        plan, &SelectRow::item0, kMaxItems, choices,
-        [&](SelectRows& batch, int n, int items, size_t) {
-          return finish(launch_choose(a, batch, n, items, most, s), s);
+        },
+        [&](SelectRows& batch, int n, int items) {
+          return finish(plan.one == One::kNo
+                            ? launch_choose(a, batch, n, items, plan.most, s)
+                            : launch_select(desc->head_dim, a, batch, n, items, plan.one, s),
+                        s);
         });
   });
 }

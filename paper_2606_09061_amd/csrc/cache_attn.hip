@@ -59,7 +59,8 @@ __global__ __launch_bounds__(kThreads, 2) void shared_kernel(
 template <int D, int B, bool LIST, class Batch>
 __global__ __launch_bounds__(kThreads) void cache_merge_kernel(const Batch b, const AttnArgs a,
                                                                int per_token, int share) {
-  constexpr int DQ = D / 4, SLOTS = kThreads / DQ, U = 8;
+  constexpr int DQ = D / 4, SLOTS = merge_slots(D), U = 8;
+  static_assert(SLOTS * DQ == kThreads, "merge_slots");
   __shared__ f32x4_t s_acc[SLOTS][DQ];
   __shared__ float s_m[SLOTS], s_w[SLOTS];
   const int64_t t = (int64_t)b.r[0].tok0 + (int)blockIdx.x / per_token;
@@ -162,21 +163,15 @@ hipError_t launch_shared_t(const AttnArgs& a, const AttnBatch& b, int n_rows, in
 }
 
 template <int D, int B>
-hipError_t launch_merge_t(const AttnArgs& a, const AttnBatch& b, int n_rows, int n_tokens,
-                          int most, hipStream_t s) {
-  constexpr int SLOTS = kThreads / (D / 4);
-  int share = 1;  // of eight pieces each, which a thread loads at once
-  while (share < SLOTS && share * 8 < most &&
-         (int64_t)n_tokens * a.hq * 2 * share / SLOTS < kMaxItems / 2)
-    share *= 2;
-  const int per = SLOTS / share, per_token = (a.hq + per - 1) / per;
+hipError_t launch_merge_t(const AttnArgs& a, const AttnBatch& b, int n_rows, int items,
+                          int per_token, int share, hipStream_t s) {
   return by_size(b, a.n_groups, n_rows, [&](const auto& x) {
     if (a.pages)
-      hipLaunchKernelGGL((cache_merge_kernel<D, B, true>), dim3(n_tokens * per_token),
-                         dim3(kThreads), 0, s, x, a, per_token, share);
+      hipLaunchKernelGGL((cache_merge_kernel<D, B, true>), dim3(items), dim3(kThreads), 0, s, x, a,
+                         per_token, share);
     else
-      hipLaunchKernelGGL((cache_merge_kernel<D, B, false>), dim3(n_tokens * per_token),
-                         dim3(kThreads), 0, s, x, a, per_token, share);
+      hipLaunchKernelGGL((cache_merge_kernel<D, B, false>), dim3(items), dim3(kThreads), 0, s, x,
+                         a, per_token, share);
   });
 }
 
@@ -196,11 +191,13 @@ hipError_t launch_shared(int d, int block, const AttnArgs& a, const AttnBatch& b
   return f(a, b, n_rows, items, s);
 }
 
-hipError_t launch_cache_merge(int d, int block, const AttnArgs& a, const AttnBatch& b, int n_rows,
-                              int n_tokens, int most, hipStream_t s) {
-  auto f = d == 128 ? (block == 16 ? launch_merge_t<128, 16> : launch_merge_t<128, 32>)
-                    : (block == 16 ? launch_merge_t<64, 16> : launch_merge_t<64, 32>);
-  return f(a, b, n_rows, n_tokens, most, s);
+hipError_t launch_cache_merge(const cp_attn_desc& d, const AttnArgs& a, const AttnBatch& b,
+                              int n_rows, int n_tokens, int most, hipStream_t s) {
+  const int share = merge_share(d, n_tokens, most), items = (int)merge_items(d, n_tokens, share);
+  const int per_token = (int)merge_items(d, 1, share);
+  auto f = d.head_dim == 128 ? (d.block_size == 16 ? launch_merge_t<128, 16> : launch_merge_t<128, 32>)
+                             : (d.block_size == 16 ? launch_merge_t<64, 16> : launch_merge_t<64, 32>);
+  return f(a, b, n_rows, items, per_token, share, s);
 }
 
 }  // namespace cpcache

@@ -3,7 +3,7 @@
 
 #include <hip/hip_runtime.h>
 
-#include "cache.hpp"
+#include "cache_plan.hpp"
 
 namespace cpcache {
 
@@ -64,9 +64,7 @@ hipError_t launch_bounds(int d, int block, const BoundsArgs& a, const BoundsRows
                          int pages, hipStream_t s);
 hipError_t launch_score(int d, const SelectArgs& a, const SelectRows& rows, int n_rows, int items,
                         hipStream_t s);
-// scores and choice of tokens that have up to so many pages, by four waves each or by
-// as many as their registers allow
-enum class One { kNo, kFour256, kFour1024, kAll1024 };
+// scores and choice in one
 hipError_t launch_select(int d, const SelectArgs& a, const SelectRows& rows, int n_rows, int items,
                          One one, hipStream_t s);
 // most: the largest number of pages of a token
@@ -85,7 +83,7 @@ hipError_t launch_shared_wide128(int block, const AttnArgs& a, const AttnBatch& 
                                  hipStream_t s);
 // the merge of the same batch's rows that have several pieces, `most` at most, of
 // n_tokens tokens
-hipError_t launch_cache_merge(int d, int block, const AttnArgs& a, const AttnBatch& b, int n_rows,
-                              int n_tokens, int most, hipStream_t s);
+hipError_t launch_cache_merge(const cp_attn_desc& d, const AttnArgs& a, const AttnBatch& b,
+                              int n_rows, int n_tokens, int most, hipStream_t s);
 
 }  // namespace cpcache

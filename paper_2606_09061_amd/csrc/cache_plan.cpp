@@ -1,5 +1,5 @@
-// Plans of cp_page_attn and cp_prefix_attn: the pieces of the key ranges and the
-// workspace.
+// Plans of cp_page_select, cp_page_attn and cp_prefix_attn: the pieces of the rows
+// and key ranges, and the workspace.
 #include "cache_plan.hpp"
 
 #include <algorithm>
@@ -173,7 +173,62 @@ void cut_groups(AttnPlan& out, const cp_attn_desc& d, bool wide) {
   }
 }
 
+// Pages that a workgroup scores: a turn of its waves (64 pages of head_dim 128), and
+// as many more as leave kScoreItems workgroups.
+constexpr int kLeastChunk = 64, kMostChunk = 512;
+constexpr int64_t kScoreItems = 1024;
+// How one launch does both, a workgroup each (token, kv head), if it does: of four waves
+// for few pages or many (token, kv head)s, of 8 or 16 where there are about as many of
+// these as CUs.  us, 32/8 heads of 128, in two launches / by 4 waves / by 16, n (token, kv
+// head)s: n 8, 63 pages 8.4 / 5.9 / 6.9, 125 8.5 / 7.2 / 8.7, 188 8.8 / 8.6 / 9.1, 250 8.8 /
+// 10.0 / 10.4; n 128, 125 9.7 / 8.2 / 9.6, 250 12.1 / 12.0 / 11.9, 475 15.7 / 19.5 / 17.1;
+// n 256, 250 15.8 / 13.4 / 13.1, 475 24.5 / 21.7 / 18.9, 1,000 38.1 / 38.2 / 31.1; n 384, 250
+// 21.2 / 18.3 / 23.3, 1,000 47.5 / 52.0 / 56.0; n 512, 475 37.5 / 29.9 / 37.2; n 2,048, 125
+// 61.8 / 48.3 / 85.8.  Of uneven numbers of pages the largest sets the time: up to 500, n
+// 256 20.1 / 20.6 / 17.9, n 512 30.2 / 29.6 / 34.0; up to 1,000, n 512 47.9 / 51.0 / 54.3.
+// (By 16 waves up to 4,096: 256 x 2,000 60.6 / 56.9, uneven 62 / 73.)  64/8 heads, n 8:
+// 125 9.3 / 8.8, 188 9.6 / 10.8.  16/16 heads of 64: n 16, 250 8.3 / 6.7; n 1,024, up to
+// 1,000 50.3 / 44.0.
+One in_one(const cp_attn_desc& d, int64_t n, int most) {
+  const bool half = d.head_dim == 64, heavy = d.num_q_heads >= 8 * d.num_kv_heads;
+  if (most <= 256)
+    return n >= 112 || half || most <= (heavy ? 128 : 176) ? One::kFour256 : One::kNo;
+  if (n > 256) return most <= (half ? 1024 : 512) ? One::kFour1024 : One::kNo;
+  return n > 128 && most <= 1024 ? One::kAll1024 : One::kNo;
+}
+
 }  // namespace
+
+void plan_select(const cp_attn_desc& desc, const cp_row_meta* rows, int32_t n_rows, int32_t n_pages,
+                 SelectPlan& out) {
+  const int hkv = desc.num_kv_heads;
+  out.rows.clear(), out.scores = 0, out.most = 0;
+  int32_t tok = 0;
+  for (int32_t r = 0; r < n_rows; ++r) {
+    const cp_row_meta& m = rows[r];
+    if (m.chunk_len == 0) continue;
+    const int32_t held = (m.ctx_len - 1) / desc.block_size + 1;
+    const int32_t stride = held > n_pages ? held : 0;  // 0: no token has to choose
+    out.most = std::max(out.most, held);
+    // a piece's workgroups of the scores fit a launch
+    const int64_t chunks = std::max(1, (stride + kLeastChunk - 1) / kLeastChunk);
+    const int32_t step = (int32_t)std::max<int64_t>(
+        1, std::min<int64_t>(kPieceTokens, kMaxItems / 2 / (chunks * hkv)));
+    for (int32_t j = 0; j < m.chunk_len; j += step) {
+      const int32_t n = std::min(step, m.chunk_len - j);
+      out.rows.push_back(
+          SelectRow{0, tok + j, n, m.chunk_start + j, m.req_id, stride, out.scores});
+      out.scores += (int64_t)n * hkv * stride;
+    }
+    tok += m.chunk_len;
+  }
+  out.chunk = kLeastChunk;
+  // (a token's scores fit a launch, whatever its pages and heads)
+  while ((out.chunk < kMostChunk && out.scores > 2 * out.chunk * kScoreItems) ||
+         (int64_t)hkv * (out.most / out.chunk + 1) > kMaxItems / 2)
+    out.chunk *= 2;
+  out.one = in_one(desc, (int64_t)tok * hkv, out.most);
+}
 
 bool plan_pages(const cp_attn_desc& desc, const cp_row_meta* rows, int32_t n_rows, int32_t n_pages,
                 AttnPlan& out) {

@@ -52,6 +52,30 @@ struct AttnPlan {
   int items_of(int n) const { return ((n - 1) >> log2_tokens) + 1; }
 };
 
+// How one launch of cp_page_select scores and chooses for tokens of up to so many pages,
+// by four waves each or by as many as their registers allow, if it does.
+enum class One { kNo, kFour256, kFour1024, kAll1024 };
+
+// Threads that choose from up to so many pages: they hold 4, 4 or 16 keys each, or, of
+// more, read them again in each pass.
+constexpr int kFewPages = 1024, kSomePages = 4096, kManyPages = 16384;
+constexpr int choose_threads(int most) { return most > kFewPages && most <= kManyPages ? 1024 : 256; }
+
+struct SelectPlan {
+  std::vector<SelectRow> rows;  // pieces of the rows, in the order of their tokens
+  int64_t scores = 0;           // that tokens which may have to choose keep
+  int most = 0;                 // the largest number of pages of a token
+  int chunk = 0;                // pages that a workgroup scores
+  One one = One::kNo;
+
+  int threads() const {  // of a workgroup that chooses, at most
+    return one == One::kNo ? choose_threads(most) : one == One::kAll1024 ? 1024 : 256;
+  }
+};
+
+void plan_select(const cp_attn_desc& desc, const cp_row_meta* rows, int32_t n_rows, int32_t n_pages,
+                 SelectPlan& out);
+
 // rows: valid for desc, within the limits of cp_cache.h.  Both return whether the
 // partial rows fit their index type.
 bool plan_pages(const cp_attn_desc& desc, const cp_row_meta* rows, int32_t n_rows, int32_t n_pages,
@@ -63,6 +87,22 @@ bool plan_prefix(const cp_attn_desc& desc, const cp_row_meta* rows, int32_t n_ro
 inline int64_t prefix_items(const PrefixRow& p, int group, int hkv) {
   const int tile = p.wide != kNarrow ? kWideTile : kNarrowTile;
   return ((int64_t)p.n * group + tile - 1) / tile * hkv * p.n_split;
+}
+
+// The merge's threads hold this many rows (token, q head) at a time, and `share` sets
+// of D / 4 of them take the pieces of one; a workgroup's rows are one token's.
+constexpr int merge_slots(int d) { return 1024 / d; }
+inline int64_t merge_items(const cp_attn_desc& d, int64_t n_tokens, int share) {
+  const int per = merge_slots(d.head_dim) / share;
+  return n_tokens * ((d.num_q_heads + per - 1) / per);
+}
+// For rows of up to so many pieces, of which a thread loads eight at once.
+inline int merge_share(const cp_attn_desc& d, int64_t n_tokens, int most) {
+  int share = 1;
+  while (share < merge_slots(d.head_dim) && share * 8 < most &&
+         merge_items(d, n_tokens, 2 * share) < kMaxItems / 2)
+    share *= 2;
+  return share;
 }
 
 }  // namespace cpcache

@@ -525,12 +525,13 @@ hipError_t launch_select(int d, const SelectArgs& a, const SelectRows& rows, int
 hipError_t launch_choose(const SelectArgs& a, const SelectRows& rows, int n_rows, int items,
                          int most, hipStream_t s) {
   return by_size(rows, n_rows, [&](const auto& r) {
-    if (most <= 1024)
-      hipLaunchKernelGGL((choose_kernel<256, 4>), dim3(items), dim3(256), 0, s, r, a, a.scores);
-    else if (most <= 4096)
-      hipLaunchKernelGGL((choose_kernel<1024, 4>), dim3(items), dim3(1024), 0, s, r, a, a.scores);
-    else if (most <= 16384)
-      hipLaunchKernelGGL((choose_kernel<1024, 16>), dim3(items), dim3(1024), 0, s, r, a, a.scores);
+    const auto held = [&](auto threads, auto keys) {
+      constexpr int NT = decltype(threads)::value, NU = decltype(keys)::value;
+      hipLaunchKernelGGL((choose_kernel<NT, NU>), dim3(items), dim3(NT), 0, s, r, a, a.scores);
+    };
+    if (most <= kFewPages) held(N<choose_threads(kFewPages)>(), N<4>());
+    else if (most <= kSomePages) held(N<choose_threads(kSomePages)>(), N<4>());
+    else if (most <= kManyPages) held(N<choose_threads(kManyPages)>(), N<16>());
     else
       hipLaunchKernelGGL(choose_long_kernel, dim3(items), dim3(kThreads), 0, s, r, a, a.scores);
   });
