@@ -89,6 +89,7 @@ int attn_launches(const cp_attn_desc& d, const AttnPlan& p, F&& f) {
       const bool other = t.group >= 0 && t.group != last, fresh = other && t.group == begun;
       const int64_t shared = fresh ? prefix_items(p.prefix[t.group], G, hkv) : 0;
       if (x.n > 0 && items + group_items + more + shared > kMaxItems) break;
+      if (x.n > 0 && merge_items(d, t.tok0 + t.n - tok0, 1) > kMaxItems) break;
       if (other) {
         if (x.n_groups == kGroups) break;
         x.b.g[x.n_groups] = p.prefix[t.group];

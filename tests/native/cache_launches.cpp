@@ -94,6 +94,8 @@ void check_attn(const cp_attn_desc& d, const AttnPlan& p) {
           CHECK(x.n >= 1 && x.n <= kAttnRows && x.n_groups <= kGroups);
           const int64_t per = std::max(1, 4 / p.unit_waves);
           grid(x.group_items + (x.items + per - 1) / per, 64 * std::max(4, p.unit_waves));
+          const int share = merge_share(d, x.n_tokens, x.most);
+          if (x.merge) grid(merge_items(d, x.n_tokens, share), 256);
           CHECK(x.part0 == part);
           int64_t items = 0, tok = p.rows[r].tok0;
           for (int i = 0; i < x.n; ++i, ++r) {
@@ -166,7 +168,8 @@ int main() {
     }
     check(d, rows, groups, spread(1, CP_CACHE_MAX_PAGES));
   }
-  // the ends of the ranges: launches of 1,024 threads for many (token, kv head)s
+  // the ends of the ranges: launches of 1,024 threads for many (token, kv head)s, and
+  // merges of 2^27 (token, q head)s
   for (int pages : {1000, 1025, 4096, 4097, 16384, 16385})
     for (int hkv : {73, 74, 128, 1024}) {
       const cp_attn_desc d = desc(hkv, hkv, 128, 16);
