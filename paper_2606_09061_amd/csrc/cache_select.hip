@@ -65,8 +65,8 @@ __device__ __forceinline__ void sum_step(double* u, int lane) {
 
 // Scores of pages [p0, p1) of kv head h of token t, by the NW waves of a workgroup:
 // store(page, key).  A wave takes 64 / L pages at a time, L = D / 8 lanes a page with
-// 8 features each.  With lo + hi and hi - lo of a feature,
-//     2 max(q lo, q hi) = q (lo + hi) + |q| (hi - lo):
+// 8 features each.  With lo + hi and hi - lo of a feature, whichever is the larger,
+//     2 max(q lo, q hi) = q (lo + hi) + |q| |hi - lo|:
 // two fp64 multiply-adds per head and feature.  Sums over a page's lanes are split
 // by head first, then by the U pages that the lanes have in hand.  At 4 heads a
 // group that is some 170 vector operations per 2 KB of bounds.  (On the fp64 matrix
@@ -133,7 +133,7 @@ __device__ __forceinline__ void score_pages(const SelectArgs& a, int64_t t, int 
         const double both = l + m, width = m - l;
 #pragma unroll
         for (int e = 0; e < G; ++e)
-          s[e] = __builtin_fma(fabs(qd[e][i]), width, __builtin_fma(qd[e][i], both, s[e]));
+          s[e] = __builtin_fma(fabs(qd[e][i]), fabs(width), __builtin_fma(qd[e][i], both, s[e]));
       }
       sum_step<4, G>(s, lane);
       if constexpr (L == 16) sum_step<8, H4>(s, lane);
