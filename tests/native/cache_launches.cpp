@@ -137,6 +137,20 @@ void check(const cp_attn_desc& d, const std::vector<cp_row_meta>& rows,
     check_attn(d, p);
 }
 
+// Groups of (rows, tokens in common) that take these kernels.
+void check_kinds(const cp_attn_desc& d, const std::vector<std::vector<int32_t>>& sizes) {
+  std::vector<cp_row_meta> rows;
+  std::vector<cp_prefix_group> groups;
+  for (const auto& g : sizes) {
+    groups.push_back({(int32_t)rows.size(), g[0], g[1]});
+    for (int32_t i = 0; i < g[0]; ++i) rows.push_back({(int32_t)rows.size(), g[1] + i, 1, g[1] + i + 1});
+  }
+  AttnPlan p;
+  CHECK(plan_prefix(d, rows.data(), (int)rows.size(), groups.data(), (int)groups.size(), p));
+  CHECK(p.prefix.size() == sizes.size());
+  for (size_t i = 0; i < sizes.size(); ++i) CHECK(p.prefix[i].wide == sizes[i][2]);
+}
+
 cp_attn_desc desc(int hq, int hkv, int head_dim, int block) {
   cp_attn_desc d{};
   d.num_q_heads = hq, d.num_kv_heads = hkv, d.head_dim = head_dim, d.block_size = block;
@@ -189,6 +203,12 @@ int main() {
         check(d, {{0, K - T, T, K}}, {}, 300);
         check(d, {{0, K - 1, 1, K}, {1, K - T, T - 1, K - 1}}, {{0, 2, K - T}}, 1);
       }
+  // the groups of tests/test_gpu_cache_far.py
+  check_kinds(desc(8, 1, 128, 16), {{5, 100000, kStreamed}, {17, 20003, kCached}, {3, 6001, kNarrow}});
+  check_kinds(desc(32, 4, 64, 32), {{6, 50001, kStreamed}, {20, 10000, kCached}, {4, 4005, kNarrow}});
+  check_kinds(desc(8, 8, 128, 32), {{40, 14000, kStreamed}, {130, 1700, kCached}, {3, 1800, kNarrow}});
+  check_kinds(desc(4, 2, 128, 16), {{31, 60003, kStreamed}, {70, 3000, kCached}, {5, 2040, kNarrow}});
+  check_kinds(desc(64, 8, 128, 16), {{6, 16000, kStreamed}, {20, 1700, kCached}, {2, 900, kNarrow}});
   puts("ok");
   return 0;
 }
