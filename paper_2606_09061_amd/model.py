@@ -202,6 +202,17 @@ def _scratch(nbytes, device, stream):
         return None
 
 
+def _grown(ws, nbytes, stream):
+    """A workspace of at least so many bytes: ws, or a new one that belongs to the
+    current stream, which is ``stream``.  Work on it may still use ws, whose memory
+    goes back to the stream that ws was allocated on: not before that work is done."""
+    import torch
+    if nbytes <= ws.numel():
+        return ws
+    ws.record_stream(stream)
+    return torch.empty(nbytes, dtype=torch.uint8, device=ws.device)
+
+
 def gemm(a, w, out, residual=None, stream=None, ws=None):
     """out [M, N] = a [M, K] @ w [N, K]^T (+ residual, which may be out itself),
     on the package's LDS-tiled MFMA kernel (cpl_gemm).  ``ws``: a uint8 device
@@ -495,8 +506,7 @@ class Model:
                        cache.page_select_workspace_bytes(self.desc, rows, budget))
         s = stream or torch.cuda.current_stream(self.dev)
         with torch.cuda.stream(s):
-            if need > self.ws.numel():
-                self.ws = torch.empty(need, dtype=torch.uint8, device=self.dev)
+            self.ws = _grown(self.ws, need, s)
             x = self.x[:T]
             torch.index_select(self.embed, 0, self.tokens[:T], out=x)
             if groups is not None:
@@ -517,8 +527,7 @@ class Model:
                 except cp.CpError as e:
                     if e.code != cp.CP_ERR_WORKSPACE:
                         raise
-                    self.ws = torch.empty(cp.workspace_bytes(self.desc, rows), dtype=torch.uint8,
-                                          device=self.dev)
+                    self.ws = _grown(self.ws, cp.workspace_bytes(self.desc, rows), s)
                     plan = cp.attn_prepare(self.desc, rows, self.ws, stream=s)
 
                 def attend(q, kc, vc, bounds, out):
@@ -551,8 +560,7 @@ class Model:
                    gemm_workspace_bytes(T, c.hidden, c.inter),
                    gemm_workspace_bytes(n_head, c.vocab, c.hidden)
                    if self.lm_head is not None else 0)
-        if need > self.ws_gemm.numel():
-            self.ws_gemm = torch.empty(need, dtype=torch.uint8, device=self.dev)
+        self.ws_gemm = _grown(self.ws_gemm, need, s)
         for L, kc, vc, bounds in zip(self.layers, self.kc, self.vc,
                                      self.bounds or [None] * len(self.layers)):
             rmsnorm(x, L["in_norm"], h, c.eps, s)
@@ -609,8 +617,7 @@ class Model:
                 words = -(-int(rows[:, 2].max()) // 64)
                 mask = torch.empty(T, words, dtype=torch.int64, device=self.dev)
                 tree.layout(parents, rows, mask, self.pos[:T], s)
-                if need > self.ws.numel():
-                    self.ws = torch.empty(need, dtype=torch.uint8, device=self.dev)
+                self.ws = _grown(self.ws, need, s)
                 x, h = self.x[:T], self.h[:T]
                 torch.index_select(self.embed, 0, tokens, out=x)
                 self._layers(rows, T, T, s,
