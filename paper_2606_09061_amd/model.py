@@ -532,7 +532,7 @@ class Model:
 
                 def attend(q, kc, vc, bounds, out):
                     cp.attn_run(plan, q, kc, vc, self.bt, out, self.ws, stream=s)
-            self._layers(rows, T, int((rows[:, 2] > 0).sum()), s, attend)
+            self._layers(rows, T, int((rows[:, 2] > 0).sum()), s, attend, page_bounds=self.bounds)
             if self.lm_head is None:
                 return None
             last = torch.from_numpy(np.cumsum(rows[:, 2]).astype(np.int64) - 1)
@@ -543,10 +543,11 @@ class Model:
             project(hl, self.lm_head, logits, None, s, self.ws_gemm)
             return torch.argmax(logits, dim=-1)
 
-    def _layers(self, rows, T, n_head, s, attend, positions=None):
+    def _layers(self, rows, T, n_head, s, attend, positions=None, page_bounds=None):
         """The decoder layers over the embeddings in x[:T] on stream ``s``: K/V
-        appended, rotated to the tokens' own positions or to ``positions``, and
-        ``attend(q, kc, vc, bounds, out)`` for the attention.  The projections'
+        appended, rotated to the tokens' own positions or to ``positions``, the
+        written pages' bounds taken where each layer's ``page_bounds`` are given,
+        and ``attend(q, kc, vc, bounds, out)`` for the attention.  The projections'
         workspace is grown for ``n_head`` rows of the LM head too."""
         import torch
 
@@ -562,7 +563,7 @@ class Model:
                    if self.lm_head is not None else 0)
         self.ws_gemm = _grown(self.ws_gemm, need, s)
         for L, kc, vc, bounds in zip(self.layers, self.kc, self.vc,
-                                     self.bounds or [None] * len(self.layers)):
+                                     page_bounds or [None] * len(self.layers)):
             rmsnorm(x, L["in_norm"], h, c.eps, s)
             project_attn(h, L["qkv"], qkv, None, s, self.ws_gemm)
             cache.qkv_append(self.desc, qkv, L["q_norm"], L["k_norm"], rows, q, kc, vc, self.bt,
@@ -629,7 +630,8 @@ class Model:
             tree.verify(logits, tokens, parents, rows, target, path, n_accepted, after, stream=s)
             if T > 0:
                 tree.kv_compact(pools, self.bt, rows, path, n_accepted, s)
-                for kc, bounds in zip(self.kc, self.bounds or ()):   # of the pages moved into
+                # of all nodes' pages, into which the accepted ones have been moved
+                for kc, bounds in zip(self.kc, self.bounds or ()):
                     cache.page_bounds(self.desc, kc, self.bt, rows, bounds, s)
         return target, path, n_accepted, after
 
