@@ -74,7 +74,8 @@ int cp_page_bounds(const cp_attn_desc *desc, const void *k_cache, const int32_t 
                    const cp_row_meta *rows, int32_t n_rows, void *bounds, void *stream);
 
 /* Workspace bytes cp_page_select needs for this batch, or 0 if the arguments
- * are invalid. */
+ * are invalid.  They serve every batch that leaves out some of its rows or
+ * tokens, too. */
 size_t cp_page_select_workspace_bytes(const cp_attn_desc *desc, const cp_row_meta *rows,
                                       int32_t n_rows, int32_t n_pages);
 
@@ -98,7 +99,9 @@ int cp_page_select(const cp_attn_desc *desc, const void *q, const void *bounds,
                    size_t ws_bytes, void *stream);
 
 /* Workspace bytes cp_page_attn needs for this batch, or 0 if the arguments are
- * invalid. */
+ * invalid.  Few lists are cut into pieces and merged, many are not: a smaller
+ * batch can need more.  max(256, (4 D + 4) Hq T ceil(n_pages B / 256)) bytes serve
+ * every batch of up to T tokens. */
 size_t cp_page_attn_workspace_bytes(const cp_attn_desc *desc, const cp_row_meta *rows,
                                     int32_t n_rows, int32_t n_pages);
 
@@ -123,7 +126,10 @@ typedef struct {
 } cp_prefix_group;
 
 /* Workspace bytes cp_prefix_attn needs for this batch, or 0 if the arguments
- * are invalid. */
+ * are invalid.  As for cp_page_attn, a smaller batch can need more.
+ * max(256, (4 D + 4) Hq T (floor(N / 256) + 2)) bytes serve every batch of up to T
+ * tokens whose contexts have up to N keys, if no row has more than one token;
+ * 16 Hkv / Hq times as many every other one. */
 size_t cp_prefix_attn_workspace_bytes(const cp_attn_desc *desc, const cp_row_meta *rows,
                                       int32_t n_rows, const cp_prefix_group *groups,
                                       int32_t n_groups);

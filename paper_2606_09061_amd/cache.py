@@ -153,6 +153,7 @@ def page_select(desc, q, bounds, block_tables, rows, pages, n_first=1, n_last=1,
 
 
 def page_attn_workspace_bytes(desc, rows, n_pages) -> int:
+    """Of this batch: a smaller one can need more (cp_cache.h states what serves all)."""
     rows, what = cp._rows(rows), "cp_page_attn_workspace_bytes"
     lib, d, r, n = load(), ctypes.byref(desc), rows.tobytes(), rows.shape[0]
     _want(1 <= n_pages <= MAX_PAGES, f"{what}: 1 to {MAX_PAGES} pages")
@@ -185,6 +186,7 @@ def _groups(groups):
 
 
 def prefix_attn_workspace_bytes(desc, rows, groups) -> int:
+    """Of this batch: a smaller one can need more (cp_cache.h states what serves all)."""
     rows, groups = cp._rows(rows), _groups(groups)
     lib, d = load(), ctypes.byref(desc)
     batch = rows.tobytes(), rows.shape[0], groups.tobytes(), groups.shape[0]
