@@ -1,8 +1,9 @@
 """Builds, in-tree, libcpattn.so (the attention step: HIP kernels + C ABI,
 gfx950, hipcc), libcplayer.so (the element-wise kernels of the decoder layer
 around it, gfx950), libcptree.so (drafted trees and forks over the cache, gfx950),
-libcpcache.so (long and shared contexts over the cache, gfx950), libcppeaks.so (peak-rate microbenchmarks, gfx950) and libcpsched.so (the host
-scheduler, plain C++17, g++)."""
+libcpcache.so (long and shared contexts over the cache, gfx950), libcppeaks.so
+(peak-rate microbenchmarks, gfx950) and libcpsched.so (the host scheduler, plain
+C++17, g++)."""
 
 from __future__ import annotations
 

@@ -476,10 +476,11 @@ class Model:
 
         ``groups`` [(first row, rows, tokens in common)]: the rows of a group share
         the pages of their first tokens (tree.kv_fork), which are read once for
-        all of them; for iterations of decode rows and short chunks.  ``budget``:
-        every token attends to so many pages of each kv head instead of all, the
-        first, the last and those whose bounds promise most (``page_bounds`` has
-        to be kept); for iterations of decode rows."""
+        all of them; for iterations of decode rows and short chunks (a long one
+        has its keys read anew for every 2 to 16 of its tokens).  ``budget``: every
+        token attends to so many pages of each kv head instead of all, the first,
+        the last and those whose bounds promise most (``page_bounds`` has to be
+        kept); for iterations of decode rows."""
         import torch
 
         from . import cache
